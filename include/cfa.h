@@ -28,8 +28,8 @@
  *   - The return value is a cfa_status: CFA_OK (0) on success, a negative CFA_ERR_* code
  *     otherwise.  No function aborts, throws, traps the GPU or spins without a bound.
  *   - cfa_last_error(plan) gives a human-readable detail of the last failure on that plan;
- *     cfa_last_error(NULL) gives the detail of the last failure of cfa_plan_create or of the
- *     checkpoint-file functions on the calling thread.
+ *     cfa_last_error(NULL) gives the detail of the last failure of cfa_plan_create, of the
+ *     checkpoint-file functions or of the operators on the calling thread.
  *   - "device pointer" means an address in the global memory of the plan's CUDA device;
  *     "host pointer" means ordinary process memory.
  *   - Streams are CUDA runtime streams (cudaStream_t); NULL is the legacy default stream.
@@ -585,6 +585,151 @@ cfa_status cfa_segment_range(uint64_t blob_bytes, uint64_t chunk_bytes, int32_t 
                              int32_t rank, uint32_t chunk, uint64_t *blob_offset,
                              uint64_t *bytes);
 
+/* ---- operators on the loaded layout -------------------------------------------------------- */
+
+/*
+ * What a serving engine runs next on the parameters that a load has written: the matrix product
+ * with a weight in its fused layout, the choice of experts per token, and the products with
+ * stacked experts.  The paper has no counterpart.  They are forward passes for serving.
+ *
+ * Conventions of the operators, beside those above:
+ *   - the calls only enqueue on `stream` (a stream of the calling thread's current device), after
+ *     all work enqueued on it before; they allocate nothing and read nothing back.  The structs
+ *     may be changed once a call returns.  Wait for a load with cfa_wait_layer(plan, l, stream, ..)
+ *     and the operators on that stream see its parameters;
+ *   - matrices are row-major with a row stride in elements (>= the row's length where there is more
+ *     than one row); dtype is BF16 or F16 where not said otherwise, the same for x and the weights;
+ *   - products and sums are held in fp32; results are rounded to nearest even, once, to y's dtype;
+ *   - zero tokens are valid and write nothing;
+ *   - infinities and NaN go through the formulas; nothing reads outside the matrices, whatever the
+ *     values (of ids too);
+ *   - cfa_last_error(NULL) on the calling thread gives the detail of a refusal.
+ * Errors of all three: CFA_ERR_INVAL (NULL pointer, size or stride out of range, unknown constant,
+ * workspace too small), CFA_ERR_DTYPE (dtype not supported there), CFA_ERR_ALIGN, CFA_ERR_OVERLAP
+ * (y overlaps an input; y may be the residual itself, same address and stride), CFA_ERR_CUDA.
+ */
+#define CFA_ACT_NONE      0
+#define CFA_ACT_RELU      1
+#define CFA_ACT_GELU      2 /* v Phi(v), Phi by the error function */
+#define CFA_ACT_GELU_TANH 3 /* 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) */
+#define CFA_ACT_SILU      4 /* v / (1 + exp(-v)) */
+
+#define CFA_LINEAR_GATED 0x1u /* w holds gate rows, then as many up rows (a fused gate_up weight) */
+
+/*
+ * y = act(x w^T + bias) + residual; with CFA_LINEAR_GATED and w = [g; u]:
+ * y = act(x g^T + bias_g) * (x u^T + bias_u) + residual.
+ *
+ *   x         [tokens, cols], w [rows, cols]; rows even when gated
+ *   bias      [rows] of bias_dtype (dtype or F32), or NULL
+ *   y         [tokens, rows] ([tokens, rows / 2] when gated) of y_dtype (dtype or F32)
+ *   residual  as y, of y_dtype, or NULL
+ *   workspace device memory of cfa_linear_workspace() bytes, 256-byte aligned (NULL where that is
+ *             0: x and w at multiples of 16 bytes with row strides that are such multiples).  An
+ *             operand off the 16-byte grid is copied there onto it by each call
+ * All pointers are multiples of their element size.
+ */
+typedef struct cfa_linear_args {
+    const void *x, *w, *bias, *residual;
+    void *y;
+    void *workspace;
+    uint64_t workspace_bytes;
+    int64_t tokens, rows, cols;
+    int64_t x_stride, w_stride, residual_stride, y_stride;
+    int32_t dtype, bias_dtype, y_dtype;
+    int32_t activation; /* CFA_ACT_* */
+    uint32_t flags;     /* CFA_LINEAR_* */
+    int32_t reserved;   /* 0 */
+} cfa_linear_args;
+
+/* Workspace bytes that cfa_linear_async needs for these arguments (host-only; the pointers count
+ * for their alignment alone). */
+cfa_status cfa_linear_workspace(const cfa_linear_args *args, uint64_t *bytes);
+cfa_status cfa_linear_async(const cfa_linear_args *args, cfa_stream stream);
+
+#define CFA_SCORE_SOFTMAX 0
+#define CFA_SCORE_SIGMOID 1
+#define CFA_ROUTE_RENORMALIZE 0x1u
+#define CFA_ROUTE_MAX_EXPERTS 1024
+#define CFA_ROUTE_MAX_TOP_K   32
+
+/*
+ * Chooses top_k experts for each token and their weights.
+ *
+ *   score    softmax over the token's logits, or sigmoid(v) = 1 / (1 + exp(-v)), in fp32
+ *   key      what the choice goes by: score + bias; without a bias softmax goes by the logit itself
+ *            (the same order, and no two logits tie by rounding)
+ *   groups   with groups > 1 the experts form that many groups of neighbours, and only those of
+ *            the top_groups best groups can be chosen.  A group's rank is its best key with
+ *            softmax, the sum of its two best keys with sigmoid (groups of one: the key)
+ *   choice   the top_k largest keys in descending order; of equal ones (keys, groups) the lowest
+ *            index comes first
+ *   weights  the scores (without bias) of the chosen experts; with CFA_ROUTE_RENORMALIZE divided by
+ *            their sum (for softmax: the softmax of the chosen logits); times scale
+ *
+ * An expert whose logit or key is -inf or NaN is not available.  Where fewer than top_k are, the
+ * places left hold id -1 and weight 0; with sigmoid, weights whose sum is 0 stay 0.  A NaN or +inf
+ * logit makes its token's softmax weights NaN, as the formula does (and with a bias every key, so
+ * that no expert is available to it).
+ */
+typedef struct cfa_route_args {
+    const void *logits;  /* [tokens, experts] of dtype (BF16, F16 or F32) */
+    const float *bias;   /* [experts], or NULL */
+    float *weights;      /* [tokens, top_k], contiguous */
+    int32_t *ids;        /* [tokens, top_k], contiguous */
+    int64_t tokens, logits_stride;
+    int32_t experts;     /* 1 .. CFA_ROUTE_MAX_EXPERTS */
+    int32_t top_k;       /* 1 .. min(experts, CFA_ROUTE_MAX_TOP_K) */
+    int32_t groups;      /* >= 1, divides experts; at most 32 */
+    int32_t top_groups;  /* 1 .. groups */
+    int32_t dtype;
+    int32_t scoring;     /* CFA_SCORE_* */
+    uint32_t flags;      /* CFA_ROUTE_* */
+    float scale;
+} cfa_route_args;
+cfa_status cfa_route_async(const cfa_route_args *args, cfa_stream stream);
+
+#define CFA_EXPERTS_GATED 0x1u /* w13 holds gate and up rows (the loader's w13) */
+#define CFA_EXPERTS_MAX   1024
+
+/*
+ * The experts' products: for every token t
+ *   y_t = residual_t + sum over j of weights[t, j] * D_e act(G_e x_t) * (U_e x_t),  e = ids[t, j]
+ * with [G_e; U_e] = w13[e - first_expert] and D_e = w2[e - first_expert]; without CFA_EXPERTS_GATED
+ * w13 is [experts, inter, hidden] and the product with U_e falls away.  Ids outside
+ * [first_expert, first_expert + experts) -- another expert-parallel rank's, or -1 -- add nothing and
+ * their weights are not read; a token with no other ids gets its residual, or zeros.
+ *
+ *   x         [tokens, hidden];  y, residual [tokens, hidden] of dtype
+ *   w13       [experts, 2 * inter, hidden] ([experts, inter, hidden] when not gated), contiguous
+ *   w2        [experts, hidden, inter], contiguous
+ *   ids       [tokens, top_k] int32, contiguous;  weights [tokens, top_k] fp32, contiguous
+ *   workspace device memory of cfa_experts_workspace() bytes, 256-byte aligned; calls that may
+ *             overlap need their own
+ * hidden and inter are multiples of 8 and w13 and w2 of 16 bytes (CFA_ERR_ALIGN).  The activated
+ * values are rounded once to dtype between the two products; experts are summed in fp32.
+ */
+typedef struct cfa_experts_args {
+    const void *x, *w13, *w2, *residual;
+    const int32_t *ids;
+    const float *weights;
+    void *y;
+    void *workspace;
+    uint64_t workspace_bytes;
+    int64_t tokens, hidden, inter;
+    int64_t x_stride, residual_stride, y_stride;
+    int32_t experts;      /* 1 .. CFA_EXPERTS_MAX */
+    int32_t first_expert; /* >= 0 */
+    int32_t top_k;        /* 1 .. CFA_ROUTE_MAX_TOP_K */
+    int32_t dtype;
+    int32_t activation;   /* CFA_ACT_* */
+    uint32_t flags;       /* CFA_EXPERTS_* */
+} cfa_experts_args;
+
+/* Workspace bytes that cfa_experts_async needs for these sizes (host-only). */
+cfa_status cfa_experts_workspace(const cfa_experts_args *args, uint64_t *bytes);
+cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
+
 /* Zeroes the plan's checksum buffer on `stream`. */
 cfa_status cfa_reset_checksums(cfa_plan *plan, cfa_stream stream);
 
@@ -613,8 +758,8 @@ const char *cfa_last_error(const cfa_plan *plan);
 const char *cfa_status_name(cfa_status st);
 
 /* sizeof of the ABI struct with this name ("cfa_tensor_entry", "cfa_dst", "cfa_plan_opts",
- * "cfa_source", "cfa_stats", "cfa_piece", "cfa_st_tensor", "cfa_chunk_times"), or 0 for an
- * unknown name; lets a binding check its
+ * "cfa_source", "cfa_stats", "cfa_piece", "cfa_st_tensor", "cfa_chunk_times", "cfa_linear_args",
+ * "cfa_route_args", "cfa_experts_args"), or 0 for an unknown name; lets a binding check its
  * own copies of the layouts.  Host-only. */
 size_t cfa_abi_sizeof(const char *type_name);
 

@@ -12,6 +12,9 @@ memory and streams only, and is imported lazily.
     plan.wait_layer(3)                       # readiness group 3 Loaded
     plan.wait_layer()                        # whole load
     ck = plan.checksums()
+
+linear, route and experts compute with what a load has written (ops.py): the product with a fused
+weight, the choice of experts, the products with stacked experts.
 """
 import contextlib
 import ctypes
@@ -22,9 +25,11 @@ import numpy as np
 
 from . import _lib
 from ._lib import ALL, DTYPE, ENTRY_DTYPE, DST_DTYPE, PIECE_DTYPE  # noqa: F401
+from .ops import experts, linear, route
 
 __all__ = ["Plan", "Source", "FileSource", "Safetensors", "StTensor", "CfaError", "make_entries",
-           "make_dsts", "ALL", "library_path", "segment_range", "AllGather"]
+           "make_dsts", "ALL", "library_path", "segment_range", "AllGather", "linear", "route",
+           "experts"]
 
 
 class CfaError(RuntimeError):

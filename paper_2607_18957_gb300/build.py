@@ -18,7 +18,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libcfa.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-CU_SOURCES = ["cfa_unpack.cu", "cfa_bulk.cu", "cfa_runtime.cu", "cfa_noalloc.cu"]
+CU_SOURCES = ["cfa_unpack.cu", "cfa_bulk.cu", "cfa_runtime.cu", "cfa_noalloc.cu", "cfa_ops.cu",
+              "cfa_route.cu", "cfa_sort.cu", "cfa_matmul.cu"]
 C_SOURCES = ["cfa_plan.c", "cfa_files.c"]
 
 
@@ -29,7 +30,7 @@ def _nvcc():
 
 def _sources():
     return [os.path.join(CSRC, f) for f in CU_SOURCES + C_SOURCES +
-            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh"]] + \
+            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h"]] + \
         [os.path.join(INCLUDE, "cfa.h")]
 
 

@@ -1,0 +1,72 @@
+/*
+ * Internal interface of the operators on the loaded layout: what their entry points (cfa_ops.cu)
+ * hand to the kernels of the products (cfa_matmul.cu), of the choice of experts (cfa_route.cu) and
+ * of the sorting of tokens by expert (cfa_sort.cu).  Not part of the C ABI.
+ */
+#ifndef CFA_OPS_H
+#define CFA_OPS_H
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cfa.h"
+#include "cfa_internal.h"
+
+/*
+ * y = act(x w^T + bias) + residual for one or several groups of x's rows, each with its own w.
+ *
+ * One group: `tokens` rows of x.  Several (n_groups > 1 or offs given): group g owns the rows
+ * [offs[g], offs[g + 1]) of x, y and residual (offs in device memory, offs[n_groups] <= tokens), and
+ * its weight starts at row g * w_rows of w.
+ * gated: w holds w_rows / 2 gate rows and as many up rows, y has w_rows / 2 columns.
+ */
+typedef struct cfa_matmul {
+    const void *x, *w, *bias, *residual;
+    void *y;
+    const int32_t *offs;
+    int64_t tokens, w_rows, cols;
+    int64_t x_stride, w_stride, r_stride, y_stride; /* elements */
+    int32_t n_groups;
+    int32_t f16;      /* 1: binary16, 0: bf16 (x, w; bias, residual and y unless f32) */
+    int32_t bias_f32, y_f32;
+    int32_t act, gated;
+    int32_t busy;     /* groups that can hold rows at all (host's bound) */
+} cfa_matmul;
+
+/* The pairs (token, choice) sorted by expert. */
+typedef struct cfa_sort {
+    const int32_t *ids; /* [pairs] */
+    int64_t pairs;
+    int32_t top_k, first, experts;
+    int32_t *hist;      /* [blocks, experts], for more than one block */
+    int32_t *offs;      /* [experts + 1] out: where each expert's rows start */
+    int32_t *place;     /* [pairs] out: a pair's row, -1 if its expert is elsewhere */
+    int32_t *token;     /* [pairs] out: the token of each row */
+} cfa_sort;
+
+/* All of these enqueue on `stream` and return a CUDA error. `early`: may start before the kernel
+ * before it on the stream has ended, and waits inside; `release`: its dependents may do so. */
+cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream);
+cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream);
+int64_t cfa_sort_blocks(int64_t pairs);
+cudaError_t cfa_launch_sort(const cfa_sort *s, cudaStream_t stream);
+/* Rows token[r] of x into rows r of xs, for r < offs[experts]. */
+cudaError_t cfa_launch_gather(const void *x, int64_t x_stride, int64_t hidden, const int32_t *token,
+                              const int32_t *rows, int64_t most, void *xs, int64_t xs_stride,
+                              cudaStream_t stream);
+/* y[t] = residual[t] + sum_j weights[t, j] part[place[t, j]]. */
+typedef struct cfa_combine {
+    const float *part; /* [rows, hidden] */
+    const float *weights;
+    const int32_t *place;
+    const void *residual;
+    void *y;
+    int64_t tokens, hidden, r_stride, y_stride;
+    int32_t top_k, f16;
+} cfa_combine;
+cudaError_t cfa_launch_combine(const cfa_combine *c, cudaStream_t stream);
+/* Rows of cols 2-byte elements onto rows of to_stride elements, the rest of each row zeros. */
+cudaError_t cfa_launch_realign(const void *from, int64_t from_stride, int64_t rows, int64_t cols,
+                               void *to, int64_t to_stride, cudaStream_t stream);
+
+#endif /* CFA_OPS_H */

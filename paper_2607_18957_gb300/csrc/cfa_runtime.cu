@@ -1481,6 +1481,9 @@ size_t cfa_abi_sizeof(const char *type_name)
     if (!std::strcmp(type_name, "cfa_piece")) return sizeof(cfa_piece);
     if (!std::strcmp(type_name, "cfa_st_tensor")) return sizeof(cfa_st_tensor);
     if (!std::strcmp(type_name, "cfa_chunk_times")) return sizeof(cfa_chunk_times);
+    if (!std::strcmp(type_name, "cfa_linear_args")) return sizeof(cfa_linear_args);
+    if (!std::strcmp(type_name, "cfa_route_args")) return sizeof(cfa_route_args);
+    if (!std::strcmp(type_name, "cfa_experts_args")) return sizeof(cfa_experts_args);
     return 0;
 }
 
