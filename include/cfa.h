@@ -730,6 +730,15 @@ typedef struct cfa_experts_args {
 cfa_status cfa_experts_workspace(const cfa_experts_args *args, uint64_t *bytes);
 cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
 
+/*
+ * The products wait for their own loads and for one another inside a kernel, each time with a limit.
+ * Returns CFA_OK if no wait has run out on the current device since the last call, CFA_ERR_DEVICE if
+ * one has (the results since then are not valid), CFA_ERR_SUSPECT if loads in flight did not end
+ * either (see there); then clears the record.  Call it after the streams in question have been
+ * waited for; it reads one word from the device.
+ */
+cfa_status cfa_op_status(void);
+
 /* Zeroes the plan's checksum buffer on `stream`. */
 cfa_status cfa_reset_checksums(cfa_plan *plan, cfa_stream stream);
 

@@ -25,11 +25,11 @@ import numpy as np
 
 from . import _lib
 from ._lib import ALL, DTYPE, ENTRY_DTYPE, DST_DTYPE, PIECE_DTYPE  # noqa: F401
-from .ops import experts, linear, route
+from .ops import experts, linear, op_status, route
 
 __all__ = ["Plan", "Source", "FileSource", "Safetensors", "StTensor", "CfaError", "make_entries",
            "make_dsts", "ALL", "library_path", "segment_range", "AllGather", "linear", "route",
-           "experts"]
+           "experts", "op_status"]
 
 
 class CfaError(RuntimeError):

@@ -127,6 +127,7 @@ SIGNATURES = {
     "cfa_route_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_experts_workspace": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_experts_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_op_status": (ctypes.c_int, []),
 }
 
 _lib = None

@@ -399,3 +399,14 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     if (!e) e = cfa_launch_combine(&c, stream);
     return cuda_result("cfa_experts", e);
 }
+
+extern "C" cfa_status cfa_op_status(void)
+{
+    int word = 0;
+    const cudaError_t e = cfa_matmul_status(&word);
+    if (e) return cuda_result("cfa_op_status", e);
+    if (!word) return CFA_OK;
+    return refuse(word == 1 ? CFA_ERR_DEVICE : CFA_ERR_SUSPECT,
+                  word == 1 ? "a product's wait ran out: its result is not valid"
+                            : "a product's wait ran out, and loads in flight did not end");
+}

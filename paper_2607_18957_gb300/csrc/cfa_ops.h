@@ -47,6 +47,8 @@ typedef struct cfa_sort {
 /* All of these enqueue on `stream` and return a CUDA error. `early`: may start before the kernel
  * before it on the stream has ended, and waits inside; `release`: its dependents may do so. */
 cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream);
+/* The current device's word of waits that ran out (0: none), cleared. */
+cudaError_t cfa_matmul_status(int *word);
 cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream);
 int64_t cfa_sort_blocks(int64_t pairs);
 cudaError_t cfa_launch_sort(const cfa_sort *s, cudaStream_t stream);

@@ -10,7 +10,7 @@ import struct
 
 from . import _lib
 
-__all__ = ["linear", "route", "experts"]
+__all__ = ["linear", "route", "experts", "op_status"]
 
 ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 SCORING = {"softmax": 0, "sigmoid": 1}
@@ -303,3 +303,10 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
         _check(lib, lib.cfa_experts_async(
             pack(workspace.data_ptr(), workspace.numel() * workspace.element_size()), handle))
     return out
+
+
+def op_status():
+    """Raises CfaError if a wait inside a product's kernel has run out on the current device since the
+    last call (the results since then are not valid).  Call it after waiting for the streams."""
+    lib = _lib.load()
+    _check(lib, lib.cfa_op_status())

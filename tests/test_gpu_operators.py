@@ -27,6 +27,13 @@ def cuda_device():
     torch.cuda.set_device(0)
 
 
+@pytest.fixture(autouse=True)
+def no_wait_ran_out(cuda_device):
+    yield
+    torch.cuda.synchronize()
+    cfa.op_status()
+
+
 def gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
