@@ -36,10 +36,11 @@ namespace {
 
 constexpr int kThreads = 192;
 constexpr int kLoader = 4, kIssuer = 5;  /* warps; 0 to 3 are the epilogue's */
-constexpr uint32_t kRows = 128;          /* weight rows per CTA */
-constexpr uint32_t kDepth = 64;          /* columns of w and x per stage: one 128-byte swizzle row */
+constexpr uint32_t kRows = 128;          /* weight rows per CTA, at most */
+constexpr uint32_t kDepth = 64;          /* columns of w and x per block: one 128-byte swizzle row */
+constexpr uint32_t kDeepBytes = 49152;   /* a stage takes more than one block up to this */
 constexpr uint32_t kRowBytes = kDepth * 2;
-constexpr uint32_t kMaxStages = 12;
+constexpr uint32_t kMaxStages = 32;
 constexpr uint32_t kSmem = 232448;       /* all that a CTA may have: one CTA per SM, so that the
                                             tensor memory is never asked for twice at once */
 constexpr uint32_t kBand = 16;           /* token tiles that share a weight tile in turn */
@@ -51,12 +52,17 @@ struct Args {
     cfa_matmul m;
     int64_t outs;        /* columns of y */
     uint32_t bn;         /* token tile */
+    uint32_t x_box;      /* rows of x per load */
+    uint32_t fr;         /* weight rows per CTA: a multiple of 8, gated of 32 */
     uint32_t stages;
-    uint32_t steps;      /* of kDepth columns */
+    uint32_t deep;       /* blocks of kDepth columns per stage */
+    uint32_t wide;       /* one load brings a stage's blocks of w (and of x if x_box is all of it) */
+    uint32_t steps;      /* blocks in all */
     uint32_t f_tiles;    /* feature tiles per group */
     uint32_t split;      /* CTAs per output tile along the columns */
     uint32_t tmem_cols;
     uint32_t release;
+    uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
 
 __device__ int g_status; /* 1: a wait ran out, 2: and so did the wait for the loads in flight */
@@ -77,33 +83,32 @@ __device__ __forceinline__ uint32_t smem_addr(const void *p)
     return (uint32_t)__cvta_generic_to_shared(p);
 }
 
-__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)
+/* Barriers go by their shared-memory address. */
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
 {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count)
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                  : "memory");
 }
 
-__device__ __forceinline__ void mbar_expect_tx(uint64_t *bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)),
-                 "r"(bytes)
-                 : "memory");
-}
-
-__device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, uint32_t parity)
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done)
-                 : "r"(smem_addr(bar)), "r"(parity)
+                 : "r"(bar), "r"(parity)
                  : "memory");
     return done != 0;
 }
 
 /* Waits for phase `parity`; false if the limit ran out here or in another warp of the CTA. */
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, Shared *s)
+__device__ __noinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, Shared *s)
 {
     for (uint32_t k = 0; k < kSpinLimit; ++k) {
         if (mbar_try_wait(bar, parity)) return true;
@@ -111,6 +116,21 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, Shared
     }
     *(volatile int *)&s->dead = 1;
     return false;
+}
+
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, Shared *s)
+{
+    return mbar_try_wait(bar, parity) || mbar_wait_long(bar, parity, s);
+}
+
+/* True for one lane of the warp; the compiler then knows that one lane alone issues what follows,
+ * and keeps the operands of copies and products in uniform registers. */
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(one));
+    return one != 0;
 }
 
 /* The address of the same variable in CTA `rank` of the cluster. */
@@ -133,60 +153,65 @@ __device__ __forceinline__ uint32_t cluster_rank()
     return r;
 }
 
+/* Tiles of a tensor map of four or five dimensions into shared memory, counted on `bar` (of a pair, the
+ * first CTA's). */
 template <bool PAIR>
-__device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap *map, int32_t k, int32_t row,
-                                       int32_t group, uint32_t bar)
-{
-    if constexpr (PAIR)
-        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile"
-                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(group), "r"(bar)
-                     : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile"
-                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(group), "r"(bar)
-                     : "memory");
-}
-
-template <bool PAIR>
-__device__ __forceinline__ void load_gated(uint32_t dst, const CUtensorMap *map, int32_t k,
-                                           int32_t row, int32_t group, uint32_t bar)
+__device__ __forceinline__ void load4(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1,
+                                      int32_t c2, int32_t c3, uint32_t bar)
 {
     if constexpr (PAIR)
         asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile"
                      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(0), "r"(group), "r"(bar)
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
                      : "memory");
     else
         asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile"
                      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(0), "r"(group), "r"(bar)
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
                      : "memory");
 }
 
 template <bool PAIR>
-__device__ __forceinline__ void load_x(uint32_t dst, const CUtensorMap *map, int32_t k, int32_t row,
-                                       uint32_t bar)
+__device__ __forceinline__ void load5(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1,
+                                      int32_t c2, int32_t c3, int32_t c4, uint32_t bar)
 {
     if constexpr (PAIR)
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
-                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(bar)
+        asm volatile("cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile"
+                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                         dst),
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
                      : "memory");
     else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile"
-                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                     "l"(map), "r"(k), "r"(row), "r"(bar)
+        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile"
+                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                         dst),
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
                      : "memory");
 }
 
-/* Shared-memory matrix of rows of 128 bytes, 128-byte swizzle, 8-row groups 1024 bytes apart. */
-__device__ __forceinline__ uint64_t matrix(uint32_t addr)
+template <bool PAIR>
+__device__ __forceinline__ void load3(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1,
+                                      int32_t c2, uint32_t bar)
 {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile"
+                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile"
+                     ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                     "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                     : "memory");
 }
+
+/* Descriptor of a shared-memory matrix of rows of 128 bytes, 128-byte swizzle, 8-row groups 1024
+ * bytes apart: the word with the address, and the other. */
+__device__ __forceinline__ uint32_t matrix_low(uint32_t addr)
+{
+    return ((addr & 0x3FFFFu) >> 4) | (1u << 16);
+}
+constexpr uint32_t kMatrixHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 
 /* fp32 accumulator, both operands bf16 or both f16, rows of the contraction contiguous. */
 __device__ __forceinline__ uint32_t instruction(int f16, uint32_t m, uint32_t n)
@@ -195,31 +220,34 @@ __device__ __forceinline__ uint32_t instruction(int f16, uint32_t m, uint32_t n)
     return (1u << 4) | (type << 7) | (type << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
+/* Accumulator d (+)= a b^T, 16 columns of the contraction. */
 template <bool PAIR>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, uint32_t add)
+__device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t inst, uint32_t add)
 {
     if constexpr (PAIR)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(inst), "r"(add)
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 ma, mb;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "mov.b64 ma, {%1, %5};\n\tmov.b64 mb, {%2, %5};\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], ma, mb, %3, p;\n\t}" ::"r"(d),
+                     "r"(a), "r"(b), "r"(inst), "r"(add), "r"(kMatrixHigh)
                      : "memory");
     else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(inst), "r"(add)
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 ma, mb;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "mov.b64 ma, {%1, %5};\n\tmov.b64 mb, {%2, %5};\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], ma, mb, %3, p;\n\t}" ::"r"(d),
+                     "r"(a), "r"(b), "r"(inst), "r"(add), "r"(kMatrixHigh)
                      : "memory");
 }
 
 /* Arrives on the barrier (of both CTAs of a pair) once all products issued so far are done. */
-template <bool PAIR> __device__ __forceinline__ void commit(uint64_t *bar)
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar)
 {
     if constexpr (PAIR)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster"
-                     ".multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3)
+                     ".multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
                      : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster"
-                     ".b64 [%0];" ::"r"(smem_addr(bar))
+                     ".b64 [%0];" ::"r"(bar)
                      : "memory");
 }
 
@@ -254,15 +282,29 @@ __device__ __forceinline__ float value(const void *p, int64_t i, int f16)
                : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
 }
 
-__device__ __forceinline__ float activate(float v, int act)
+/* One switch for a batch of values, so that they run side by side. */
+template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
     switch (act) {
-    case CFA_ACT_RELU: return v < 0.0f ? 0.0f : v;
-    case CFA_ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    case CFA_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+        break;
+    case CFA_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.0f + erff(v[i] * 0.70710678118654752f));
+        break;
     case CFA_ACT_GELU_TANH:
-        return 0.5f * v * (1.0f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
-    case CFA_ACT_SILU: return v / (1.0f + expf(-v));
-    default: return v;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = 0.5f * v[i] *
+                   (1.0f + tanhf(0.79788456080286536f * (v[i] + 0.044715f * v[i] * v[i] * v[i])));
+        break;
+    case CFA_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
+        break;
+    default: break;
     }
 }
 
@@ -295,51 +337,127 @@ __device__ __forceinline__ Tile tile_at(const Args &a, const Shared *s, int32_t 
     return o;
 }
 
-/* Stores up to 16 tokens' values of one output column: activation, bias, residual, rounding.
+/* One value of y: plus the residual, rounded. */
+__device__ __forceinline__ void store_one(const cfa_matmul &m, int64_t row, int64_t col, float v)
+{
+    if (m.residual) {
+        const int64_t at = row * m.r_stride + col;
+        v += m.y_f32 ? static_cast<const float *>(m.residual)[at] : value(m.residual, at, m.f16);
+    }
+    const int64_t at = row * m.y_stride + col;
+    if (m.y_f32) static_cast<float *>(m.y)[at] = v;
+    else if (m.f16) static_cast<__half *>(m.y)[at] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(m.y)[at] = __float2bfloat16_rn(v);
+}
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi, int f16)
+{
+    if (f16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+__device__ __forceinline__ float2 unpack(uint32_t v, int f16)
+{
+    if (f16) return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&v));
+}
+
+/* N tokens' values of the lane's column: token i of the batch stands at row + i * step, if i * step
+ * + 1 <= n.  Neighbouring lanes trade every second value, so that an even lane stores columns (c, c
+ * + 1) of the tokens 0, 2, .. of the batch and an odd lane (c - 1, c) of the tokens 1, 3, ..; pairs
+ * is false where y or the residual is off that grid. */
+template <int N>
+__device__ __forceinline__ void store(const Args &a, float (&v)[N], int64_t row, int step, int n,
+                                      int64_t col)
+{
+    const cfa_matmul &m = a.m;
+    if (!a.pairs) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (col < a.outs && i * step < n) store_one(m, row + i * step, col, v[i]);
+        return;
+    }
+    const int odd = threadIdx.x & 1;
+    const bool in = (col | 1) < a.outs;         /* both columns of the pair */
+    const bool last = !in && !odd && col < a.outs; /* a last column on its own */
+    float2 o[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * i] : v[2 * i + 1], 1);
+        o[i] = odd ? make_float2(got, v[2 * i + 1]) : make_float2(v[2 * i], got);
+    }
+    if (last) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i * step < n) store_one(m, row + i * step, col, v[i]);
+    }
+    if (!in) return;
+    const int64_t c = col - odd;
+    const int first = odd * step; /* token of o[0] */
+    if (m.residual) {
+        const int64_t at = (row + first) * m.r_stride + c;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            if (first + 2 * i * step >= n) continue;
+            const int64_t from = at + 2 * i * step * m.r_stride;
+            const float2 r =
+                m.y_f32 ? *reinterpret_cast<const float2 *>(
+                              static_cast<const float *>(m.residual) + from)
+                        : unpack(*reinterpret_cast<const uint32_t *>(
+                                     static_cast<const uint16_t *>(m.residual) + from), m.f16);
+            o[i].x += r.x;
+            o[i].y += r.y;
+        }
+    }
+    const int64_t at = (row + first) * m.y_stride + c;
+    if (m.y_f32) {
+        float *to = static_cast<float *>(m.y) + at;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+            if (first + 2 * i * step < n)
+                *reinterpret_cast<float2 *>(to + 2 * i * step * m.y_stride) = o[i];
+    } else {
+        uint16_t *to = static_cast<uint16_t *>(m.y) + at;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+            if (first + 2 * i * step < n)
+                *reinterpret_cast<uint32_t *>(to + 2 * i * step * m.y_stride) =
+                    pack(o[i].x, o[i].y, m.f16);
+    }
+}
+
+/* 16 tokens' sums of the lane's weight row, of which n are in the tile: bias, activation, store.
  * Gated: lanes 0-15 hold gate values and lanes 16-31 the up values of the same 16 columns; of two
  * tokens the lower half finishes the first and the upper half the second. */
 template <bool GATED>
 __device__ __forceinline__ void finish(const Args &a, float (&v)[16], int64_t row, int n, int64_t col,
-                                       bool in, float bias, float bias_up)
+                                       float bias)
 {
     const cfa_matmul &m = a.m;
+    if (m.bias) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] += bias;
+    }
     if constexpr (GATED) {
         const bool upper = threadIdx.x & 16;
+        float gate[8], up[8];
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) {
-            if (j >= n) break;
-            const float give = upper ? v[j] : v[j + 1];
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, give, 16);
-            const float gate = upper ? got : v[j], up = upper ? v[j + 1] : got;
-            const int mine = j + (upper ? 1 : 0);
-            if (!in || mine >= n) continue;
-            float o = activate(gate + bias, m.act) * (up + bias_up);
-            if (m.residual) {
-                const int64_t at = (row + mine) * m.r_stride + col;
-                o += m.y_f32 ? static_cast<const float *>(m.residual)[at]
-                             : value(m.residual, at, m.f16);
-            }
-            const int64_t at = (row + mine) * m.y_stride + col;
-            if (m.y_f32) static_cast<float *>(m.y)[at] = o;
-            else if (m.f16) static_cast<__half *>(m.y)[at] = __float2half_rn(o);
-            else static_cast<__nv_bfloat16 *>(m.y)[at] = __float2bfloat16_rn(o);
+        for (int j = 0; j < 8; ++j) {
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[2 * j] : v[2 * j + 1], 16);
+            gate[j] = upper ? got : v[2 * j];
+            up[j] = upper ? v[2 * j + 1] : got;
         }
+        activate(gate, m.act);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gate[j] *= up[j];
+        store<8>(a, gate, row + (upper ? 1 : 0), 2, n - (upper ? 1 : 0), col);
     } else {
-        if (!in) return;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if (j >= n) break;
-            float o = activate(v[j] + bias, m.act);
-            if (m.residual) {
-                const int64_t at = (row + j) * m.r_stride + col;
-                o += m.y_f32 ? static_cast<const float *>(m.residual)[at]
-                             : value(m.residual, at, m.f16);
-            }
-            const int64_t at = (row + j) * m.y_stride + col;
-            if (m.y_f32) static_cast<float *>(m.y)[at] = o;
-            else if (m.f16) static_cast<__half *>(m.y)[at] = __float2half_rn(o);
-            else static_cast<__nv_bfloat16 *>(m.y)[at] = __float2bfloat16_rn(o);
-        }
+        activate(v, m.act);
+        store<16>(a, v, row, 1, n, col);
     }
 }
 
@@ -352,7 +470,7 @@ __device__ void drain(const Args &a, Shared *s, uint32_t issued, bool second)
     for (uint32_t l = issued - most; l < issued; ++l) {
         bool done = false;
         for (uint32_t k = 0; !done && k < kDrainLimit; ++k)
-            done = mbar_try_wait(s->full + l % a.stages, (l / a.stages) & 1u);
+            done = mbar_try_wait(smem_addr(s->full + l % a.stages), (l / a.stages) & 1u);
         if (!done && !second) word = 2;
     }
     atomicMax(&g_status, word);
@@ -365,23 +483,28 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     Shared *s = reinterpret_cast<Shared *>(raw);
     const uint32_t ring = (smem_addr(raw) + (uint32_t)sizeof(Shared) + 1023u) & ~1023u;
     const uint32_t x_rows = PAIR ? a.bn / 2 : a.bn;
-    const uint32_t w_bytes = kRows * kRowBytes, x_bytes = x_rows * kRowBytes;
-    const uint32_t stage = w_bytes + x_bytes;
+    const uint32_t w_bytes = a.fr * kRowBytes, x_bytes = x_rows * kRowBytes;
+    const uint32_t block = w_bytes + x_bytes, stage = block * a.deep;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool cluster = PAIR || a.split > 1;
-    const uint32_t rank = cluster ? cluster_rank() : 0;
+    const uint32_t rank = PAIR || a.split > 1 ? cluster_rank() : 0;
     const uint32_t ctas = PAIR ? 2 : a.split; /* that share a tile */
-    const uint32_t features = (PAIR ? 2 : 1) * (GATED ? kRows / 2 : kRows);
+    const uint32_t per_cta = GATED ? a.fr / 2 : a.fr, features = (PAIR ? 2 : 1) * per_cta;
     const cfa_matmul &m = a.m;
+    const uint32_t full = smem_addr(s->full), empty = smem_addr(s->empty);
+    const uint32_t acc_full = smem_addr(s->acc_full), acc_empty = smem_addr(s->acc_empty);
 
+    if (threadIdx.x == kLoader * 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < a.stages; ++i) {
-            mbar_init(s->full + i, 1);
-            mbar_init(s->empty + i, 1);
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(s->acc_full + i, 1);
-            mbar_init(s->acc_empty + i, PAIR ? 8 : 4);
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, PAIR ? 8 : 4);
         }
         s->dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -431,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     }
     fence_before();
     __syncthreads();
-    if (cluster) cluster_sync();
+    if constexpr (PAIR) cluster_sync();
     fence_after();
     const uint32_t tmem = s->tmem;
     const int32_t total = s->total;
@@ -440,92 +563,148 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t k0 = PAIR ? 0 : rank * a.steps / a.split;
     const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps / a.split;
     const bool sync_tiles = !PAIR && a.split > 1;
+    const uint32_t deep = a.deep, stages = a.stages;
+    const bool wide = a.wide;
     bool ok = true;
 
     if (warp == kLoader) {
-        uint32_t at = 0, phase = 1; /* stage; an empty ring counts as released once */
-        uint32_t issued = 0;
-        int32_t group = 0;
-        if (lane == 0) asm volatile("fence.proxy.async.global;" ::: "memory");
-        for (int32_t t = begin; t < total; t += stride) {
-            if (lane == 0) {
+        if (elect_one()) {
+            uint32_t at = 0, phase = 1; /* stage; an empty ring counts as released once */
+            uint32_t issued = 0;
+            int32_t group = 0;
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+            for (int32_t t = begin; t < total; t += stride) {
                 const Tile o = tile_at(a, s, t, &group, features);
                 /* rows of x for this CTA: of a pair, each holds half of the columns in use */
                 uint32_t half = 0;
                 if constexpr (PAIR) half = rank * (((uint32_t)o.rows + 31u) / 32u * 16u);
                 const int32_t row = o.row + (int32_t)half;
-                const int32_t f = (int32_t)o.feature + (int32_t)(rank * (GATED ? 64u : 128u)) *
-                                                           (PAIR ? 1 : 0);
-                for (uint32_t k = k0; k < k1; ++k) {
-                    ok = ok && mbar_wait(s->empty + at, phase, s);
+                const int32_t f = (int32_t)o.feature + (PAIR ? (int32_t)(rank * per_cta) : 0);
+                /* of x, as many boxes as hold the rows in use (of a pair, in each half) */
+                const uint32_t in_use = PAIR ? ((uint32_t)o.rows + 31u) / 32u * 16u
+                                             : (uint32_t)o.rows;
+                const uint32_t boxes = (in_use + a.x_box - 1) / a.x_box;
+                const bool x_whole = wide && a.x_box == x_rows;
+                const uint32_t x_loaded = x_whole ? deep * x_bytes
+                                                  : boxes * a.x_box * kRowBytes;
+                const uint32_t w_loaded = deep * w_bytes;
+                for (uint32_t k = k0; k < k1; k += deep) {
+                    ok = ok && mbar_wait(empty + 8 * at, phase, s);
                     if (!ok) break;
-                    const uint32_t dst = ring + at * stage;
-                    uint32_t bar = smem_addr(s->full + at);
+                    const uint32_t blocks = min(deep, k1 - k);
+                    const uint32_t dst = ring + at * stage, dst_x = dst + w_loaded;
+                    uint32_t bar = full + 8 * at;
+                    if (!PAIR || rank == 0) {
+                        const uint32_t bytes = (wide ? w_loaded : blocks * w_bytes) +
+                                               (x_whole ? x_loaded : blocks * x_loaded);
+                        mbar_expect_tx(bar, PAIR ? 2 * bytes : bytes);
+                    }
                     if constexpr (PAIR) bar = map_to(bar, 0);
-                    if (!PAIR || rank == 0)
-                        mbar_expect_tx(s->full + at, PAIR ? 2 * stage : stage);
-                    const int32_t c = (int32_t)(k * kDepth);
-                    if constexpr (GATED) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            load_gated<PAIR>(dst + q * 32 * kRowBytes, &a.wmap, c, f + 16 * q,
-                                             o.group, bar);
+                    if (wide) {
+                        if constexpr (GATED)
+                            load5<PAIR>(dst, &a.wmap, 0, 0, 2 * o.group, f / 16, (int32_t)k, bar);
+                        else load4<PAIR>(dst, &a.wmap, 0, f, (int32_t)k, o.group, bar);
                     } else {
-                        load_w<PAIR>(dst, &a.wmap, c, f, o.group, bar);
+                        for (uint32_t i = 0; i < blocks; ++i) {
+                            const int32_t c = (int32_t)((k + i) * kDepth);
+                            if constexpr (GATED) {
+                                for (uint32_t q = 0; q < a.fr / 32; ++q)
+                                    load4<PAIR>(dst + i * w_bytes + q * 32 * kRowBytes, &a.wmap, c,
+                                                f + (int32_t)(16 * q), 0, o.group, bar);
+                            } else {
+                                load3<PAIR>(dst + i * w_bytes, &a.wmap, c, f, o.group, bar);
+                            }
+                        }
                     }
-                    load_x<PAIR>(dst + w_bytes, &a.xmap, c, row, bar);
+                    if (x_whole) {
+                        load3<PAIR>(dst_x, &a.xmap, 0, row, (int32_t)k, bar);
+                    } else {
+                        for (uint32_t i = 0; i < blocks; ++i)
+                            for (uint32_t q = 0; q < boxes; ++q) {
+                                const uint32_t to = dst_x + i * x_bytes + q * a.x_box * kRowBytes;
+                                const int32_t r = row + (int32_t)(q * a.x_box);
+                                if (wide) load3<PAIR>(to, &a.xmap, 0, r, (int32_t)(k + i), bar);
+                                else load3<PAIR>(to, &a.xmap, (int32_t)((k + i) * kDepth), r, 0, bar);
+                            }
+                    }
                     ++issued;
-                    if (++at == a.stages) {
+                    if (++at == stages) {
                         at = 0;
                         phase ^= 1;
                     }
                 }
+                if (sync_tiles) {
+                    cluster_sync();
+                    cluster_sync();
+                }
             }
-            __syncwarp();
-            if (sync_tiles) {
+            if (*(volatile int *)&s->dead) drain(a, s, issued, PAIR && rank);
+        } else if (sync_tiles) {
+            for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
                 cluster_sync();
             }
         }
-        if (lane == 0 && *(volatile int *)&s->dead) drain(a, s, issued, PAIR && rank);
+        __syncwarp();
     } else if (warp == kIssuer) {
-        const bool issues = lane == 0 && (!PAIR || rank == 0);
-        uint32_t at = 0, phase = 0, buf = 0, buf_phase = 1;
-        int32_t group = 0;
-        for (int32_t t = begin; t < total; t += stride) {
-            if (issues) {
-                const Tile o = tile_at(a, s, t, &group, features);
-                const uint32_t unit = PAIR ? 32u : 16u;
-                const uint32_t inst = instruction(m.f16, PAIR ? 256u : 128u,
-                                                  ((uint32_t)o.rows + unit - 1) / unit * unit);
-                const uint32_t d = tmem + buf * a.bn;
-                ok = ok && mbar_wait(s->acc_empty + buf, buf_phase, s);
-                fence_after();
-                for (uint32_t k = k0; k < k1; ++k) {
-                    ok = ok && mbar_wait(s->full + at, phase, s);
-                    if (!ok) break;
+        if (elect_one()) {
+            uint32_t at = 0, phase = 0, buf = 0, buf_phase = 1;
+            int32_t group = 0;
+            /* descriptors count in 16 bytes */
+            const uint32_t w_first = matrix_low(ring), x_first = w_first + (deep * w_bytes >> 4);
+            const uint32_t stage_on = stage >> 4, w_on = w_bytes >> 4, x_on = x_bytes >> 4;
+            for (int32_t t = begin; t < total; t += stride) {
+                if (!PAIR || rank == 0) {
+                    const Tile o = tile_at(a, s, t, &group, features);
+                    const uint32_t unit = PAIR ? 32u : 16u;
+                    const uint32_t inst = instruction(m.f16, PAIR ? 256u : 128u,
+                                                      ((uint32_t)o.rows + unit - 1) / unit * unit);
+                    const uint32_t d = tmem + buf * (a.tmem_cols / 2);
+                    /* each stage's barrier is looked at before the products of the one before are
+                     * issued, so that the look costs no time of its own */
+                    bool there = mbar_try_wait(full + 8 * at, phase);
+                    ok = ok && mbar_wait(acc_empty + 8 * buf, buf_phase, s);
                     fence_after();
-                    const uint32_t src = ring + at * stage;
-                    const uint64_t da = matrix(src), db = matrix(src + w_bytes);
+                    uint32_t add = 0; /* the first product of a tile overwrites */
+                    for (uint32_t k = k0; k < k1; k += deep) {
+                        ok = ok && (there || mbar_wait(full + 8 * at, phase, s));
+                        if (!ok) break;
+                        fence_after();
+                        uint32_t blocks = min(deep, k1 - k);
+                        uint32_t w = w_first + at * stage_on, x = x_first + at * stage_on;
+                        const uint32_t done = empty + 8 * at;
+                        if (++at == stages) {
+                            at = 0;
+                            phase ^= 1;
+                        }
+                        there = k + deep < k1 && mbar_try_wait(full + 8 * at, phase);
+                        do {
 #pragma unroll
-                    for (uint32_t q = 0; q < kDepth / 16; ++q) /* 32 bytes further in the row */
-                        mma<PAIR>(d, da + q * 2, db + q * 2, inst, k > k0 || q > 0);
-                    commit<PAIR>(s->empty + at);
-                    if (++at == a.stages) {
-                        at = 0;
-                        phase ^= 1;
+                            for (uint32_t q = 0; q < kDepth / 16; ++q) { /* 32 bytes further */
+                                mma<PAIR>(d, w + q * 2, x + q * 2, inst, add);
+                                add = 1;
+                            }
+                            w += w_on;
+                            x += x_on;
+                        } while (--blocks);
+                        commit<PAIR>(done);
                     }
+                    if (ok) commit<PAIR>(acc_full + 8 * buf);
+                    if (buf) buf_phase ^= 1;
+                    buf ^= 1;
                 }
-                if (ok) commit<PAIR>(s->acc_full + buf);
-                if (buf) buf_phase ^= 1;
-                buf ^= 1;
+                if (sync_tiles) {
+                    cluster_sync();
+                    cluster_sync();
+                }
             }
-            __syncwarp();
-            if (sync_tiles) {
+        } else if (sync_tiles) {
+            for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
                 cluster_sync();
             }
         }
+        __syncwarp();
     } else {
         uint32_t buf = 0, buf_phase = 0;
         int32_t group = 0;
@@ -535,26 +714,24 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         for (int32_t t = begin; t < total; t += stride) {
             const Tile o = tile_at(a, s, t, &group, features);
             int64_t col = o.feature + (GATED ? warp * 16 + (lane & 15) : warp * 32 + lane);
-            if constexpr (PAIR) col += rank * (GATED ? 64 : 128);
-            const bool in = col < a.outs;
-            float bias = 0.0f, bias_up = 0.0f;
-            if (m.bias && in) {
-                bias = m.bias_f32 ? static_cast<const float *>(m.bias)[col]
-                                  : value(m.bias, col, m.f16);
-                if (GATED)
-                    bias_up = m.bias_f32 ? static_cast<const float *>(m.bias)[a.outs + col]
-                                         : value(m.bias, a.outs + col, m.f16);
+            if constexpr (PAIR) col += rank * per_cta;
+            if ((uint32_t)(warp * 32 + lane) >= a.fr) col = a.outs; /* a lane without a row */
+            float bias = 0.0f; /* of the lane's weight row */
+            if (m.bias && col < a.outs) {
+                const int64_t at = col + (GATED && lane >= 16 ? a.outs : 0);
+                bias = m.bias_f32 ? static_cast<const float *>(m.bias)[at]
+                                  : value(m.bias, at, m.f16);
             }
-            ok = ok && mbar_wait(s->acc_full + buf, buf_phase, s);
+            ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
             ok = __all_sync(0xFFFFFFFFu, ok);
             fence_after();
-            const uint32_t src = tmem + lanes + buf * a.bn;
+            const uint32_t src = tmem + lanes + buf * (a.tmem_cols / 2);
             float v[16];
             if (!sync_tiles) {
                 for (int32_t c = 0; ok && c < o.rows; c += 16) {
                     __syncwarp();
                     tmem_load(src + c, v);
-                    finish<GATED>(a, v, o.row + c, o.rows - c, col, in, bias, bias_up);
+                    finish<GATED>(a, v, o.row + c, o.rows - c, col, bias);
                 }
             } else {
                 for (int32_t c = 0; ok && c < o.rows; c += 16) {
@@ -567,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             fence_before();
             __syncwarp();
             if (lane == 0) {
-                const uint32_t bar = smem_addr(s->acc_empty + buf);
+                const uint32_t bar = acc_empty + 8 * buf;
                 asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
                                  PAIR ? map_to(bar, 0) : bar)
                              : "memory");
@@ -596,7 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                             v[j] += p;
                         }
                     }
-                    finish<GATED>(a, v, o.row + c, c1 - c, col, in, bias, bias_up);
+                    finish<GATED>(a, v, o.row + c, c1 - c, col, bias);
                 }
                 cluster_sync();
             }
@@ -606,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *(volatile int *)&s->dead) atomicMax(&g_status, 1);
-    if (cluster) cluster_sync();
+    if constexpr (PAIR) cluster_sync();
     if (warp == kIssuer) {
         if constexpr (PAIR)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem),
@@ -708,49 +885,130 @@ cudaError_t clusters_of(Device &d, bool pair, bool gated, unsigned size, int *n)
     return *n > 0 ? cudaSuccess : cudaErrorInvalidConfiguration;
 }
 
-} // namespace
+/* How a product is cut. */
+struct Cut {
+    bool pair;
+    uint32_t bn, fr, split;
+};
 
-cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream)
+/* Microseconds that one block of kDepth columns takes a CTA (a pair): the four products and what
+ * their issue costs, measured with the loads left out. */
+double block_us(bool pair, uint32_t bn, uint32_t fr)
 {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e) return e;
-    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-    Device &d = g_device[dev];
-    int sms = d.sms.load();
-    if (!sms) {
-        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e) return e;
-        d.sms.store(sms);
+    if (pair) return bn <= 128 ? 0.22 : 0.22 + (bn - 128) * (0.29 - 0.22) / 128;
+    if (bn <= 32) return fr <= 64 ? 0.117 : 0.14;
+    if (bn <= 64) return 0.18;
+    return bn <= 128 ? 0.212 : 0.212 + (bn - 128) * (0.29 - 0.212) / 128;
+}
+
+/* The cut with the least estimated time.  A launch takes its latency, and the longest of
+ *   - the products of the CTA with the most tiles,
+ *   - that CTA's loads, at what one SM can take in,
+ *   - the bytes of all from memory: the weight once, x once.
+ * Groups are taken as equally full, their number of rows being all that the host knows. */
+Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
+{
+    const double kLaunch = 4.0, kSplit[3] = {0.0, 1.5, 2.0}; /* us: alone; 2, 4 CTAs per tile */
+    const double kSmBytes = 90e3, kBytes = 6.4e6;            /* per us: an SM, the memory */
+    const int64_t busy = m->busy, rows = (m->tokens + busy - 1) / busy;
+    const double once = 2.0 * m->cols * ((double)m->w_rows * busy + (double)m->tokens) / kBytes;
+    Cut best = {};
+    double least = 1e30;
+    for (int pair = 0; pair < 2; ++pair) {
+        const uint32_t unit = pair ? 32 : 16;
+        uint32_t last = 0;
+        for (int64_t parts = 1; parts <= 64; ++parts) {
+            const int64_t even = (rows + parts - 1) / parts;
+            /* uneven groups: room for half as much again where that saves a second tile */
+            const int64_t room = busy > 1 && parts == 1 ? even + even / 2 : even;
+            uint32_t bn = (uint32_t)((room + unit - 1) / unit * unit);
+            if (even > 256) continue;
+            if (bn > 256) bn = 256;
+            if (pair && bn < 128) break;
+            if (bn == last) continue;
+            last = bn;
+            const int64_t n_tiles = (rows + bn - 1) / bn * busy;
+            for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += m->gated ? 32 : 8) {
+                const uint32_t features = (pair ? 2 : 1) * (m->gated ? fr / 2 : fr);
+                const int64_t tiles = n_tiles * ((outs + features - 1) / features);
+                for (uint32_t log = 0; log < 3; ++log) {
+                    const uint32_t split = 1u << log, share = pair ? 2 : split;
+                    if (log && (pair || bn > 64 || steps < 4 * split)) break;
+                    /* clusters of four leave some SMs out */
+                    const int64_t slots = log == 2 ? sms * 9 / 38 : sms / share;
+                    const double turns = (double)((tiles + slots - 1) / slots);
+                    const double blocks = turns * ((steps + split - 1) / split);
+                    const double in = (double)(fr + (pair ? bn / 2 : bn)) * kRowBytes / kSmBytes;
+                    const double step = block_us(pair, bn, fr);
+                    double us = blocks * (in > step ? in : step);
+                    if (us < once) us = once;
+                    us += kLaunch + kSplit[log];
+                    if (us < least * 0.995) {
+                        least = us;
+                        best = {pair != 0, bn, fr, split};
+                    }
+                }
+            }
+        }
     }
-    const bool gated = m->gated;
+    return best;
+}
+
+/* The cut of sizes seen lately on this thread is looked up: weighing them all takes as long as a
+ * launch. */
+Cut cut_of(const cfa_matmul *m, int sms)
+{
+    struct Known {
+        int64_t tokens, w_rows, cols;
+        int32_t busy, gated, sms;
+        Cut cut;
+    };
+    static thread_local Known known[64] = {};
+    const uint64_t key = ((uint64_t)m->tokens * 0x9E3779B97F4A7C15ull) ^
+                         ((uint64_t)m->w_rows * 0xC2B2AE3D27D4EB4Full) ^
+                         ((uint64_t)m->cols * 0x165667B19E3779F9ull) ^ (uint64_t)m->busy;
+    Known &k = known[(key >> 40) & 63u];
+    if (k.tokens != m->tokens || k.w_rows != m->w_rows || k.cols != m->cols || k.busy != m->busy ||
+        k.gated != m->gated || k.sms != sms)
+        k = {m->tokens, m->w_rows, m->cols, m->busy, m->gated, sms,
+             choose(m, m->gated ? m->w_rows / 2 : m->w_rows,
+                    (uint32_t)((m->cols + kDepth - 1) / kDepth), sms)};
+    return k.cut;
+}
+
+cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int early, int release,
+                   cudaStream_t stream)
+{
+    cudaError_t e;
+    const bool gated = m->gated, pair = cut.pair;
     Args a = {};
     a.m = *m;
     a.outs = gated ? m->w_rows / 2 : m->w_rows;
     a.steps = (uint32_t)((m->cols + kDepth - 1) / kDepth);
     a.release = (uint32_t)release;
-
-    /* rows of a group, as far as the host knows */
-    const int64_t rows = (m->tokens + m->busy - 1) / m->busy;
-    const bool pair = rows > 128;
-    a.bn = 256;
-    if (!pair)
-        for (a.bn = 16; a.bn < rows; a.bn *= 2) {
-        }
-    const uint32_t features = (pair ? 2 : 1) * (gated ? kRows / 2 : kRows);
+    a.bn = cut.bn;
+    a.fr = cut.fr;
+    a.split = cut.split;
+    const uint32_t features = (pair ? 2 : 1) * (gated ? a.fr / 2 : a.fr);
     a.f_tiles = (uint32_t)((a.outs + features - 1) / features);
-    const int64_t likely = m->busy * ((rows + a.bn - 1) / a.bn) * a.f_tiles;
     const int64_t most = ((m->tokens + a.bn - 1) / a.bn + m->busy - 1) * a.f_tiles;
-    a.split = 1;
-    if (!pair && a.bn <= 64) {
-        int64_t n = likely < sms ? sms / likely : 1;
-        if (n > a.steps / 4) n = a.steps / 4;
-        a.split = (uint32_t)(n < 1 ? 1 : n > 8 ? 8 : n);
-    }
+    const uint64_t two = m->y_f32 ? 8 : 4;
+    a.pairs = (((uintptr_t)m->y | (uintptr_t)m->residual) % two) == 0 &&
+              (m->tokens <= 1 || (m->y_stride % 2 == 0 && (!m->residual || m->r_stride % 2 == 0)));
     const uint32_t x_rows = pair ? a.bn / 2 : a.bn;
-    const uint32_t stage = (kRows + x_rows) * kRowBytes;
+    a.x_box = m->offs && x_rows % 32 == 0 ? 32 : x_rows;
+    const uint32_t block = (a.fr + x_rows) * kRowBytes;
+    for (a.deep = 4; a.deep > 1 && block * a.deep > kDeepBytes; a.deep /= 2) {
+    }
+    const uint32_t stage = block * a.deep;
+    /* whole blocks of columns, so that they can be a dimension of their own */
+    a.wide = m->cols % kDepth == 0 && (!gated || a.outs % 16 == 0);
+    /* the products read kRows rows of each block of w, whatever lies behind the a.fr of them */
+    const uint32_t after = a.fr + a.deep * x_rows;
+    const uint32_t behind = kRows > after ? (kRows - after) * kRowBytes : 0;
+    const uint32_t partial = a.split > 1 ? a.bn * kRows * 4u : 0u;
     const uint32_t left = kSmem - (uint32_t)sizeof(Shared) - 1024u -
-                          (a.split > 1 ? a.bn * kRows * 4u : 0u);
+                          (partial > behind ? partial : behind);
     a.stages = left / stage < kMaxStages ? left / stage : kMaxStages;
     for (a.tmem_cols = 32; a.tmem_cols < 2 * a.bn; a.tmem_cols *= 2) {
     }
@@ -774,26 +1032,64 @@ cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaS
     const cuuint64_t wld = (m->w_rows > 1 ? (cuuint64_t)m->w_stride : whole) * 2;
     const cuuint64_t xld = (m->tokens > 1 ? (cuuint64_t)m->x_stride : whole) * 2;
     bool fine;
-    if (gated) {
-        const cuuint64_t dim[4] = {k, (cuuint64_t)a.outs, 2, (cuuint64_t)m->n_groups};
-        const cuuint64_t stride[3] = {wld, wld * a.outs, wld * a.outs * 2};
+    const cuuint64_t deep = kRowBytes, groups = (cuuint64_t)m->n_groups; /* a block further: bytes */
+    const cuuint64_t outs = (cuuint64_t)a.outs, rows = (cuuint64_t)m->w_rows;
+    if (a.wide && gated) { /* 64 columns, 16 rows, gate or up of each group, 16 rows on, block */
+        const cuuint64_t dim[5] = {kDepth, 16, 2 * groups, outs / 16, k / kDepth};
+        const cuuint64_t stride[4] = {wld, wld * outs, wld * 16, deep};
+        const cuuint32_t box[5] = {kDepth, 16, 2, a.fr / 32, a.deep};
+        fine = encode(&a.wmap, m->f16, m->w, 5, dim, stride, box);
+    } else if (gated) {
+        const cuuint64_t dim[4] = {k, outs, 2, groups};
+        const cuuint64_t stride[3] = {wld, wld * outs, wld * outs * 2};
         const cuuint32_t box[4] = {kDepth, 16, 2, 1};
         fine = encode(&a.wmap, m->f16, m->w, 4, dim, stride, box);
+    } else if (a.wide) {
+        const cuuint64_t dim[4] = {kDepth, rows, k / kDepth, groups};
+        const cuuint64_t stride[3] = {wld, deep, wld * rows};
+        const cuuint32_t box[4] = {kDepth, a.fr, a.deep, 1};
+        fine = encode(&a.wmap, m->f16, m->w, 4, dim, stride, box);
     } else {
-        const cuuint64_t dim[3] = {k, (cuuint64_t)m->w_rows, (cuuint64_t)m->n_groups};
-        const cuuint64_t stride[2] = {wld, wld * m->w_rows};
-        const cuuint32_t box[3] = {kDepth, kRows, 1};
+        const cuuint64_t dim[3] = {k, rows, groups};
+        const cuuint64_t stride[2] = {wld, wld * rows};
+        const cuuint32_t box[3] = {kDepth, a.fr, 1};
         fine = encode(&a.wmap, m->f16, m->w, 3, dim, stride, box);
     }
-    const cuuint64_t dim[2] = {k, (cuuint64_t)m->tokens}, stride[1] = {xld};
-    const cuuint32_t box[2] = {kDepth, x_rows};
-    if (!fine || !encode(&a.xmap, m->f16, m->x, 2, dim, stride, box))
-        return cudaErrorInvalidValue;
+    if (fine && a.wide) {
+        const cuuint64_t dim[3] = {kDepth, (cuuint64_t)m->tokens, k / kDepth};
+        const cuuint64_t stride[2] = {xld, deep};
+        const cuuint32_t box[3] = {kDepth, a.x_box, a.x_box == x_rows ? a.deep : 1};
+        fine = encode(&a.xmap, m->f16, m->x, 3, dim, stride, box);
+    } else if (fine) {
+        const cuuint64_t dim[3] = {k, (cuuint64_t)m->tokens, 1};
+        const cuuint64_t stride[2] = {xld, xld * (cuuint64_t)m->tokens};
+        const cuuint32_t box[3] = {kDepth, a.x_box, 1};
+        fine = encode(&a.xmap, m->f16, m->x, 3, dim, stride, box);
+    }
+    if (!fine) return cudaErrorInvalidValue;
 
     Config c;
     configure(&c, (unsigned)clusters * size, size, early != 0, stream);
     void *p[] = {&a};
     return cudaLaunchKernelExC(&c.cfg, fn, p);
+}
+
+} // namespace
+
+cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    Device &d = g_device[dev];
+    int sms = d.sms.load();
+    if (!sms) {
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e) return e;
+        d.sms.store(sms);
+    }
+    return launch(m, d, sms, cut_of(m, sms), early, release, stream);
 }
 
 cudaError_t cfa_matmul_status(int *word)

@@ -238,7 +238,7 @@ namespace {
 
 struct ExpertsPlan {
     int64_t pairs;
-    uint64_t hist, offs, place, token, xs, mid, part, total; /* offsets into the workspace */
+    uint64_t hist, offs, place, xs, mid, part, total; /* offsets into the workspace */
 };
 
 cfa_status experts_plan(const cfa_experts_args *a, ExpertsPlan *p)
@@ -267,7 +267,6 @@ cfa_status experts_plan(const cfa_experts_args *a, ExpertsPlan *p)
     p->hist = part((uint64_t)cfa_sort_blocks(p->pairs) * a->experts * 4);
     p->offs = part((uint64_t)(a->experts + 1) * 4);
     p->place = part(n * 4);
-    p->token = part(n * 4);
     p->xs = part(n * a->hidden * 2);
     p->mid = part(n * a->inter * 2);
     p->part = part(n * a->hidden * 4);
@@ -352,11 +351,7 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     s.hist = reinterpret_cast<int32_t *>(ws + p.hist);
     s.offs = reinterpret_cast<int32_t *>(ws + p.offs);
     s.place = reinterpret_cast<int32_t *>(ws + p.place);
-    s.token = reinterpret_cast<int32_t *>(ws + p.token);
-    cudaError_t e = cfa_launch_sort(&s, stream);
-    if (!e)
-        e = cfa_launch_gather(a->x, a->x_stride, a->hidden, s.token, s.offs + a->experts, p.pairs,
-                              ws + p.xs, a->hidden, stream);
+    cudaError_t e = cfa_launch_sort(&s, a->x, a->x_stride, a->hidden, ws + p.xs, stream);
     cfa_matmul m = {};
     m.offs = s.offs;
     m.tokens = p.pairs;

@@ -38,10 +38,9 @@ typedef struct cfa_sort {
     const int32_t *ids; /* [pairs] */
     int64_t pairs;
     int32_t top_k, first, experts;
-    int32_t *hist;      /* [blocks, experts], for more than one block */
+    int32_t *hist;      /* [cfa_sort_blocks(pairs), experts] */
     int32_t *offs;      /* [experts + 1] out: where each expert's rows start */
     int32_t *place;     /* [pairs] out: a pair's row, -1 if its expert is elsewhere */
-    int32_t *token;     /* [pairs] out: the token of each row */
 } cfa_sort;
 
 /* All of these enqueue on `stream` and return a CUDA error. `early`: may start before the kernel
@@ -50,12 +49,11 @@ cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaS
 /* The current device's word of waits that ran out (0: none), cleared. */
 cudaError_t cfa_matmul_status(int *word);
 cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream);
+/* Rows of hist that the sort of so many pairs needs. */
 int64_t cfa_sort_blocks(int64_t pairs);
-cudaError_t cfa_launch_sort(const cfa_sort *s, cudaStream_t stream);
-/* Rows token[r] of x into rows r of xs, for r < offs[experts]. */
-cudaError_t cfa_launch_gather(const void *x, int64_t x_stride, int64_t hidden, const int32_t *token,
-                              const int32_t *rows, int64_t most, void *xs, int64_t xs_stride,
-                              cudaStream_t stream);
+/* The sort, and the tokens' rows of x into their places in xs (rows of `hidden` elements). */
+cudaError_t cfa_launch_sort(const cfa_sort *s, const void *x, int64_t x_stride, int64_t hidden,
+                            void *xs, cudaStream_t stream);
 /* y[t] = residual[t] + sum_j weights[t, j] part[place[t, j]]. */
 typedef struct cfa_combine {
     const float *part; /* [rows, hidden] */

@@ -23,36 +23,40 @@ SIZES = {"cfa_linear_args": _LINEAR.size, "cfa_route_args": _ROUTE.size,
          "cfa_experts_args": _EXPERTS.size}
 
 torch = None
-_CODE = None   # torch dtype -> CFA_DTYPE_*
-_DTYPE = None  # dtype name -> torch dtype
+_CODE = None    # torch dtype -> CFA_DTYPE_*
+_DTYPE = None   # dtype name -> torch dtype
+_lib_c = None
+_raw_stream = _device = _grad = None
 
 
 def _start():
-    global torch, _CODE, _DTYPE
+    global torch, _CODE, _DTYPE, _lib_c, _raw_stream, _device, _grad
     import torch as t
+    _lib_c = _lib.load()
     _DTYPE = {"bf16": t.bfloat16, "f16": t.float16, "f32": t.float32}
     _CODE = {v: _lib.DTYPE[k] for k, v in _DTYPE.items()}
+    _raw_stream, _device = t._C._cuda_getCurrentRawStream, t._C._cuda_getDevice
+    _grad = t.is_grad_enabled
     torch = t
 
 
-def _check(lib, st):
+def _check(st):
     if st != _lib.CFA_OK:
         from . import _check as check
         check(st)
 
 
-def _operands(device, **tensors):
-    grad = torch.is_grad_enabled()
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
-        if t.shape and t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError(f"{name}: the last dimension must be contiguous")
-        if grad and t.requires_grad:
-            raise ValueError(f"{name} requires a gradient, and the operators have no backward "
-                             "pass: call them under torch.no_grad()")
+def _on(t, name, device):
+    """Refuses an operand that is on another device, not contiguous in its last dimension, or part
+    of a graph that a backward pass would need."""
+    if device < 0 or t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}" if device >= 0 else
+                         f"the operators run on CUDA tensors, not on {t.device}")
+    if not t.is_contiguous() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if t.requires_grad and _grad():
+        raise ValueError(f"{name} requires a gradient, and the operators have no backward pass: "
+                         "call them under torch.no_grad()")
 
 
 def _code(t, name):
@@ -70,58 +74,44 @@ def _one_of(table, name, what):
 
 
 def _rows(t, name, cols):
-    """A tensor [..., cols] as rows: (tensor, row count, row stride)."""
-    if t.dim() == 2:
-        n, c = t.shape
-    elif t.dim() and t.shape[-1]:
-        c = t.shape[-1]
+    """A tensor [..., cols] as rows: (row count, row stride)."""
+    shape = t.shape
+    if len(shape) == 2:
+        n, c = shape
+        stride = t.stride(0)
+    elif shape and shape[-1]:
+        c = shape[-1]
         n = t.numel() // c
-        t = t.view(n, c)  # raises where the rows do not lie evenly
+        stride = t.view(n, c).stride(0)  # raises where the rows do not lie evenly
     else:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}")
+        raise ValueError(f"{name}: shape {tuple(shape)}")
     if c != cols:
         raise ValueError(f"{name}: rows of {c}, not {cols}")
-    return t, n, t.stride(0)
+    return n, stride
 
 
 class _On:
-    """The stream that a call enqueues on, current while it allocates."""
+    """A stream that a call enqueues on, current while the call allocates."""
 
     def __init__(self, stream, device):
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=device)
-        self.handle = stream.cuda_stream
         self.guard = torch.cuda.stream(stream)
 
     def __enter__(self):
         self.guard.__enter__()
-        return self.handle
 
     def __exit__(self, *exc):
         self.guard.__exit__(*exc)
 
 
-class _Current:
-    def __init__(self, device):
-        self.guard = None
-        if device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-        self.device = device
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
-
-
-def _enter(stream, device):
-    if device.type != "cuda":
-        raise ValueError(f"the operators run on CUDA tensors, not on {device}")
-    return _Current(device) if stream is None else _On(stream, device)
+def _elsewhere(stream, device):
+    """The guard of a call that is not for the current device's current stream, or None."""
+    if stream is not None:
+        return _On(stream, device)
+    if device != _device():
+        return torch.cuda.device(device)
+    return None
 
 
 def _workspace(given, need, device):
@@ -148,52 +138,68 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
     """
     if torch is None:
         _start()
-    device = x.device
-    _operands(device, x=x, weight=weight, bias=bias, residual=residual, out=out)
-    if weight.dim() != 2:
-        raise ValueError(f"weight: shape {tuple(weight.shape)}")
-    n, k = weight.shape
-    x2, t, xs = _rows(x, "x", k)
+    device = x.get_device()
+    _on(x, "x", device)
+    _on(weight, "weight", device)
+    guard = _elsewhere(stream, device)
+    if guard is not None:
+        with guard:
+            return linear(x, weight, bias, activation=activation, gated=gated, residual=residual,
+                          out=out, out_dtype=out_dtype, workspace=workspace)
+    wshape = weight.shape
+    if len(wshape) != 2:
+        raise ValueError(f"weight: shape {tuple(wshape)}")
+    n, k = wshape
+    t, xs = _rows(x, "x", k)
+    dtype = x.dtype
     code = _code(x, "x")
-    if weight.dtype != x.dtype:
-        raise ValueError(f"weight is {weight.dtype}, x {x.dtype}")
-    if bias is not None and bias.shape != (n,):
-        raise ValueError(f"bias: shape {tuple(bias.shape)}, not ({n},)")
-    if gated and n % 2:
-        raise ValueError(f"a gated weight has an even number of rows, not {n}")
+    if weight.dtype is not dtype:
+        raise ValueError(f"weight is {weight.dtype}, x {dtype}")
     act = _one_of(ACTIVATION, activation, "activation")
-    no = n // 2 if gated else n
-    shape = x.shape[:-1] + (no,)
-    lib = _lib.load()
-    with _enter(stream, device) as handle:
-        if out is None:
-            dt = x.dtype if out_dtype is None else _one_of(_DTYPE, out_dtype, "out_dtype")
-            out = torch.empty(shape, dtype=dt, device=device)
-        elif out.shape != shape or (out_dtype is not None and
-                                    out.dtype != _one_of(_DTYPE, out_dtype, "out_dtype")):
+    no = n
+    if gated:
+        if n % 2:
+            raise ValueError(f"a gated weight has an even number of rows, not {n}")
+        no = n // 2
+    bp = bc = rp = rs = buf = size = 0
+    if bias is not None:
+        _on(bias, "bias", device)
+        if bias.shape != (n,):
+            raise ValueError(f"bias: shape {tuple(bias.shape)}, not ({n},)")
+        bp, bc = bias.data_ptr(), _code(bias, "bias")
+    xshape = x.shape
+    shape = (t, no) if len(xshape) == 2 else xshape[:-1] + (no,)
+    odtype = dtype if out_dtype is None else _one_of(_DTYPE, out_dtype, "out_dtype")
+    if out is None:
+        out = torch.empty(shape, dtype=odtype, device=x.device)
+        os_ = no
+    else:
+        _on(out, "out", device)
+        if out.shape != shape or (out_dtype is not None and out.dtype is not odtype):
             raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, not {tuple(shape)}")
-        o2, _, os_ = _rows(out, "out", no)
-        rp = rs = 0
-        if residual is not None:
-            if residual.shape != shape or residual.dtype != out.dtype:
-                raise ValueError(f"residual: {residual.dtype} {tuple(residual.shape)}, not "
-                                 f"{out.dtype} {tuple(shape)}")
-            r2, _, rs = _rows(residual, "residual", no)
-            rp = r2.data_ptr()
-        xp, wp, ws = x2.data_ptr(), weight.data_ptr(), weight.stride(0)
-        bp, bc = (0, 0) if bias is None else (bias.data_ptr(), _code(bias, "bias"))
-
-        def pack(buf, size):
-            return _LINEAR.pack(xp, wp, bp, rp, o2.data_ptr(), buf, size, t, n, k, xs, ws, rs,
-                                os_, code, bc, _code(out, "out"), act, GATED if gated else 0, 0)
-        buf = size = 0
-        if (xp | wp | (xs | ws) * 2) & 15:
-            need = _lib.ctypes.c_uint64()
-            _check(lib, lib.cfa_linear_workspace(pack(0, 0), _lib.ctypes.byref(need)))
-            if need.value:
-                workspace = _workspace(workspace, need.value, device)
-                buf, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _check(lib, lib.cfa_linear_async(pack(buf, size), handle))
+        odtype = out.dtype
+        _, os_ = _rows(out, "out", no)
+    if residual is not None:
+        _on(residual, "residual", device)
+        if residual.shape != shape or residual.dtype is not odtype:
+            raise ValueError(f"residual: {residual.dtype} {tuple(residual.shape)}, not {odtype} "
+                             f"{tuple(shape)}")
+        _, rs = _rows(residual, "residual", no)
+        rp = residual.data_ptr()
+    xp, wp, ws = x.data_ptr(), weight.data_ptr(), weight.stride(0)
+    if (xp | wp | (xs | ws) * 2) & 15:
+        need = _lib.ctypes.c_uint64()
+        _check(_lib_c.cfa_linear_workspace(
+            _LINEAR.pack(xp, wp, bp, rp, 0, 0, 0, t, n, k, xs, ws, rs, os_, code, bc, code, act,
+                         0, 0), _lib.ctypes.byref(need)))
+        if need.value:
+            workspace = _workspace(workspace, need.value, x.device)
+            buf, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = _lib_c.cfa_linear_async(
+        _LINEAR.pack(xp, wp, bp, rp, out.data_ptr(), buf, size, t, n, k, xs, ws, rs, os_, code, bc,
+                     _code(out, "out"), act, GATED if gated else 0, 0), _raw_stream(device))
+    if st:
+        _check(st)
     return out
 
 
@@ -212,34 +218,44 @@ def route(logits, top_k, *, scoring="softmax", bias=None, groups=1, top_groups=1
     """
     if torch is None:
         _start()
-    device = logits.device
-    _operands(device, logits=logits, bias=bias)
-    e = logits.shape[-1] if logits.dim() else 0
-    l2, t, ls = _rows(logits, "logits", e)
-    if bias is not None and (bias.shape != (e,) or bias.dtype != torch.float32):
-        raise ValueError(f"bias: {bias.dtype} {tuple(bias.shape)}, not float32 ({e},)")
+    device = logits.get_device()
+    _on(logits, "logits", device)
+    guard = _elsewhere(stream, device)
+    if guard is not None:
+        with guard:
+            return route(logits, top_k, scoring=scoring, bias=bias, groups=groups,
+                         top_groups=top_groups, renormalize=renormalize, scale=scale, out=out)
+    lshape = logits.shape
+    e = lshape[-1] if lshape else 0
+    t, ls = _rows(logits, "logits", e)
+    bp = 0
+    if bias is not None:
+        _on(bias, "bias", device)
+        if bias.shape != (e,) or bias.dtype is not torch.float32:
+            raise ValueError(f"bias: {bias.dtype} {tuple(bias.shape)}, not float32 ({e},)")
+        bp = bias.data_ptr()
     top_k = int(top_k)
-    shape = logits.shape[:-1] + (top_k,)
-    lib = _lib.load()
-    with _enter(stream, device) as handle:
-        if out is None:
-            if top_k < 1:
-                raise ValueError(f"top_k is {top_k}")
-            weights = torch.empty(shape, dtype=torch.float32, device=device)
-            ids = torch.empty(shape, dtype=torch.int32, device=device)
-        else:
-            weights, ids = out
-            for o, dt, name in ((weights, torch.float32, "weights"), (ids, torch.int32, "ids")):
-                if (o.shape != shape or o.dtype != dt or o.device != device or
-                        not o.is_contiguous()):
-                    raise ValueError(f"{name}: {o.dtype} {tuple(o.shape)}, not a contiguous {dt} "
-                                     f"{tuple(shape)}")
-        args = _ROUTE.pack(l2.data_ptr(), 0 if bias is None else bias.data_ptr(),
-                           weights.data_ptr(), ids.data_ptr(), t, ls, e, top_k, groups,
-                           top_groups, _code(logits, "logits"),
-                           _one_of(SCORING, scoring, "scoring"),
-                           RENORMALIZE if renormalize else 0, scale)
-        _check(lib, lib.cfa_route_async(args, handle))
+    if top_k < 1:
+        raise ValueError(f"top_k is {top_k}")
+    shape = (t, top_k) if len(lshape) == 2 else lshape[:-1] + (top_k,)
+    code = _code(logits, "logits")
+    score = _one_of(SCORING, scoring, "scoring") if scoring != "softmax" else 0
+    if out is None:
+        weights = torch.empty(shape, dtype=torch.float32, device=logits.device)
+        ids = torch.empty(shape, dtype=torch.int32, device=logits.device)
+    else:
+        weights, ids = out
+        for o, dt, name in ((weights, torch.float32, "weights"), (ids, torch.int32, "ids")):
+            _on(o, name, device)
+            if o.shape != shape or o.dtype is not dt or not o.is_contiguous():
+                raise ValueError(f"{name}: {o.dtype} {tuple(o.shape)}, not a contiguous {dt} "
+                                 f"{tuple(shape)}")
+    st = _lib_c.cfa_route_async(
+        _ROUTE.pack(logits.data_ptr(), bp, weights.data_ptr(), ids.data_ptr(), t, ls, e, top_k,
+                    groups, top_groups, code, score, RENORMALIZE if renormalize else 0, scale),
+        _raw_stream(device))
+    if st:
+        _check(st)
     return weights, ids
 
 
@@ -251,62 +267,71 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
     w13       [E, 2 I, H] (gate rows, then up rows) or [E, I, H] (no gate);  w2 [E, H, I]: the
               experts first_expert .. first_expert + E - 1, as loaded.  Other ids add nothing
     residual  [..., H] of x's dtype; `out` may be the same tensor
-    workspace  uint8 tensor of experts_workspace bytes (default: allocated)
+    workspace  uint8 tensor (default: allocated; its size is cfa_experts_workspace of cfa.h)
     """
     if torch is None:
         _start()
-    device = x.device
-    _operands(device, x=x, ids=ids, weights=weights, w13=w13, w2=w2, residual=residual, out=out)
+    device = x.get_device()
+    _on(x, "x", device)
+    guard = _elsewhere(stream, device)
+    if guard is not None:
+        with guard:
+            return experts(x, ids, weights, w13, w2, activation=activation,
+                           first_expert=first_expert, residual=residual, out=out,
+                           workspace=workspace)
+    for v, name in ((ids, "ids"), (weights, "weights"), (w13, "w13"), (w2, "w2")):
+        _on(v, name, device)
+        if not v.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
     if w13.dim() != 3 or w2.dim() != 3:
         raise ValueError(f"w13 {tuple(w13.shape)} and w2 {tuple(w2.shape)} have three dimensions")
     e, h, i = w2.shape
     gated = w13.shape == (e, 2 * i, h)
     if not gated and w13.shape != (e, i, h):
         raise ValueError(f"w13 {tuple(w13.shape)} does not fit w2 {tuple(w2.shape)}")
-    if w13.dtype != x.dtype or w2.dtype != x.dtype:
-        raise ValueError(f"w13 is {w13.dtype}, w2 {w2.dtype}, x {x.dtype}")
-    if not (w13.is_contiguous() and w2.is_contiguous()):
-        raise ValueError("w13 and w2 must be contiguous")
-    x2, t, xs = _rows(x, "x", h)
-    top_k = ids.shape[-1] if ids.dim() else 0
-    if (ids.shape != x.shape[:-1] + (top_k,) or weights.shape != ids.shape or
-            ids.dtype != torch.int32 or weights.dtype != torch.float32 or
-            not (ids.is_contiguous() and weights.is_contiguous())):
-        raise ValueError(f"ids {ids.dtype} {tuple(ids.shape)} and weights {weights.dtype} "
-                         f"{tuple(weights.shape)} must be contiguous int32 and float32 "
-                         f"{tuple(x.shape[:-1])} + (top_k,)")
+    dtype = x.dtype
+    if w13.dtype is not dtype or w2.dtype is not dtype:
+        raise ValueError(f"w13 is {w13.dtype}, w2 {w2.dtype}, x {dtype}")
+    t, xs = _rows(x, "x", h)
+    shape, ishape = x.shape, ids.shape
+    top_k = ishape[-1] if ishape else 0
+    if (ishape[:-1] != shape[:-1] or weights.shape != ishape or ids.dtype is not torch.int32 or
+            weights.dtype is not torch.float32):
+        raise ValueError(f"ids {ids.dtype} {tuple(ishape)} and weights {weights.dtype} "
+                         f"{tuple(weights.shape)} must be int32 and float32 {tuple(shape[:-1])} + "
+                         "(top_k,)")
     code = _code(x, "x")
     act = _one_of(ACTIVATION, activation, "activation")
-    lib = _lib.load()
-    with _enter(stream, device) as handle:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
-        elif out.shape != x.shape or out.dtype != x.dtype:
-            raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, not {x.dtype} "
-                             f"{tuple(x.shape)}")
-        o2, _, os_ = _rows(out, "out", h)
-        rp = rs = 0
-        if residual is not None:
-            if residual.shape != x.shape or residual.dtype != x.dtype:
-                raise ValueError(f"residual: {residual.dtype} {tuple(residual.shape)}, not "
-                                 f"{x.dtype} {tuple(x.shape)}")
-            r2, _, rs = _rows(residual, "residual", h)
-            rp = r2.data_ptr()
-
-        def pack(buf, size):
-            return _EXPERTS.pack(x2.data_ptr(), w13.data_ptr(), w2.data_ptr(), rp, ids.data_ptr(),
-                                 weights.data_ptr(), o2.data_ptr(), buf, size, t, h, i, xs, rs,
-                                 os_, e, first_expert, top_k, code, act, GATED if gated else 0)
-        need = _lib.ctypes.c_uint64()
-        _check(lib, lib.cfa_experts_workspace(pack(0, 0), _lib.ctypes.byref(need)))
-        workspace = _workspace(workspace, need.value, device)
-        _check(lib, lib.cfa_experts_async(
-            pack(workspace.data_ptr(), workspace.numel() * workspace.element_size()), handle))
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+        os_ = h
+    else:
+        _on(out, "out", device)
+        if out.shape != shape or out.dtype is not dtype:
+            raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, not {dtype} {tuple(shape)}")
+        _, os_ = _rows(out, "out", h)
+    rp = rs = 0
+    if residual is not None:
+        _on(residual, "residual", device)
+        if residual.shape != shape or residual.dtype is not dtype:
+            raise ValueError(f"residual: {residual.dtype} {tuple(residual.shape)}, not {dtype} "
+                             f"{tuple(shape)}")
+        _, rs = _rows(residual, "residual", h)
+        rp = residual.data_ptr()
+    ptrs = (x.data_ptr(), w13.data_ptr(), w2.data_ptr(), rp, ids.data_ptr(), weights.data_ptr(),
+            out.data_ptr())
+    rest = (t, h, i, xs, rs, os_, e, first_expert, top_k, code, act, GATED if gated else 0)
+    need = _lib.ctypes.c_uint64()
+    _check(_lib_c.cfa_experts_workspace(_EXPERTS.pack(*ptrs, 0, 0, *rest),
+                                        _lib.ctypes.byref(need)))
+    workspace = _workspace(workspace, need.value, x.device)
+    _check(_lib_c.cfa_experts_async(
+        _EXPERTS.pack(*ptrs, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                      *rest), _raw_stream(device)))
     return out
 
 
 def op_status():
     """Raises CfaError if a wait inside a product's kernel has run out on the current device since the
     last call (the results since then are not valid).  Call it after waiting for the streams."""
-    lib = _lib.load()
-    _check(lib, lib.cfa_op_status())
+    _check(_lib.load().cfa_op_status())
