@@ -16,8 +16,8 @@
  * half of the tokens, so each operand is loaded once per pair.
  * split: with few output tiles a cluster of CTAs shares one, each over its part of the columns of w;
  * the partial sums meet in shared memory and are added in the order of the CTAs.
- * Gated: the stage holds 16 gate rows, then the 16 up rows that belong to them, and so on, so both
- * values of an output lie in one warp, 16 lanes apart.
+ * Gated: the stage holds 8 gate rows, then the 8 up rows that belong to them, and so on, so both
+ * values of an output lie in one warp, 8 lanes apart.
  *
  * Every wait has a limit.  One that runs out sets the status word that cfa_op_status reads; its CTA
  * then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
@@ -40,26 +40,31 @@ constexpr uint32_t kRows = 128;          /* weight rows per CTA, at most */
 constexpr uint32_t kDepth = 64;          /* columns of w and x per block: one 128-byte swizzle row */
 constexpr uint32_t kDeepBytes = 49152;   /* a stage takes more than one block up to this */
 constexpr uint32_t kRowBytes = kDepth * 2;
-constexpr uint32_t kMaxStages = 32;
+constexpr uint32_t kMaxStages = 32;      /* no more than a warp has lanes */
 constexpr uint32_t kSmem = 232448;       /* all that a CTA may have: one CTA per SM, so that the
                                             tensor memory is never asked for twice at once */
 constexpr uint32_t kBand = 16;           /* token tiles that share a weight tile in turn */
+constexpr uint32_t kBoxes = 4;           /* heights of the loads of x */
 constexpr uint32_t kSpinLimit = 1u << 20;    /* polls of a wait */
 constexpr uint32_t kDrainLimit = 1u << 16;   /* polls for loads in flight after one ran out */
 
 struct Args {
-    CUtensorMap wmap, xmap;
+    CUtensorMap wmap, xmap[kBoxes]; /* a stage's blocks of w and of x at once, whole blocks only */
+    CUtensorMap wtail, xtail[kBoxes]; /* one block; columns behind the last read as zeros */
     cfa_matmul m;
     int64_t outs;        /* columns of y */
     uint32_t bn;         /* token tile */
-    uint32_t x_box;      /* rows of x per load */
-    uint32_t fr;         /* weight rows per CTA: a multiple of 8, gated of 32 */
+    uint32_t x_box[kBoxes]; /* rows of x per load: all of the tile's, and less for ragged groups; 0:
+                            no such map */
+    uint32_t fr;         /* weight rows per CTA: a multiple of 8, gated of 16 */
     uint32_t stages;
     uint32_t deep;       /* blocks of kDepth columns per stage */
-    uint32_t wide;       /* one load brings a stage's blocks of w (and of x if x_box is all of it) */
+    uint32_t wide;       /* a gated w has groups of 8 rows, or w is not gated */
+    uint32_t whole;      /* whole blocks; the last of steps may lack columns */
     uint32_t steps;      /* blocks in all */
     uint32_t f_tiles;    /* feature tiles per group */
-    uint32_t split;      /* CTAs per output tile along the columns */
+    int32_t total;       /* output tiles, of one group */
+    uint32_t split;      /* log2 of the CTAs per output tile along the columns */
     uint32_t tmem_cols;
     uint32_t release;
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
@@ -73,10 +78,14 @@ struct Shared {
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem;
     int dead;
-    int32_t total; /* output tiles */
-    int32_t first[CFA_EXPERTS_MAX + 1]; /* output tiles before each group's */
-    int32_t row[CFA_EXPERTS_MAX + 1];   /* rows of x before each group's */
+    int32_t total;   /* output tiles */
+    int32_t group[]; /* output tiles before each group's, and rows of x before each group's, in turn */
 };
+
+__host__ __device__ inline uint32_t shared_bytes(int32_t groups)
+{
+    return (uint32_t)sizeof(Shared) + ((uint32_t)groups + 1u) * 8u;
+}
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p)
 {
@@ -144,6 +153,12 @@ __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank)
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+/* The same where nothing written has to be seen: the others have read what they need. */
+__device__ __forceinline__ void cluster_done()
+{
+    asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory");
 }
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -320,19 +335,29 @@ struct Tile {
 __device__ __forceinline__ Tile tile_at(const Args &a, const Shared *s, int32_t t, int32_t *group,
                                         uint32_t features)
 {
-    int32_t g = *group;
-    while (t >= s->first[g + 1]) ++g;
-    *group = g;
-    const uint32_t local = (uint32_t)(t - s->first[g]);
-    const int32_t rows = s->row[g + 1] - s->row[g];
-    const uint32_t tiles = ((uint32_t)rows + a.bn - 1) / a.bn;
-    const uint32_t band = local / (kBand * a.f_tiles), rest = local - band * kBand * a.f_tiles;
-    const uint32_t left = tiles - band * kBand, width = left < kBand ? left : kBand;
-    const uint32_t f = rest / width, n = band * kBand + rest % width;
     Tile o;
-    o.group = g;
+    int32_t rows = (int32_t)a.m.tokens, before = 0;
+    uint32_t local = (uint32_t)t;
+    o.group = 0;
+    if (a.m.offs) {
+        int32_t g = *group;
+        while (t >= s->group[2 * g + 2]) ++g;
+        *group = o.group = g;
+        local = (uint32_t)(t - s->group[2 * g]);
+        before = s->group[2 * g + 1];
+        rows = s->group[2 * g + 3] - before;
+    }
+    uint32_t f = local, n = 0;
+    if ((uint32_t)rows > a.bn) { /* more than one token tile */
+        const uint32_t tiles = ((uint32_t)rows + a.bn - 1) / a.bn;
+        const uint32_t band = tiles <= kBand ? 0 : local / (kBand * a.f_tiles);
+        const uint32_t rest = local - band * kBand * a.f_tiles;
+        const uint32_t left = tiles - band * kBand, width = left < kBand ? left : kBand;
+        f = rest / width;
+        n = band * kBand + rest - f * width;
+    }
     o.feature = (int64_t)f * features;
-    o.row = s->row[g] + (int32_t)(n * a.bn);
+    o.row = before + (int32_t)(n * a.bn);
     o.rows = min((int32_t)a.bn, rows - (int32_t)(n * a.bn));
     return o;
 }
@@ -430,34 +455,33 @@ __device__ __forceinline__ void store(const Args &a, float (&v)[N], int64_t row,
     }
 }
 
-/* 16 tokens' sums of the lane's weight row, of which n are in the tile: bias, activation, store.
- * Gated: lanes 0-15 hold gate values and lanes 16-31 the up values of the same 16 columns; of two
- * tokens the lower half finishes the first and the upper half the second. */
-template <bool GATED>
-__device__ __forceinline__ void finish(const Args &a, float (&v)[16], int64_t row, int n, int64_t col,
+/* N of 16 tokens' sums of the lane's weight row, of which n are in the tile: bias, activation, store.
+ * Gated: of 16 lanes, 8 hold gate values and the next 8 the up values of the same columns; of two tokens
+ * the gate's lanes finish the first and the others the second. */
+template <bool GATED, int N>
+__device__ __forceinline__ void finish(const Args &a, float (&all)[16], int64_t row, int n, int64_t col,
                                        float bias)
 {
     const cfa_matmul &m = a.m;
-    if (m.bias) {
+    float v[N];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] += bias;
-    }
+    for (int j = 0; j < N; ++j) v[j] = m.bias ? all[j] + bias : all[j];
     if constexpr (GATED) {
-        const bool upper = threadIdx.x & 16;
-        float gate[8], up[8];
+        const bool upper = threadIdx.x & 8;
+        float gate[N / 2], up[N / 2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[2 * j] : v[2 * j + 1], 16);
+        for (int j = 0; j < N / 2; ++j) {
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[2 * j] : v[2 * j + 1], 8);
             gate[j] = upper ? got : v[2 * j];
             up[j] = upper ? v[2 * j + 1] : got;
         }
         activate(gate, m.act);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gate[j] *= up[j];
-        store<8>(a, gate, row + (upper ? 1 : 0), 2, n - (upper ? 1 : 0), col);
+        for (int j = 0; j < N / 2; ++j) gate[j] *= up[j];
+        store<N / 2>(a, gate, row + (upper ? 1 : 0), 2, n - (upper ? 1 : 0), col);
     } else {
         activate(v, m.act);
-        store<16>(a, v, row, 1, n, col);
+        store<N>(a, v, row, 1, n, col);
     }
 }
 
@@ -481,33 +505,36 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
 {
     extern __shared__ uint8_t raw[];
     Shared *s = reinterpret_cast<Shared *>(raw);
-    const uint32_t ring = (smem_addr(raw) + (uint32_t)sizeof(Shared) + 1023u) & ~1023u;
+    const uint32_t ring = (smem_addr(raw) + shared_bytes(a.m.n_groups) + 1023u) & ~1023u;
     const uint32_t x_rows = PAIR ? a.bn / 2 : a.bn;
     const uint32_t w_bytes = a.fr * kRowBytes, x_bytes = x_rows * kRowBytes;
     const uint32_t block = w_bytes + x_bytes, stage = block * a.deep;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = PAIR || a.split > 1 ? cluster_rank() : 0;
-    const uint32_t ctas = PAIR ? 2 : a.split; /* that share a tile */
+    const uint32_t share = PAIR ? 1 : a.split; /* log2 of the CTAs that share a tile */
+    const uint32_t rank = share ? cluster_rank() : 0;
     const uint32_t per_cta = GATED ? a.fr / 2 : a.fr, features = (PAIR ? 2 : 1) * per_cta;
     const cfa_matmul &m = a.m;
     const uint32_t full = smem_addr(s->full), empty = smem_addr(s->empty);
     const uint32_t acc_full = smem_addr(s->acc_full), acc_empty = smem_addr(s->acc_empty);
 
-    if (threadIdx.x == kLoader * 32) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap) : "memory");
-    }
-    if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < a.stages; ++i) {
-            mbar_init(full + 8 * i, 1);
-            mbar_init(empty + 8 * i, 1);
+    /* The loader sets the barriers up and, where the host could count the tiles, goes on to its loads
+     * while the others still wait for the tensor memory. */
+    if (warp == kLoader) {
+        if ((uint32_t)lane < a.stages) {
+            mbar_init(full + 8 * lane, 1);
+            mbar_init(empty + 8 * lane, 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, PAIR ? 8 : 4);
+        if (lane < 2) {
+            mbar_init(acc_full + 8 * lane, 1);
+            mbar_init(acc_empty + 8 * lane, PAIR ? 8 : 4);
         }
-        s->dead = 0;
+        if (lane == 0) {
+            s->dead = 0;
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap[0]) : "memory");
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == kIssuer) {
         if constexpr (PAIR) {
@@ -526,14 +553,14 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (warp == 0) { /* the groups' rows and tiles */
+    if (m.offs && warp == 0) { /* the groups' rows and tiles */
         int32_t tiles = 0;
         for (int32_t g0 = 0; g0 < m.n_groups; g0 += 32) {
             const int32_t g = g0 + lane;
             int32_t r0 = 0, r1 = 0, n = 0;
             if (g < m.n_groups) {
-                r0 = m.offs ? m.offs[g] : 0;
-                r1 = m.offs ? m.offs[g + 1] : (int32_t)m.tokens;
+                r0 = m.offs[g];
+                r1 = m.offs[g + 1];
                 n = (int32_t)(((uint32_t)(r1 - r0) + a.bn - 1) / a.bn * a.f_tiles);
             }
             int32_t sum = n;
@@ -543,28 +570,33 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 if (lane >= o) sum += before;
             }
             if (g < m.n_groups) {
-                s->first[g] = tiles + sum - n;
-                s->row[g] = r0;
-                s->row[g + 1] = r1;
+                s->group[2 * g] = tiles + sum - n;
+                s->group[2 * g + 1] = r0;
+                if (g + 1 == m.n_groups) s->group[2 * g + 3] = r1;
             }
             tiles += __shfl_sync(0xFFFFFFFFu, sum, 31);
-            __syncwarp();
         }
-        if (lane == 0) s->first[m.n_groups] = s->total = tiles;
+        if (lane == 0) s->group[2 * m.n_groups] = s->total = tiles;
     }
     fence_before();
-    __syncthreads();
-    if constexpr (PAIR) cluster_sync();
+    if constexpr (PAIR) {
+        __syncthreads();
+        cluster_sync();
+    } else if (warp == kLoader && !m.offs) {
+        __syncwarp();
+        asm volatile("barrier.cta.arrive 1, %0;" ::"n"(kThreads) : "memory");
+    } else {
+        asm volatile("barrier.cta.sync 1, %0;" ::"n"(kThreads) : "memory");
+    }
     fence_after();
-    const uint32_t tmem = s->tmem;
-    const int32_t total = s->total;
-    const int32_t stride = (int32_t)(gridDim.x / ctas), begin = (int32_t)(blockIdx.x / ctas);
+    const int32_t total = m.offs ? s->total : a.total;
+    const int32_t stride = (int32_t)(gridDim.x >> share), begin = (int32_t)(blockIdx.x >> share);
     /* this CTA's part of the columns */
-    const uint32_t k0 = PAIR ? 0 : rank * a.steps / a.split;
-    const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps / a.split;
-    const bool sync_tiles = !PAIR && a.split > 1;
+    const uint32_t k0 = PAIR ? 0 : rank * a.steps >> share;
+    const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps >> share;
+    const bool sync_tiles = !PAIR && share > 0;
     const uint32_t deep = a.deep, stages = a.stages;
-    const bool wide = a.wide;
+    const uint32_t at_once_to = a.wide ? a.whole : 0; /* blocks that a stage's loads can bring at once */
     bool ok = true;
 
     if (warp == kLoader) {
@@ -580,52 +612,46 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 if constexpr (PAIR) half = rank * (((uint32_t)o.rows + 31u) / 32u * 16u);
                 const int32_t row = o.row + (int32_t)half;
                 const int32_t f = (int32_t)o.feature + (PAIR ? (int32_t)(rank * per_cta) : 0);
-                /* of x, as many boxes as hold the rows in use (of a pair, in each half) */
                 const uint32_t in_use = PAIR ? ((uint32_t)o.rows + 31u) / 32u * 16u
                                              : (uint32_t)o.rows;
-                const uint32_t boxes = (in_use + a.x_box - 1) / a.x_box;
-                const bool x_whole = wide && a.x_box == x_rows;
-                const uint32_t x_loaded = x_whole ? deep * x_bytes
-                                                  : boxes * a.x_box * kRowBytes;
-                const uint32_t w_loaded = deep * w_bytes;
+                /* the lowest box of x that holds the rows in use */
+                uint32_t box = 0;
+                while (box + 1 < kBoxes && a.x_box[box + 1] >= in_use) ++box;
+                const CUtensorMap *const xmap = a.xmap + box, *const xtail = a.xtail + box;
+                const uint32_t x_one = a.x_box[box] * kRowBytes;
+                const uint32_t w_loaded = deep * w_bytes, all = w_loaded + deep * x_one;
                 for (uint32_t k = k0; k < k1; k += deep) {
                     ok = ok && mbar_wait(empty + 8 * at, phase, s);
                     if (!ok) break;
                     const uint32_t blocks = min(deep, k1 - k);
                     const uint32_t dst = ring + at * stage, dst_x = dst + w_loaded;
+                    /* all blocks of the stage at once, unless the one that lacks columns is among
+                     * them */
+                    const bool at_once = k + blocks <= at_once_to;
                     uint32_t bar = full + 8 * at;
                     if (!PAIR || rank == 0) {
-                        const uint32_t bytes = (wide ? w_loaded : blocks * w_bytes) +
-                                               (x_whole ? x_loaded : blocks * x_loaded);
+                        const uint32_t bytes = at_once ? all : blocks * (w_bytes + x_one);
                         mbar_expect_tx(bar, PAIR ? 2 * bytes : bytes);
                     }
                     if constexpr (PAIR) bar = map_to(bar, 0);
-                    if (wide) {
+                    if (at_once) {
                         if constexpr (GATED)
-                            load5<PAIR>(dst, &a.wmap, 0, 0, 2 * o.group, f / 16, (int32_t)k, bar);
+                            load5<PAIR>(dst, &a.wmap, 0, 0, 2 * o.group, f / 8, (int32_t)k, bar);
                         else load4<PAIR>(dst, &a.wmap, 0, f, (int32_t)k, o.group, bar);
+                        load3<PAIR>(dst_x, xmap, 0, row, (int32_t)k, bar);
                     } else {
                         for (uint32_t i = 0; i < blocks; ++i) {
                             const int32_t c = (int32_t)((k + i) * kDepth);
+                            const uint32_t to = dst + i * w_bytes;
                             if constexpr (GATED) {
-                                for (uint32_t q = 0; q < a.fr / 32; ++q)
-                                    load4<PAIR>(dst + i * w_bytes + q * 32 * kRowBytes, &a.wmap, c,
-                                                f + (int32_t)(16 * q), 0, o.group, bar);
+                                for (uint32_t q = 0; q < a.fr / 16; ++q)
+                                    load4<PAIR>(to + q * 16 * kRowBytes, &a.wtail, c,
+                                                f + (int32_t)(8 * q), 0, o.group, bar);
                             } else {
-                                load3<PAIR>(dst + i * w_bytes, &a.wmap, c, f, o.group, bar);
+                                load3<PAIR>(to, &a.wtail, c, f, o.group, bar);
                             }
+                            load3<PAIR>(dst_x + i * x_one, xtail, c, row, 0, bar);
                         }
-                    }
-                    if (x_whole) {
-                        load3<PAIR>(dst_x, &a.xmap, 0, row, (int32_t)k, bar);
-                    } else {
-                        for (uint32_t i = 0; i < blocks; ++i)
-                            for (uint32_t q = 0; q < boxes; ++q) {
-                                const uint32_t to = dst_x + i * x_bytes + q * a.x_box * kRowBytes;
-                                const int32_t r = row + (int32_t)(q * a.x_box);
-                                if (wide) load3<PAIR>(to, &a.xmap, 0, r, (int32_t)(k + i), bar);
-                                else load3<PAIR>(to, &a.xmap, (int32_t)((k + i) * kDepth), r, 0, bar);
-                            }
                     }
                     ++issued;
                     if (++at == stages) {
@@ -635,14 +661,14 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 }
                 if (sync_tiles) {
                     cluster_sync();
-                    cluster_sync();
+                    cluster_done();
                 }
             }
             if (*(volatile int *)&s->dead) drain(a, s, issued, PAIR && rank);
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
-                cluster_sync();
+                cluster_done();
             }
         }
         __syncwarp();
@@ -650,9 +676,10 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         if (elect_one()) {
             uint32_t at = 0, phase = 0, buf = 0, buf_phase = 1;
             int32_t group = 0;
+            const uint32_t tmem = s->tmem;
             /* descriptors count in 16 bytes */
             const uint32_t w_first = matrix_low(ring), x_first = w_first + (deep * w_bytes >> 4);
-            const uint32_t stage_on = stage >> 4, w_on = w_bytes >> 4, x_on = x_bytes >> 4;
+            const uint32_t stage_on = stage >> 4, w_on = w_bytes >> 4;
             for (int32_t t = begin; t < total; t += stride) {
                 if (!PAIR || rank == 0) {
                     const Tile o = tile_at(a, s, t, &group, features);
@@ -660,6 +687,11 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     const uint32_t inst = instruction(m.f16, PAIR ? 256u : 128u,
                                                       ((uint32_t)o.rows + unit - 1) / unit * unit);
                     const uint32_t d = tmem + buf * (a.tmem_cols / 2);
+                    const uint32_t in_use = PAIR ? ((uint32_t)o.rows + 31u) / 32u * 16u
+                                                 : (uint32_t)o.rows;
+                    uint32_t box = 0;
+                    while (box + 1 < kBoxes && a.x_box[box + 1] >= in_use) ++box;
+                    const uint32_t x_on = a.x_box[box] * kRowBytes >> 4;
                     /* each stage's barrier is looked at before the products of the one before are
                      * issued, so that the look costs no time of its own */
                     bool there = mbar_try_wait(full + 8 * at, phase);
@@ -672,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                         fence_after();
                         uint32_t blocks = min(deep, k1 - k);
                         uint32_t w = w_first + at * stage_on, x = x_first + at * stage_on;
-                        const uint32_t done = empty + 8 * at;
+                                                const uint32_t done = empty + 8 * at;
                         if (++at == stages) {
                             at = 0;
                             phase ^= 1;
@@ -695,88 +727,108 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 }
                 if (sync_tiles) {
                     cluster_sync();
-                    cluster_sync();
+                    cluster_done();
                 }
             }
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
-                cluster_sync();
+                cluster_done();
             }
         }
         __syncwarp();
     } else {
         uint32_t buf = 0, buf_phase = 0;
         int32_t group = 0;
-        const uint32_t lanes = (uint32_t)warp * 32u << 16;
+        const uint32_t lanes = s->tmem + ((uint32_t)warp * 32u << 16);
         float *partial = reinterpret_cast<float *>(
             raw + (ring - smem_addr(raw)) + a.stages * stage); /* [bn][128], split > 1 */
-        for (int32_t t = begin; t < total; t += stride) {
+        /* The first tile is gone through twice: first without a wait, without rows and so without
+         * stores, which brings the code into the instruction cache while the sums are under way. */
+        bool dry = true;
+        for (int32_t t = begin; t < total;) {
             const Tile o = tile_at(a, s, t, &group, features);
-            int64_t col = o.feature + (GATED ? warp * 16 + (lane & 15) : warp * 32 + lane);
+            int64_t col = o.feature + (GATED ? warp * 16 + (lane >> 4) * 8 + (lane & 7)
+                                             : warp * 32 + lane);
             if constexpr (PAIR) col += rank * per_cta;
             if ((uint32_t)(warp * 32 + lane) >= a.fr) col = a.outs; /* a lane without a row */
             float bias = 0.0f; /* of the lane's weight row */
             if (m.bias && col < a.outs) {
-                const int64_t at = col + (GATED && lane >= 16 ? a.outs : 0);
+                const int64_t at = col + (GATED && (lane & 8) ? a.outs : 0);
                 bias = m.bias_f32 ? static_cast<const float *>(m.bias)[at]
                                   : value(m.bias, at, m.f16);
             }
-            ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            fence_after();
-            const uint32_t src = tmem + lanes + buf * (a.tmem_cols / 2);
+            if (!dry) {
+                ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                fence_after();
+            }
+            const uint32_t src = lanes + buf * (a.tmem_cols / 2);
+            int32_t c0 = 0, c1 = o.rows;
+            uint32_t sharers = 0;
             float v[16];
-            if (!sync_tiles) {
+            if (sync_tiles) {
                 for (int32_t c = 0; ok && c < o.rows; c += 16) {
                     __syncwarp();
-                    tmem_load(src + c, v);
-                    finish<GATED>(a, v, o.row + c, o.rows - c, col, bias);
-                }
-            } else {
-                for (int32_t c = 0; ok && c < o.rows; c += 16) {
                     tmem_load(src + c, v);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         partial[(c + j) * kRows + warp * 32 + lane] = v[j];
                 }
+                if (!dry) cluster_sync();
+                /* each CTA of the cluster finishes its share of the tokens */
+                const int32_t even = (((o.rows - 1) >> share) + 2) & ~1;
+                c0 = (int32_t)rank * even;
+                c1 = min(o.rows, c0 + even);
+                sharers = dry ? 1u : 1u << share;
+            }
+            const bool few = c1 - c0 <= 4;
+            const uint32_t base = smem_addr(partial) + (uint32_t)(warp * 32 + lane) * 4u;
+            if (dry) c1 = min(c1, c0 + 1);
+            for (int32_t c = c0; ok && c < c1; c += 16) {
+                __syncwarp();
+                if (sharers == 0) {
+                    tmem_load(src + c, v);
+                } else {
+                    float p[4][16]; /* all on their way before the first is added */
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t from = map_to(base, dry ? rank : (uint32_t)r % sharers) +
+                                              (uint32_t)c * (kRows * 4u);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            p[r][j] = 0.0f;
+                            if (r < sharers && j < c1 - c)
+                                asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                                             : "=f"(p[r][j])
+                                             : "r"(from + (uint32_t)j * (kRows * 4u)));
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        v[j] = ((p[0][j] + p[1][j]) + p[2][j]) + p[3][j];
+                }
+                const int n = dry ? 0 : c1 - c;
+                if (few) finish<GATED, 4>(a, v, o.row + c, n, col, bias);
+                else finish<GATED, 16>(a, v, o.row + c, n, col, bias);
+            }
+            if (dry) {
+                dry = false;
+                continue;
             }
             fence_before();
             __syncwarp();
             if (lane == 0) {
                 const uint32_t bar = acc_empty + 8 * buf;
-                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                /* relaxed: the sums have been read, and the stores of y need not have ended */
+                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
                                  PAIR ? map_to(bar, 0) : bar)
                              : "memory");
             }
             if (buf) buf_phase ^= 1;
             buf ^= 1;
-            if (sync_tiles) {
-                cluster_sync();
-                /* each CTA of the cluster finishes its share of the tokens */
-                const uint32_t share = (((uint32_t)o.rows + a.split - 1) / a.split + 1u) & ~1u;
-                const int32_t c0 = (int32_t)(rank * share);
-                const int32_t c1 = min(o.rows, c0 + (int32_t)share);
-                const uint32_t base = smem_addr(partial) + (uint32_t)(warp * 32 + lane) * 4u;
-                for (int32_t c = c0; ok && c < c1; c += 16) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-                    for (uint32_t r = 0; r < a.split; ++r) {
-                        const uint32_t from = map_to(base, r);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            float p = 0.0f;
-                            if (c + j < c1)
-                                asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                                             : "=f"(p)
-                                             : "r"(from + (uint32_t)(c + j) * (kRows * 4u)));
-                            v[j] += p;
-                        }
-                    }
-                    finish<GATED>(a, v, o.row + c, c1 - c, col, bias);
-                }
-                cluster_sync();
-            }
+            if (sync_tiles) cluster_done();
+            t += stride;
         }
     }
 
@@ -785,6 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     if (threadIdx.x == 0 && *(volatile int *)&s->dead) atomicMax(&g_status, 1);
     if constexpr (PAIR) cluster_sync();
     if (warp == kIssuer) {
+        const uint32_t tmem = s->tmem;
         if constexpr (PAIR)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                          "r"(a.tmem_cols));
@@ -888,17 +941,16 @@ cudaError_t clusters_of(Device &d, bool pair, bool gated, unsigned size, int *n)
 /* How a product is cut. */
 struct Cut {
     bool pair;
-    uint32_t bn, fr, split;
+    uint32_t bn, fr, split; /* split: log2 */
 };
 
 /* Microseconds that one block of kDepth columns takes a CTA (a pair): the four products and what
  * their issue costs, measured with the loads left out. */
 double block_us(bool pair, uint32_t bn, uint32_t fr)
 {
-    if (pair) return bn <= 128 ? 0.22 : 0.22 + (bn - 128) * (0.29 - 0.22) / 128;
-    if (bn <= 32) return fr <= 64 ? 0.117 : 0.14;
-    if (bn <= 64) return 0.18;
-    return bn <= 128 ? 0.212 : 0.212 + (bn - 128) * (0.29 - 0.212) / 128;
+    if (pair) return bn <= 128 ? 0.16 : 0.16 + (bn - 128) * (0.29 - 0.16) / 128;
+    if (bn <= 64) return fr <= 64 ? 0.1 : 0.11;
+    return bn <= 128 ? 0.21 : 0.21 + (bn - 128) * (0.29 - 0.21) / 128;
 }
 
 /* The cut with the least estimated time.  A launch takes its latency, and the longest of
@@ -928,7 +980,7 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
             if (bn == last) continue;
             last = bn;
             const int64_t n_tiles = (rows + bn - 1) / bn * busy;
-            for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += m->gated ? 32 : 8) {
+            for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += m->gated ? 16 : 8) {
                 const uint32_t features = (pair ? 2 : 1) * (m->gated ? fr / 2 : fr);
                 const int64_t tiles = n_tiles * ((outs + features - 1) / features);
                 for (uint32_t log = 0; log < 3; ++log) {
@@ -945,7 +997,7 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
                     us += kLaunch + kSplit[log];
                     if (us < least * 0.995) {
                         least = us;
-                        best = {pair != 0, bn, fr, split};
+                        best = {pair != 0, bn, fr, log};
                     }
                 }
             }
@@ -992,22 +1044,25 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const uint32_t features = (pair ? 2 : 1) * (gated ? a.fr / 2 : a.fr);
     a.f_tiles = (uint32_t)((a.outs + features - 1) / features);
     const int64_t most = ((m->tokens + a.bn - 1) / a.bn + m->busy - 1) * a.f_tiles;
+    a.total = (int32_t)most;
     const uint64_t two = m->y_f32 ? 8 : 4;
     a.pairs = (((uintptr_t)m->y | (uintptr_t)m->residual) % two) == 0 &&
               (m->tokens <= 1 || (m->y_stride % 2 == 0 && (!m->residual || m->r_stride % 2 == 0)));
     const uint32_t x_rows = pair ? a.bn / 2 : a.bn;
-    a.x_box = m->offs && x_rows % 32 == 0 ? 32 : x_rows;
+    a.x_box[0] = x_rows;
+    if (m->offs) /* ragged groups: half as high, a quarter, an eighth */
+        for (uint32_t i = 1; i < kBoxes; ++i) a.x_box[i] = (x_rows >> i) / 8 * 8;
     const uint32_t block = (a.fr + x_rows) * kRowBytes;
     for (a.deep = 4; a.deep > 1 && block * a.deep > kDeepBytes; a.deep /= 2) {
     }
     const uint32_t stage = block * a.deep;
-    /* whole blocks of columns, so that they can be a dimension of their own */
-    a.wide = m->cols % kDepth == 0 && (!gated || a.outs % 16 == 0);
+    a.wide = !gated || a.outs % 8 == 0;
+    a.whole = (uint32_t)(m->cols / kDepth);
     /* the products read kRows rows of each block of w, whatever lies behind the a.fr of them */
     const uint32_t after = a.fr + a.deep * x_rows;
     const uint32_t behind = kRows > after ? (kRows - after) * kRowBytes : 0;
-    const uint32_t partial = a.split > 1 ? a.bn * kRows * 4u : 0u;
-    const uint32_t left = kSmem - (uint32_t)sizeof(Shared) - 1024u -
+    const uint32_t partial = a.split ? a.bn * kRows * 4u : 0u;
+    const uint32_t left = kSmem - shared_bytes(m->n_groups) - 1024u -
                           (partial > behind ? partial : behind);
     a.stages = left / stage < kMaxStages ? left / stage : kMaxStages;
     for (a.tmem_cols = 32; a.tmem_cols < 2 * a.bn; a.tmem_cols *= 2) {
@@ -1020,7 +1075,7 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
         if (e) return e;
         d.ready.fetch_or(bit);
     }
-    const unsigned size = pair ? 2 : a.split;
+    const unsigned size = pair ? 2 : 1u << a.split;
     int clusters = sms;
     if (size > 1) {
         e = clusters_of(d, pair, gated, size, &clusters);
@@ -1031,40 +1086,48 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const cuuint64_t k = (cuuint64_t)m->cols, whole = (k + 7) / 8 * 8;
     const cuuint64_t wld = (m->w_rows > 1 ? (cuuint64_t)m->w_stride : whole) * 2;
     const cuuint64_t xld = (m->tokens > 1 ? (cuuint64_t)m->x_stride : whole) * 2;
-    bool fine;
-    const cuuint64_t deep = kRowBytes, groups = (cuuint64_t)m->n_groups; /* a block further: bytes */
+    /* The maps of whole blocks have the blocks as a dimension, so that one load brings several. */
+    bool fine = true;
+    const cuuint64_t on = kRowBytes, groups = (cuuint64_t)m->n_groups, blocks = a.whole;
     const cuuint64_t outs = (cuuint64_t)a.outs, rows = (cuuint64_t)m->w_rows;
-    if (a.wide && gated) { /* 64 columns, 16 rows, gate or up of each group, 16 rows on, block */
-        const cuuint64_t dim[5] = {kDepth, 16, 2 * groups, outs / 16, k / kDepth};
-        const cuuint64_t stride[4] = {wld, wld * outs, wld * 16, deep};
-        const cuuint32_t box[5] = {kDepth, 16, 2, a.fr / 32, a.deep};
-        fine = encode(&a.wmap, m->f16, m->w, 5, dim, stride, box);
-    } else if (gated) {
-        const cuuint64_t dim[4] = {k, outs, 2, groups};
-        const cuuint64_t stride[3] = {wld, wld * outs, wld * outs * 2};
-        const cuuint32_t box[4] = {kDepth, 16, 2, 1};
-        fine = encode(&a.wmap, m->f16, m->w, 4, dim, stride, box);
-    } else if (a.wide) {
-        const cuuint64_t dim[4] = {kDepth, rows, k / kDepth, groups};
-        const cuuint64_t stride[3] = {wld, deep, wld * rows};
-        const cuuint32_t box[4] = {kDepth, a.fr, a.deep, 1};
-        fine = encode(&a.wmap, m->f16, m->w, 4, dim, stride, box);
-    } else {
-        const cuuint64_t dim[3] = {k, rows, groups};
-        const cuuint64_t stride[2] = {wld, wld * rows};
-        const cuuint32_t box[3] = {kDepth, a.fr, 1};
-        fine = encode(&a.wmap, m->f16, m->w, 3, dim, stride, box);
+    const cuuint64_t tokens = (cuuint64_t)m->tokens;
+    if (a.wide && blocks) {
+        if (gated) { /* 64 columns, 8 rows, gate or up of each group, the next 8 rows, block */
+            const cuuint64_t dim[5] = {kDepth, 8, 2 * groups, outs / 8, blocks};
+            const cuuint64_t stride[4] = {wld, wld * outs, wld * 8, on};
+            const cuuint32_t box[5] = {kDepth, 8, 2, a.fr / 16, a.deep};
+            fine = encode(&a.wmap, m->f16, m->w, 5, dim, stride, box);
+        } else {
+            const cuuint64_t dim[4] = {kDepth, rows, blocks, groups};
+            const cuuint64_t stride[3] = {wld, on, wld * rows};
+            const cuuint32_t box[4] = {kDepth, a.fr, a.deep, 1};
+            fine = encode(&a.wmap, m->f16, m->w, 4, dim, stride, box);
+        }
+        const cuuint64_t dim[3] = {kDepth, tokens, blocks};
+        const cuuint64_t stride[2] = {xld, on};
+        for (uint32_t i = 0; fine && i < kBoxes && a.x_box[i]; ++i) {
+            const cuuint32_t box[3] = {kDepth, a.x_box[i], a.deep};
+            fine = encode(&a.xmap[i], m->f16, m->x, 3, dim, stride, box);
+        }
     }
-    if (fine && a.wide) {
-        const cuuint64_t dim[3] = {kDepth, (cuuint64_t)m->tokens, k / kDepth};
-        const cuuint64_t stride[2] = {xld, deep};
-        const cuuint32_t box[3] = {kDepth, a.x_box, a.x_box == x_rows ? a.deep : 1};
-        fine = encode(&a.xmap, m->f16, m->x, 3, dim, stride, box);
-    } else if (fine) {
-        const cuuint64_t dim[3] = {k, (cuuint64_t)m->tokens, 1};
-        const cuuint64_t stride[2] = {xld, xld * (cuuint64_t)m->tokens};
-        const cuuint32_t box[3] = {kDepth, a.x_box, 1};
-        fine = encode(&a.xmap, m->f16, m->x, 3, dim, stride, box);
+    if (fine && (!a.wide || a.steps > a.whole)) {
+        if (gated) {
+            const cuuint64_t dim[4] = {k, outs, 2, groups};
+            const cuuint64_t stride[3] = {wld, wld * outs, wld * outs * 2};
+            const cuuint32_t box[4] = {kDepth, 8, 2, 1};
+            fine = encode(&a.wtail, m->f16, m->w, 4, dim, stride, box);
+        } else {
+            const cuuint64_t dim[3] = {k, rows, groups};
+            const cuuint64_t stride[2] = {wld, wld * rows};
+            const cuuint32_t box[3] = {kDepth, a.fr, 1};
+            fine = encode(&a.wtail, m->f16, m->w, 3, dim, stride, box);
+        }
+        const cuuint64_t dim[3] = {k, tokens, 1};
+        const cuuint64_t stride[2] = {xld, xld * tokens};
+        for (uint32_t i = 0; fine && i < kBoxes && a.x_box[i]; ++i) {
+            const cuuint32_t box[3] = {kDepth, a.x_box[i], 1};
+            fine = encode(&a.xtail[i], m->f16, m->x, 3, dim, stride, box);
+        }
     }
     if (!fine) return cudaErrorInvalidValue;
 
