@@ -1,15 +1,21 @@
 /*
- * Choice of experts.  One warp a token: each lane holds every 32nd logit, the top_k come out one at
- * a time as the warp's largest key, a key being the fp32 value mapped onto unsigned integers of the
- * same order, with equal keys going to the lowest index.
+ * Choice of experts.  One warp a token: each lane holds R neighbouring logits, so that a group of
+ * experts lies in a few neighbouring lanes.  The top_k come out one at a time as the warp's largest
+ * key, a key being the fp32 value mapped onto unsigned integers of the same order; every lane keeps
+ * the best of its own, and only the lane that has just given its best looks for the next one.  Equal
+ * keys go to the lowest index.
+ *
+ * Up to a few thousand tokens this is bound by the launch and by the chain of loads, exponentials and
+ * top_k warp reductions of one token; the bytes (4 KiB read and written per token of 256 fp32 logits
+ * at the most) would take a tenth of that.
  */
 #include <math.h>
 
-#include "cfa_device.cuh"
-#include "cfa_ops.h"
-
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include "cfa_device.cuh"
+#include "cfa_ops.h"
 
 namespace {
 
@@ -24,11 +30,49 @@ __device__ __forceinline__ uint32_t order_of(float v)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ float logit(const cfa_route_args &a, int64_t i)
+__device__ __forceinline__ float from_bits(uint32_t b, int32_t dtype) /* of a 2-byte type */
 {
-    if (a.dtype == CFA_DTYPE_F32) return static_cast<const float *>(a.logits)[i];
-    if (a.dtype == CFA_DTYPE_F16) return __half2float(static_cast<const __half *>(a.logits)[i]);
-    return __bfloat162float(static_cast<const __nv_bfloat16 *>(a.logits)[i]);
+    if (dtype == CFA_DTYPE_F16) return __half2float(__ushort_as_half((unsigned short)b));
+    return __bfloat162float(__ushort_as_bfloat16((unsigned short)b));
+}
+
+/* The lane's R logits, -inf behind the last.  (All loads go past L1: see cfa_matmul.cu.) */
+template <int R>
+__device__ __forceinline__ void load(const cfa_route_args &a, const uint8_t *row, int first, bool vec,
+                                     float (&v)[R])
+{
+    if (a.dtype == CFA_DTYPE_F32) {
+        const float *p = reinterpret_cast<const float *>(row) + first;
+        if (R % 4 == 0 && vec) {
+#pragma unroll
+            for (int r = 0; r + 3 < R; r += 4) {
+                const float4 q = __ldcg(reinterpret_cast<const float4 *>(p + r));
+                v[r] = q.x;
+                v[r + 1] = q.y;
+                v[r + 2] = q.z;
+                v[r + 3] = q.w;
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) v[r] = first + r < a.experts ? __ldcg(p + r) : -INFINITY;
+        }
+    } else {
+        const unsigned short *p = reinterpret_cast<const unsigned short *>(row) + first;
+        if (R % 4 == 0 && vec) {
+#pragma unroll
+            for (int r = 0; r + 3 < R; r += 4) {
+                const uint2 q = __ldcg(reinterpret_cast<const uint2 *>(p + r));
+                v[r] = from_bits(q.x & 0xFFFFu, a.dtype);
+                v[r + 1] = from_bits(q.x >> 16, a.dtype);
+                v[r + 2] = from_bits(q.y & 0xFFFFu, a.dtype);
+                v[r + 3] = from_bits(q.y >> 16, a.dtype);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                v[r] = first + r < a.experts ? from_bits(__ldcg(p + r), a.dtype) : -INFINITY;
+        }
+    }
 }
 
 __device__ __forceinline__ float warp_max(float v)
@@ -45,6 +89,61 @@ __device__ __forceinline__ float warp_add(float v)
     return v;
 }
 
+/* (first, second) of two values together with another two in descending order */
+__device__ __forceinline__ void merge(float &first, float &second, float a, float b)
+{
+    const float low = fminf(first, a);
+    first = fmaxf(first, a);
+    second = fmaxf(fmaxf(second, b), low);
+}
+
+/* Which lanes' keys lie in a group that is kept; by lanes where every lane's keys lie in one group of
+ * 2^n neighbouring lanes, otherwise through shared memory. */
+template <int R>
+__device__ __forceinline__ void keep_groups(const cfa_route_args &a, float (&key)[R], float *mine,
+                                            int lane, bool sum_two)
+{
+    const int size = a.experts / a.groups, lanes = size / R;
+    if (size == lanes * R && (lanes & (lanes - 1)) == 0) {
+        float first = -INFINITY, second = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < R; ++r) merge(first, second, key[r], -INFINITY);
+        for (int o = 1; o < lanes; o <<= 1)
+            merge(first, second, __shfl_xor_sync(kAll, first, o), __shfl_xor_sync(kAll, second, o));
+        const uint32_t best = order_of(sum_two && size > 1 ? first + second : first);
+        const int group = lane / lanes;
+        int before = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t other = __shfl_sync(kAll, best, g * lanes);
+            before += other > best || (other == best && g < group);
+        }
+        if (before >= a.top_groups) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) key[r] = -INFINITY;
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (lane * R + r < a.experts) mine[lane * R + r] = key[r];
+    __syncwarp();
+    float first = -INFINITY, second = -INFINITY;
+    if (lane < a.groups)
+        for (int i = 0; i < size; ++i) merge(first, second, mine[lane * size + i], -INFINITY);
+    const uint32_t best = order_of(sum_two && size > 1 ? first + second : first);
+    int before = 0;
+    for (int g = 0; g < a.groups; ++g) {
+        const uint32_t other = __shfl_sync(kAll, best, g);
+        before += other > best || (other == best && g < lane);
+    }
+    const uint32_t kept = __ballot_sync(kAll, lane < a.groups && before < a.top_groups);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int e = lane * R + r;
+        if (e < a.experts && !(kept >> (e / size) & 1u)) key[r] = -INFINITY;
+    }
+}
+
 /* R: logits per lane. */
 template <int R>
 __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_args a)
@@ -55,103 +154,81 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (t >= a.tokens) return;
 
+    const int es = a.dtype == CFA_DTYPE_F32 ? 4 : 2;
+    const uint8_t *row = static_cast<const uint8_t *>(a.logits) + t * a.logits_stride * es;
+    const bool vec = a.experts == 32 * R && ((uintptr_t)row & (uintptr_t)(4 * es - 1)) == 0;
     float v[R], key[R];
+    load<R>(a, row, lane * R, vec, v);
     float top = -INFINITY;
     bool nan = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int e = r * 32 + lane;
-        v[r] = e < a.experts ? logit(a, t * a.logits_stride + e) : -INFINITY;
         nan |= v[r] != v[r];
         top = fmaxf(top, v[r]);
     }
     const bool softmax = a.scoring == CFA_SCORE_SOFTMAX;
+    const bool renormalize = a.flags & CFA_ROUTE_RENORMALIZE;
     float norm = 1.0f;
     if (softmax) {
-        top = warp_max(top);
         nan = __any_sync(kAll, nan);
-        float sum = 0.0f;
+        if (!renormalize || a.bias) { /* the sum over all of them counts */
+            top = warp_max(top);
+            float sum = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 32 + lane < a.experts) sum += v[r] > -INFINITY ? expf(v[r] - top) : 0.0f;
-        norm = nan ? NAN : warp_add(sum);
+            for (int r = 0; r < R; ++r) sum += v[r] > -INFINITY ? expf(v[r] - top) : 0.0f;
+            norm = nan ? NAN : warp_add(sum);
+        }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int e = r * 32 + lane;
+        const int e = lane * R + r;
         float k = softmax ? v[r] : 1.0f / (1.0f + expf(-v[r]));
         if (a.bias && e < a.experts)
-            k = (softmax ? expf(v[r] - top) / norm : k) + a.bias[e];
+            k = (softmax ? expf(v[r] - top) / norm : k) + __ldcg(a.bias + e);
         key[r] = v[r] > -INFINITY ? k : -INFINITY;
     }
+    if (a.groups > 1) keep_groups<R>(a, key, s_key + warp * a.experts, lane, !softmax);
 
-    if (a.groups > 1) {
-        float *mine = s_key + warp * a.experts;
+    uint32_t k[R], best = 0; /* the lane's best key, its place and its logit */
+    int at = 0;
+    float z = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 32 + lane < a.experts) mine[r * 32 + lane] = key[r];
-        __syncwarp();
-        const int size = a.experts / a.groups;
-        float first = -INFINITY, second = -INFINITY;
-        if (lane < a.groups)
-            for (int i = 0; i < size; ++i) {
-                const float k = mine[lane * size + i];
-                if (!(k > -INFINITY)) continue;
-                if (k > first) {
-                    second = first;
-                    first = k;
-                } else if (k > second) {
-                    second = k;
-                }
-            }
-        const float best = softmax || size == 1 ? first : first + second;
-        /* a group is kept if fewer than top_groups come before it */
-        int before = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const float o = __shfl_sync(kAll, best, g);
-            const uint32_t x = order_of(o), y = order_of(best);
-            before += x > y || (x == y && g < lane);
-        }
-        const uint32_t kept = __ballot_sync(kAll, lane < a.groups && before < a.top_groups);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int e = r * 32 + lane;
-            if (e < a.experts && !(kept >> (e / size) & 1u)) key[r] = -INFINITY;
+    for (int r = R - 1; r >= 0; --r) {
+        k[r] = order_of(key[r]);
+        if (k[r] >= best) {
+            best = k[r];
+            at = r;
+            z = v[r];
         }
     }
-
-    uint32_t k[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) k[r] = order_of(key[r]);
     float chosen = -INFINITY; /* lane j: the logit of choice j */
     int id = -1;
     for (int j = 0; j < a.top_k; ++j) {
-        uint32_t best = 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r) best = max(best, k[r]);
-        best = __reduce_max_sync(kAll, best);
-        if (best == 0) break; /* nothing left to choose */
-        uint32_t e = kAll;
-        float z = 0.0f;
-#pragma unroll
-        for (int r = R - 1; r >= 0; --r)
-            if (k[r] == best) {
-                e = r * 32 + lane;
-                z = v[r];
-            }
-        const uint32_t win = __reduce_min_sync(kAll, e);
-        z = __shfl_sync(kAll, z, win & 31u);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 32 + lane == win) k[r] = 0;
+        const uint32_t most = __reduce_max_sync(kAll, best);
+        if (most == 0) break; /* nothing left to choose */
+        const int win = __ffs(__ballot_sync(kAll, best == most)) - 1;
+        const int e = __shfl_sync(kAll, lane * R + at, win);
+        const float logit = __shfl_sync(kAll, z, win);
         if (lane == j) {
-            chosen = z;
-            id = (int)win;
+            chosen = logit;
+            id = e;
+        }
+        if (lane == win) {
+            const int gone = at;
+            best = 0;
+#pragma unroll
+            for (int r = R - 1; r >= 0; --r) {
+                if (r == gone) k[r] = 0;
+                if (k[r] >= best) {
+                    best = k[r];
+                    at = r;
+                    z = v[r];
+                }
+            }
         }
     }
 
     float w = 0.0f;
-    const bool renormalize = a.flags & CFA_ROUTE_RENORMALIZE;
     if (softmax) {
         if (renormalize) {
             const float m = warp_max(chosen);
@@ -190,7 +267,10 @@ cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream)
 {
     if (a->experts <= 32) return launch<1>(*a, stream);
     if (a->experts <= 64) return launch<2>(*a, stream);
+    if (a->experts <= 96) return launch<3>(*a, stream);
     if (a->experts <= 128) return launch<4>(*a, stream);
+    if (a->experts <= 160) return launch<5>(*a, stream);
+    if (a->experts <= 192) return launch<6>(*a, stream);
     if (a->experts <= 256) return launch<8>(*a, stream);
     if (a->experts <= 512) return launch<16>(*a, stream);
     return launch<32>(*a, stream);
