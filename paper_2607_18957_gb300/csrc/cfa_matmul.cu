@@ -38,7 +38,8 @@ constexpr int kThreads = 192;
 constexpr int kLoader = 4, kIssuer = 5;  /* warps; 0 to 3 are the epilogue's */
 constexpr uint32_t kRows = 128;          /* weight rows per CTA, at most */
 constexpr uint32_t kDepth = 64;          /* columns of w and x per block: one 128-byte swizzle row */
-constexpr uint32_t kDeepBytes = 49152;   /* a stage takes more than one block up to this */
+constexpr uint32_t kDeepBytes = 65536;   /* a stage takes more than one block up to this (of a pair,
+                                            whose products take longer: half of it) */
 constexpr uint32_t kRowBytes = kDepth * 2;
 constexpr uint32_t kMaxStages = 32;      /* no more than a warp has lanes */
 constexpr uint32_t kSmem = 232448;       /* all that a CTA may have: one CTA per SM, so that the
@@ -67,6 +68,7 @@ struct Args {
     uint32_t split;      /* log2 of the CTAs per output tile along the columns */
     uint32_t tmem_cols;
     uint32_t release;
+    uint32_t early_w;    /* w, and what tells the groups' rows, is there before the launch's wait */
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
 
@@ -291,11 +293,15 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+/* Loads go past L1, which may hold what an older kernel read there: a launch can start before the one
+ * before it has ended (cfa_launch_ctl), so that its start clears nothing written after it. */
 __device__ __forceinline__ float value(const void *p, int64_t i, int f16)
 {
-    return f16 ? __half2float(static_cast<const __half *>(p)[i])
-               : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    const unsigned short b = __ldcg(static_cast<const unsigned short *>(p) + i);
+    return f16 ? __half2float(__ushort_as_half(b)) : __bfloat162float(__ushort_as_bfloat16(b));
 }
+
+__device__ __forceinline__ float value(const float *p, int64_t i) { return __ldcg(p + i); }
 
 /* One switch for a batch of values, so that they run side by side. */
 template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
@@ -367,7 +373,8 @@ __device__ __forceinline__ void store_one(const cfa_matmul &m, int64_t row, int6
 {
     if (m.residual) {
         const int64_t at = row * m.r_stride + col;
-        v += m.y_f32 ? static_cast<const float *>(m.residual)[at] : value(m.residual, at, m.f16);
+        v += m.y_f32 ? value(static_cast<const float *>(m.residual), at)
+                     : value(m.residual, at, m.f16);
     }
     const int64_t at = row * m.y_stride + col;
     if (m.y_f32) static_cast<float *>(m.y)[at] = v;
@@ -430,10 +437,10 @@ __device__ __forceinline__ void store(const Args &a, float (&v)[N], int64_t row,
             if (first + 2 * i * step >= n) continue;
             const int64_t from = at + 2 * i * step * m.r_stride;
             const float2 r =
-                m.y_f32 ? *reinterpret_cast<const float2 *>(
-                              static_cast<const float *>(m.residual) + from)
-                        : unpack(*reinterpret_cast<const uint32_t *>(
-                                     static_cast<const uint16_t *>(m.residual) + from), m.f16);
+                m.y_f32 ? __ldcg(reinterpret_cast<const float2 *>(
+                              static_cast<const float *>(m.residual) + from))
+                        : unpack(__ldcg(reinterpret_cast<const uint32_t *>(
+                                     static_cast<const uint16_t *>(m.residual) + from)), m.f16);
             o[i].x += r.x;
             o[i].y += r.y;
         }
@@ -500,6 +507,34 @@ __device__ void drain(const Args &a, Shared *s, uint32_t issued, bool second)
     atomicMax(&g_status, word);
 }
 
+/* A stage's blocks of w, from block k on. */
+template <bool PAIR, bool GATED>
+__device__ __forceinline__ void load_w(const Args &a, bool at_once, uint32_t dst, uint32_t blocks,
+                                       uint32_t k, int32_t f, int32_t group, uint32_t bar)
+{
+    if (at_once) {
+        if constexpr (GATED) load5<PAIR>(dst, &a.wmap, 0, 0, 2 * group, f / 8, (int32_t)k, bar);
+        else load4<PAIR>(dst, &a.wmap, 0, f, (int32_t)k, group, bar);
+        return;
+    }
+    for (uint32_t i = 0; i < blocks; ++i, dst += a.fr * kRowBytes) {
+        const int32_t c = (int32_t)((k + i) * kDepth);
+        if constexpr (GATED) {
+            for (uint32_t q = 0; q < a.fr / 16; ++q)
+                load4<PAIR>(dst + q * 16 * kRowBytes, &a.wtail, c, f + (int32_t)(8 * q), 0, group,
+                            bar);
+        } else {
+            load3<PAIR>(dst, &a.wtail, c, f, group, bar);
+        }
+    }
+}
+
+__device__ __forceinline__ void launch_wait(const Args &a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 template <bool PAIR, bool GATED>
 __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_constant__ Args a)
 {
@@ -551,32 +586,49 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         }
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (m.offs && warp == 0) { /* the groups' rows and tiles */
-        int32_t tiles = 0;
-        for (int32_t g0 = 0; g0 < m.n_groups; g0 += 32) {
-            const int32_t g = g0 + lane;
-            int32_t r0 = 0, r1 = 0, n = 0;
-            if (g < m.n_groups) {
-                r0 = m.offs[g];
-                r1 = m.offs[g + 1];
-                n = (int32_t)(((uint32_t)(r1 - r0) + a.bn - 1) / a.bn * a.f_tiles);
+    if (!a.early_w) launch_wait(a);
+    if (m.offs) { /* the groups' rows and tiles */
+        if (m.ids) { /* counted from the pairs themselves */
+            for (int32_t g = threadIdx.x; g < m.n_groups; g += kThreads) s->group[2 * g + 2] = 0;
+            __syncthreads();
+            for (int32_t i = threadIdx.x; i < m.n_ids; i += kThreads) {
+                const int64_t g = (int64_t)__ldcg(m.ids + i) - m.first;
+                if (g >= 0 && g < m.n_groups) atomicAdd(&s->group[2 * g + 2], 1);
             }
-            int32_t sum = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int32_t before = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-                if (lane >= o) sum += before;
-            }
-            if (g < m.n_groups) {
-                s->group[2 * g] = tiles + sum - n;
-                s->group[2 * g + 1] = r0;
-                if (g + 1 == m.n_groups) s->group[2 * g + 3] = r1;
-            }
-            tiles += __shfl_sync(0xFFFFFFFFu, sum, 31);
+            __syncthreads();
         }
-        if (lane == 0) s->group[2 * m.n_groups] = s->total = tiles;
+        if (warp == 0) {
+            int32_t tiles = 0, rows = 0;
+            for (int32_t g0 = 0; g0 < m.n_groups; g0 += 32) {
+                const int32_t g = g0 + lane;
+                int32_t r = 0, n = 0;
+                if (g < m.n_groups) {
+                    r = m.ids ? s->group[2 * g + 2] : __ldcg(m.offs + g + 1) - __ldcg(m.offs + g);
+                    n = (int32_t)(((uint32_t)r + a.bn - 1) / a.bn * a.f_tiles);
+                }
+                int32_t sum = n, row = r;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int32_t x = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                    const int32_t y = __shfl_up_sync(0xFFFFFFFFu, row, o);
+                    if (lane >= o) {
+                        sum += x;
+                        row += y;
+                    }
+                }
+                __syncwarp();
+                if (g < m.n_groups) { /* what comes before the next group */
+                    s->group[2 * g + 2] = tiles + sum;
+                    s->group[2 * g + 3] = rows + row;
+                }
+                tiles += __shfl_sync(0xFFFFFFFFu, sum, 31);
+                rows += __shfl_sync(0xFFFFFFFFu, row, 31);
+            }
+            if (lane == 0) {
+                s->group[0] = s->group[1] = 0;
+                s->total = tiles;
+            }
+        }
     }
     fence_before();
     if constexpr (PAIR) {
@@ -598,6 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t deep = a.deep, stages = a.stages;
     const uint32_t at_once_to = a.wide ? a.whole : 0; /* blocks that a stage's loads can bring at once */
     bool ok = true;
+    if (a.early_w && warp != kLoader) launch_wait(a);
 
     if (warp == kLoader) {
         if (elect_one()) {
@@ -605,6 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             uint32_t issued = 0;
             int32_t group = 0;
             asm volatile("fence.proxy.async.global;" ::: "memory");
+            bool waited = !a.early_w;
             for (int32_t t = begin; t < total; t += stride) {
                 const Tile o = tile_at(a, s, t, &group, features);
                 /* rows of x for this CTA: of a pair, each holds half of the columns in use */
@@ -620,39 +674,48 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 const CUtensorMap *const xmap = a.xmap + box, *const xtail = a.xtail + box;
                 const uint32_t x_one = a.x_box[box] * kRowBytes;
                 const uint32_t w_loaded = deep * w_bytes, all = w_loaded + deep * x_one;
+                /* Stages of the first tile get their w before the launch's wait, as many as there are,
+                 * and then their x. */
+                uint32_t ahead = 0;
+                if (!waited) {
+                    const uint32_t all_stages = (k1 - k0 + deep - 1) / deep;
+                    ahead = all_stages < stages ? all_stages : stages;
+                    for (uint32_t i = 0; i < ahead; ++i) {
+                        const uint32_t k = k0 + i * deep, bar = full + 8 * i;
+                        const uint32_t blocks = min(deep, k1 - k);
+                        const bool at_once = k + blocks <= at_once_to;
+                        mbar_expect_tx(bar, at_once ? all : blocks * (w_bytes + x_one));
+                        load_w<PAIR, GATED>(a, at_once, ring + i * stage, blocks, k, f, o.group, bar);
+                    }
+                    waited = true;
+                    launch_wait(a);
+                    asm volatile("fence.proxy.async.global;" ::: "memory");
+                }
                 for (uint32_t k = k0; k < k1; k += deep) {
-                    ok = ok && mbar_wait(empty + 8 * at, phase, s);
-                    if (!ok) break;
                     const uint32_t blocks = min(deep, k1 - k);
-                    const uint32_t dst = ring + at * stage, dst_x = dst + w_loaded;
+                    const uint32_t dst = ring + at * stage;
                     /* all blocks of the stage at once, unless the one that lacks columns is among
                      * them */
                     const bool at_once = k + blocks <= at_once_to;
                     uint32_t bar = full + 8 * at;
-                    if (!PAIR || rank == 0) {
-                        const uint32_t bytes = at_once ? all : blocks * (w_bytes + x_one);
-                        mbar_expect_tx(bar, PAIR ? 2 * bytes : bytes);
-                    }
-                    if constexpr (PAIR) bar = map_to(bar, 0);
-                    if (at_once) {
-                        if constexpr (GATED)
-                            load5<PAIR>(dst, &a.wmap, 0, 0, 2 * o.group, f / 8, (int32_t)k, bar);
-                        else load4<PAIR>(dst, &a.wmap, 0, f, (int32_t)k, o.group, bar);
-                        load3<PAIR>(dst_x, xmap, 0, row, (int32_t)k, bar);
+                    if (ahead) {
+                        --ahead;
                     } else {
-                        for (uint32_t i = 0; i < blocks; ++i) {
-                            const int32_t c = (int32_t)((k + i) * kDepth);
-                            const uint32_t to = dst + i * w_bytes;
-                            if constexpr (GATED) {
-                                for (uint32_t q = 0; q < a.fr / 16; ++q)
-                                    load4<PAIR>(to + q * 16 * kRowBytes, &a.wtail, c,
-                                                f + (int32_t)(8 * q), 0, o.group, bar);
-                            } else {
-                                load3<PAIR>(to, &a.wtail, c, f, o.group, bar);
-                            }
-                            load3<PAIR>(dst_x + i * x_one, xtail, c, row, 0, bar);
+                        ok = ok && mbar_wait(empty + 8 * at, phase, s);
+                        if (!ok) break;
+                        if (!PAIR || rank == 0) {
+                            const uint32_t bytes = at_once ? all : blocks * (w_bytes + x_one);
+                            mbar_expect_tx(bar, PAIR ? 2 * bytes : bytes);
                         }
+                        if constexpr (PAIR) bar = map_to(bar, 0);
+                        load_w<PAIR, GATED>(a, at_once, dst, blocks, k, f, o.group, bar);
                     }
+                    if (at_once)
+                        load3<PAIR>(dst + w_loaded, xmap, 0, row, (int32_t)k, bar);
+                    else
+                        for (uint32_t i = 0; i < blocks; ++i)
+                            load3<PAIR>(dst + w_loaded + i * x_one, xtail,
+                                        (int32_t)((k + i) * kDepth), row, 0, bar);
                     ++issued;
                     if (++at == stages) {
                         at = 0;
@@ -664,6 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     cluster_done();
                 }
             }
+            if (!waited) launch_wait(a);
             if (*(volatile int *)&s->dead) drain(a, s, issued, PAIR && rank);
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
@@ -755,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             float bias = 0.0f; /* of the lane's weight row */
             if (m.bias && col < a.outs) {
                 const int64_t at = col + (GATED && (lane & 8) ? a.outs : 0);
-                bias = m.bias_f32 ? static_cast<const float *>(m.bias)[at]
+                bias = m.bias_f32 ? value(static_cast<const float *>(m.bias), at)
                                   : value(m.bias, at, m.f16);
             }
             if (!dry) {
@@ -944,60 +1008,72 @@ struct Cut {
     uint32_t bn, fr, split; /* split: log2 */
 };
 
-/* Microseconds that one block of kDepth columns takes a CTA (a pair): the four products and what
- * their issue costs, measured with the loads left out. */
-double block_us(bool pair, uint32_t bn, uint32_t fr)
+/* Bytes of one stage's blocks that may be taken together, and how many blocks that makes. */
+uint32_t deep_of(bool pair, uint32_t bn, uint32_t fr)
 {
-    if (pair) return bn <= 128 ? 0.16 : 0.16 + (bn - 128) * (0.29 - 0.16) / 128;
-    if (bn <= 64) return fr <= 64 ? 0.1 : 0.11;
-    return bn <= 128 ? 0.21 : 0.21 + (bn - 128) * (0.29 - 0.21) / 128;
+    const uint32_t block = (fr + (pair ? bn / 2 : bn)) * kRowBytes;
+    uint32_t deep = 4;
+    while (deep > 1 && block * deep > (pair ? kDeepBytes / 2 : kDeepBytes)) deep /= 2;
+    return deep;
 }
 
-/* The cut with the least estimated time.  A launch takes its latency, and the longest of
- *   - the products of the CTA with the most tiles,
- *   - that CTA's loads, at what one SM can take in,
- *   - the bytes of all from memory: the weight once, x once.
- * Groups are taken as equally full, their number of rows being all that the host knows. */
+/* Estimated microseconds of a product.  The CTA with the most tiles goes through its blocks at the
+ * pace of their products and of their issue, or of what one SM can take in; a tile's epilogue runs
+ * under the next tile's products, but for the last; and all CTAs together are held by L2 and memory.
+ * The constants are a fit to 13,800 timings: 182 sizes (1 to 4096 tokens, 256 to 28,672 rows, 1024 to
+ * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.7 % longer than
+ * the best of those on average, 42 % at the worst. */
+double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int64_t rows, const Cut &c)
+{
+    const double kSplit[3] = {0.0, 3.4, 3.8}; /* one, two and four CTAs per tile */
+    const uint32_t features = (c.pair ? 2 : 1) * (m->gated ? c.fr / 2 : c.fr);
+    const int64_t n_tiles = (rows + c.bn - 1) / c.bn;
+    const double tiles = (double)(n_tiles * m->busy * ((outs + features - 1) / features));
+    /* clusters of four leave some SMs out */
+    const int64_t slots = c.pair || c.split == 1 ? sms / 2 : c.split == 2 ? sms * 9 / 38 : sms;
+    const double turns = (double)(((int64_t)tiles + slots - 1) / slots);
+    const double blocks = (double)((steps + (1u << c.split) - 1) >> c.split);
+    const double used = n_tiles == 1 ? (double)((rows + 15) / 16 * 16) : (double)c.bn;
+    const double bytes = (double)(c.fr + (c.pair ? c.bn / 2 : c.bn)) * kRowBytes;
+    const double mma = used * (c.pair ? 0.00081 : 0.00085);
+    double step = (mma > 0.159 ? mma : 0.159) + 0.088 / deep_of(c.pair, c.bn, c.fr);
+    if (step < bytes / 133e3) step = bytes / 133e3;
+    const double tokens = (double)(rows < c.bn ? rows : c.bn);
+    const double epilogue = 0.026 * tokens / (1u << c.split), products = blocks * step;
+    const double chain = turns * ((products > epilogue ? products : epilogue) + 0.55) + epilogue;
+    const double l2 = tiles * steps * (c.pair ? 2 : 1) * bytes / 17.1e6;
+    const double mem = 2.0 * m->cols * ((double)m->w_rows * m->busy + (double)m->likely) / 6.6e6;
+    const double shared = (l2 > mem ? l2 : mem) + 1.2;
+    return 2.8 + kSplit[c.split] + (chain > shared ? chain : shared);
+}
+
+/* The cut with the least estimate.  Groups are taken as equally full, their number of rows being all
+ * that the host knows. */
 Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
 {
-    const double kLaunch = 4.0, kSplit[3] = {0.0, 1.5, 2.0}; /* us: alone; 2, 4 CTAs per tile */
-    const double kSmBytes = 90e3, kBytes = 6.4e6;            /* per us: an SM, the memory */
-    const int64_t busy = m->busy, rows = (m->tokens + busy - 1) / busy;
-    const double once = 2.0 * m->cols * ((double)m->w_rows * busy + (double)m->tokens) / kBytes;
+    const int64_t busy = m->busy, rows = (m->likely + busy - 1) / busy;
     Cut best = {};
     double least = 1e30;
     for (int pair = 0; pair < 2; ++pair) {
         const uint32_t unit = pair ? 32 : 16;
         uint32_t last = 0;
-        for (int64_t parts = 1; parts <= 64; ++parts) {
+        for (int64_t parts = (rows + 255) / 256; parts < (rows + 255) / 256 + 64; ++parts) {
             const int64_t even = (rows + parts - 1) / parts;
             /* uneven groups: room for half as much again where that saves a second tile */
             const int64_t room = busy > 1 && parts == 1 ? even + even / 2 : even;
             uint32_t bn = (uint32_t)((room + unit - 1) / unit * unit);
-            if (even > 256) continue;
             if (bn > 256) bn = 256;
-            if (pair && bn < 128) break;
+            if (pair && bn < 96) break;
             if (bn == last) continue;
             last = bn;
-            const int64_t n_tiles = (rows + bn - 1) / bn * busy;
-            for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += m->gated ? 16 : 8) {
-                const uint32_t features = (pair ? 2 : 1) * (m->gated ? fr / 2 : fr);
-                const int64_t tiles = n_tiles * ((outs + features - 1) / features);
-                for (uint32_t log = 0; log < 3; ++log) {
-                    const uint32_t split = 1u << log, share = pair ? 2 : split;
-                    if (log && (pair || bn > 64 || steps < 4 * split)) break;
-                    /* clusters of four leave some SMs out */
-                    const int64_t slots = log == 2 ? sms * 9 / 38 : sms / share;
-                    const double turns = (double)((tiles + slots - 1) / slots);
-                    const double blocks = turns * ((steps + split - 1) / split);
-                    const double in = (double)(fr + (pair ? bn / 2 : bn)) * kRowBytes / kSmBytes;
-                    const double step = block_us(pair, bn, fr);
-                    double us = blocks * (in > step ? in : step);
-                    if (us < once) us = once;
-                    us += kLaunch + kSplit[log];
+            for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += 16) {
+                for (uint32_t split = 0; split < 3; ++split) {
+                    if (split && (pair || bn > 128 || steps < 4u << split)) break;
+                    const Cut c = {pair != 0, bn, fr, split};
+                    const double us = estimate(m, outs, steps, sms, rows, c);
                     if (us < least * 0.995) {
                         least = us;
-                        best = {pair != 0, bn, fr, log};
+                        best = c;
                     }
                 }
             }
@@ -1011,18 +1087,18 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
 Cut cut_of(const cfa_matmul *m, int sms)
 {
     struct Known {
-        int64_t tokens, w_rows, cols;
+        int64_t likely, w_rows, cols;
         int32_t busy, gated, sms;
         Cut cut;
     };
     static thread_local Known known[64] = {};
-    const uint64_t key = ((uint64_t)m->tokens * 0x9E3779B97F4A7C15ull) ^
+    const uint64_t key = ((uint64_t)m->likely * 0x9E3779B97F4A7C15ull) ^
                          ((uint64_t)m->w_rows * 0xC2B2AE3D27D4EB4Full) ^
                          ((uint64_t)m->cols * 0x165667B19E3779F9ull) ^ (uint64_t)m->busy;
     Known &k = known[(key >> 40) & 63u];
-    if (k.tokens != m->tokens || k.w_rows != m->w_rows || k.cols != m->cols || k.busy != m->busy ||
+    if (k.likely != m->likely || k.w_rows != m->w_rows || k.cols != m->cols || k.busy != m->busy ||
         k.gated != m->gated || k.sms != sms)
-        k = {m->tokens, m->w_rows, m->cols, m->busy, m->gated, sms,
+        k = {m->likely, m->w_rows, m->cols, m->busy, m->gated, sms,
              choose(m, m->gated ? m->w_rows / 2 : m->w_rows,
                     (uint32_t)((m->cols + kDepth - 1) / kDepth), sms)};
     return k.cut;
@@ -1038,6 +1114,7 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     a.outs = gated ? m->w_rows / 2 : m->w_rows;
     a.steps = (uint32_t)((m->cols + kDepth - 1) / kDepth);
     a.release = (uint32_t)release;
+    a.early_w = m->w_ready && !pair;
     a.bn = cut.bn;
     a.fr = cut.fr;
     a.split = cut.split;
@@ -1051,10 +1128,9 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const uint32_t x_rows = pair ? a.bn / 2 : a.bn;
     a.x_box[0] = x_rows;
     if (m->offs) /* ragged groups: half as high, a quarter, an eighth */
-        for (uint32_t i = 1; i < kBoxes; ++i) a.x_box[i] = (x_rows >> i) / 8 * 8;
+        for (uint32_t i = 1; i < kBoxes && x_rows >> i >= 16; ++i) a.x_box[i] = (x_rows >> i) / 8 * 8;
     const uint32_t block = (a.fr + x_rows) * kRowBytes;
-    for (a.deep = 4; a.deep > 1 && block * a.deep > kDeepBytes; a.deep /= 2) {
-    }
+    a.deep = deep_of(pair, a.bn, a.fr);
     const uint32_t stage = block * a.deep;
     a.wide = !gated || a.outs % 8 == 0;
     a.whole = (uint32_t)(m->cols / kDepth);

@@ -183,6 +183,7 @@ extern "C" cfa_status cfa_linear_async(const cfa_linear_args *a, cfa_stream stre
     m.r_stride = a->residual_stride;
     m.y_stride = a->y_stride;
     m.n_groups = m.busy = 1;
+    m.likely = a->tokens;
     m.f16 = a->dtype == CFA_DTYPE_F16;
     m.bias_f32 = a->bias && a->bias_dtype == CFA_DTYPE_F32;
     m.y_f32 = a->y_dtype == CFA_DTYPE_F32;
@@ -235,6 +236,8 @@ extern "C" cfa_status cfa_route_async(const cfa_route_args *a, cfa_stream stream
 /* ---- experts ---- */
 
 namespace {
+
+constexpr int64_t kCounted = 1024; /* choices that the first product's CTAs count for themselves */
 
 struct ExpertsPlan {
     int64_t pairs;
@@ -357,6 +360,9 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     m.tokens = p.pairs;
     m.n_groups = a->experts;
     m.busy = (int32_t)(p.pairs < a->experts ? p.pairs : a->experts);
+    /* experts before the first are other ranks': their share of the pairs is not here */
+    m.likely = p.pairs * a->experts / ((int64_t)a->first_expert + a->experts);
+    if (m.likely < m.busy) m.likely = m.busy;
     m.f16 = a->dtype == CFA_DTYPE_F16;
     m.x = ws + p.xs;
     m.x_stride = a->hidden;
@@ -367,7 +373,19 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     m.y_stride = a->inter;
     m.act = a->activation;
     m.gated = gated;
+    /* The sort's launch lets this one start once all before the call has ended, and this one the
+     * next once the sort has: their weights are there before what they multiply them with. */
+    m.w_ready = 1;
+    if (p.pairs <= kCounted) {
+        m.ids = a->ids;
+        m.n_ids = (int32_t)p.pairs;
+        m.first = a->first_expert;
+    } else {
+        m.w_ready = 0;
+    }
     if (!e) e = cfa_launch_matmul(&m, 1, 1, stream);
+    m.ids = nullptr;
+    m.w_ready = 1;
     m.x = m.y;
     m.x_stride = a->inter;
     m.w = a->w2;

@@ -24,6 +24,11 @@ typedef struct cfa_matmul {
     const void *x, *w, *bias, *residual;
     void *y;
     const int32_t *offs;
+    /* ids: the choices from which offs was counted, if the kernel is to count for itself: then it needs
+     * offs only as a mark.  w_ready: w and the choices (without ids: offs) are in memory when the
+     * launch starts, although the launch before it may not have ended */
+    const int32_t *ids;
+    int32_t n_ids, first, w_ready;
     int64_t tokens, w_rows, cols;
     int64_t x_stride, w_stride, r_stride, y_stride; /* elements */
     int32_t n_groups;
@@ -31,6 +36,7 @@ typedef struct cfa_matmul {
     int32_t bias_f32, y_f32;
     int32_t act, gated;
     int32_t busy;     /* groups that can hold rows at all (host's bound) */
+    int64_t likely;   /* rows to expect in all groups, at most `tokens` */
 } cfa_matmul;
 
 /* The pairs (token, choice) sorted by expert. */

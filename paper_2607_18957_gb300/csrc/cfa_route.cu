@@ -36,13 +36,13 @@ __device__ __forceinline__ float from_bits(uint32_t b, int32_t dtype) /* of a 2-
     return __bfloat162float(__ushort_as_bfloat16((unsigned short)b));
 }
 
-/* The lane's R logits, -inf behind the last.  (All loads go past L1: see cfa_matmul.cu.) */
+/* The lane's R of n values, -inf behind the last.  (All loads go past L1: see cfa_matmul.cu.) */
 template <int R>
-__device__ __forceinline__ void load(const cfa_route_args &a, const uint8_t *row, int first, bool vec,
+__device__ __forceinline__ void load(int32_t dtype, int n, const void *row, int first, bool vec,
                                      float (&v)[R])
 {
-    if (a.dtype == CFA_DTYPE_F32) {
-        const float *p = reinterpret_cast<const float *>(row) + first;
+    if (dtype == CFA_DTYPE_F32) {
+        const float *p = static_cast<const float *>(row) + first;
         if (R % 4 == 0 && vec) {
 #pragma unroll
             for (int r = 0; r + 3 < R; r += 4) {
@@ -54,23 +54,23 @@ __device__ __forceinline__ void load(const cfa_route_args &a, const uint8_t *row
             }
         } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r) v[r] = first + r < a.experts ? __ldcg(p + r) : -INFINITY;
+            for (int r = 0; r < R; ++r) v[r] = first + r < n ? __ldcg(p + r) : -INFINITY;
         }
     } else {
-        const unsigned short *p = reinterpret_cast<const unsigned short *>(row) + first;
+        const unsigned short *p = static_cast<const unsigned short *>(row) + first;
         if (R % 4 == 0 && vec) {
 #pragma unroll
             for (int r = 0; r + 3 < R; r += 4) {
                 const uint2 q = __ldcg(reinterpret_cast<const uint2 *>(p + r));
-                v[r] = from_bits(q.x & 0xFFFFu, a.dtype);
-                v[r + 1] = from_bits(q.x >> 16, a.dtype);
-                v[r + 2] = from_bits(q.y & 0xFFFFu, a.dtype);
-                v[r + 3] = from_bits(q.y >> 16, a.dtype);
+                v[r] = from_bits(q.x & 0xFFFFu, dtype);
+                v[r + 1] = from_bits(q.x >> 16, dtype);
+                v[r + 2] = from_bits(q.y & 0xFFFFu, dtype);
+                v[r + 3] = from_bits(q.y >> 16, dtype);
             }
         } else {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                v[r] = first + r < a.experts ? from_bits(__ldcg(p + r), a.dtype) : -INFINITY;
+                v[r] = first + r < n ? from_bits(__ldcg(p + r), dtype) : -INFINITY;
         }
     }
 }
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
     const uint8_t *row = static_cast<const uint8_t *>(a.logits) + t * a.logits_stride * es;
     const bool vec = a.experts == 32 * R && ((uintptr_t)row & (uintptr_t)(4 * es - 1)) == 0;
     float v[R], key[R];
-    load<R>(a, row, lane * R, vec, v);
+    load<R>(a.dtype, a.experts, row, lane * R, vec, v);
     float top = -INFINITY;
     bool nan = false;
 #pragma unroll
@@ -179,14 +179,20 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
             norm = nan ? NAN : warp_add(sum);
         }
     }
+    if (a.bias) {
+        float b[R];
+        load<R>(CFA_DTYPE_F32, a.experts, a.bias, lane * R,
+                a.experts == 32 * R && ((uintptr_t)a.bias & 15u) == 0, b);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int e = lane * R + r;
-        float k = softmax ? v[r] : 1.0f / (1.0f + expf(-v[r]));
-        if (a.bias && e < a.experts)
-            k = (softmax ? expf(v[r] - top) / norm : k) + __ldcg(a.bias + e);
-        key[r] = v[r] > -INFINITY ? k : -INFINITY;
+        for (int r = 0; r < R; ++r)
+            key[r] = (softmax ? expf(v[r] - top) / norm : 1.0f / (1.0f + expf(-v[r]))) + b[r];
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = softmax ? v[r] : 1.0f / (1.0f + expf(-v[r]));
     }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (!(v[r] > -INFINITY)) key[r] = -INFINITY;
     if (a.groups > 1) keep_groups<R>(a, key, s_key + warp * a.experts, lane, !softmax);
 
     uint32_t k[R], best = 0; /* the lane's best key, its place and its logit */

@@ -18,6 +18,7 @@ constexpr int64_t kOnePass = 16384;   /* pairs that every block of the sort coun
 constexpr int64_t kBlockPairs = 1024; /* pairs per count, at least, where there are more */
 constexpr int64_t kMostBlocks = 128;
 
+/* All loads of what other kernels write go past L1, which may hold what an older one read there. */
 __device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release()
 {
@@ -32,7 +33,7 @@ __host__ __device__ inline int64_t block_pairs(int64_t pairs)
 
 __device__ __forceinline__ int expert_of(const cfa_sort &s, int64_t p)
 {
-    const int64_t e = (int64_t)s.ids[p] - s.first;
+    const int64_t e = (int64_t)__ldcg(s.ids + p) - s.first;
     return e >= 0 && e < s.experts ? (int)e : -1;
 }
 
@@ -68,7 +69,16 @@ struct PlaceArgs {
 /* Adds pairs [p0, p1) to n, expert by expert. */
 __device__ __forceinline__ void count(const cfa_sort &s, int64_t p0, int64_t p1, int32_t *n)
 {
-    for (int64_t p = p0 + threadIdx.x; p < p1; p += kThreads) {
+    int64_t p = p0 + threadIdx.x;
+    for (; p + 7 * kThreads < p1; p += 8 * kThreads) { /* eight loads under way at once */
+        int e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = expert_of(s, p + i * kThreads);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e[i] >= 0) atomicAdd(n + e[i], 1);
+    }
+    for (; p < p1; p += kThreads) {
         const int e = expert_of(s, p);
         if (e >= 0) atomicAdd(n + e, 1);
     }
@@ -100,7 +110,7 @@ __global__ void __launch_bounds__(kThreads) cfa_place_kernel(const PlaceArgs a)
             int32_t lower = 0, upper = 0;
 #pragma unroll 8
             for (int b = 0; b < a.blocks; ++b) {
-                const int32_t n = s.hist[(int64_t)b * s.experts + e];
+                const int32_t n = __ldcg(s.hist + (int64_t)b * s.experts + e);
                 if (b < mine) lower += n;
                 else upper += n;
             }
@@ -171,88 +181,105 @@ __global__ void __launch_bounds__(kThreads) cfa_place_kernel(const PlaceArgs a)
             const int64_t n = a.hidden / 8;
             int64_t h = lane;
             for (; h + 96 < n; h += 128) {
-                const uint4 v0 = f[h], v1 = f[h + 32], v2 = f[h + 64], v3 = f[h + 96];
+                const uint4 v0 = __ldcg(f + h), v1 = __ldcg(f + h + 32), v2 = __ldcg(f + h + 64),
+                            v3 = __ldcg(f + h + 96);
                 o[h] = v0;
                 o[h + 32] = v1;
                 o[h + 64] = v2;
                 o[h + 96] = v3;
             }
-            for (; h < n; h += 32) o[h] = f[h];
+            for (; h < n; h += 32) o[h] = __ldcg(f + h);
         } else {
-            for (int64_t h = lane; h < a.hidden; h += 32) to[h] = from[h];
+            for (int64_t h = lane; h < a.hidden; h += 32) to[h] = __ldcg(from + h);
         }
     }
 }
 
-__device__ __forceinline__ float half_at(const void *p, int64_t i, int f16)
+__device__ __forceinline__ float half_of(unsigned short b, int f16)
 {
-    return f16 ? __half2float(static_cast<const __half *>(p)[i])
-               : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    return f16 ? __half2float(__ushort_as_half(b)) : __bfloat162float(__ushort_as_bfloat16(b));
 }
 
-/* Sum over the choices of a token, in their order and in fp32: N columns from h on. */
-template <int N>
-__device__ __forceinline__ void add_choices(const cfa_combine &c, int64_t t, int64_t h, float *sum)
-{
-#pragma unroll 4
-    for (int j = 0; j < c.top_k; ++j) {
-        const int64_t row = c.place[t * c.top_k + j];
-        if (row < 0) continue;
-        const float w = c.weights[t * c.top_k + j];
-        const float *from = c.part + row * c.hidden + h;
-        if constexpr (N == 8) {
-            const float4 a = *reinterpret_cast<const float4 *>(from);
-            const float4 b = *reinterpret_cast<const float4 *>(from + 4);
-            sum[0] += w * a.x;
-            sum[1] += w * a.y;
-            sum[2] += w * a.z;
-            sum[3] += w * a.w;
-            sum[4] += w * b.x;
-            sum[5] += w * b.y;
-            sum[6] += w * b.z;
-            sum[7] += w * b.w;
-        } else {
-            sum[0] += w * *from;
-        }
-    }
-}
-
-/* A thread takes eight columns of one token, or one where y or the residual is off the 16-byte grid. */
+/* A thread takes eight columns of one token, or one where y or the residual is off the 16-byte grid,
+ * and adds the token's choices in their order, in fp32.  Where their rows lie, their weights and the
+ * residual are read before the launch's wait: all that is there since the launch before last. */
+constexpr int kAhead = 8; /* choices read ahead */
 template <int N>
 __global__ void __launch_bounds__(kThreads) cfa_combine_kernel(const cfa_combine c)
 {
-    wait_before();
     const int64_t per = c.hidden / N, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= c.tokens * per) return;
-    const int64_t t = i / per, h = (i - t * per) * N;
-    float sum[N] = {};
-    add_choices<N>(c, t, h, sum);
+    const bool in = i < c.tokens * per;
+    const int64_t t = in ? i / per : 0, h = in ? (i - t * per) * N : 0;
     const int64_t at = t * c.y_stride + h, from = t * c.r_stride + h;
-    if constexpr (N == 8) {
-        if (c.residual) {
-            const uint4 r = *reinterpret_cast<const uint4 *>(
-                static_cast<const uint16_t *>(c.residual) + from);
+    const int32_t *place = c.place + t * c.top_k;
+    const float *weights = c.weights + t * c.top_k;
+    int32_t row[kAhead];
+    float w[kAhead], sum[N] = {}, r[N] = {};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += half_at(&r, k, c.f16);
+    for (int j = 0; j < kAhead; ++j) {
+        row[j] = in && j < c.top_k ? __ldcg(place + j) : -1;
+        w[j] = row[j] >= 0 ? __ldcg(weights + j) : 0.0f;
+    }
+    if (in && c.residual) {
+        if constexpr (N == 8) {
+            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(
+                static_cast<const uint16_t *>(c.residual) + from));
+            const unsigned short *b = reinterpret_cast<const unsigned short *>(&v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = half_of(b[k], c.f16);
+        } else {
+            r[0] = half_of(__ldcg(static_cast<const unsigned short *>(c.residual) + from), c.f16);
         }
-        uint32_t w[4];
+    }
+    wait_before();
+    if (!in) return;
+    const float *part = c.part + h;
+    if constexpr (N == 8) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (row[j] < 0) continue;
+            const float4 *p = reinterpret_cast<const float4 *>(part + row[j] * c.hidden);
+            const float4 a = __ldcg(p), b = __ldcg(p + 1);
+            sum[0] += w[j] * a.x;
+            sum[1] += w[j] * a.y;
+            sum[2] += w[j] * a.z;
+            sum[3] += w[j] * a.w;
+            sum[4] += w[j] * b.x;
+            sum[5] += w[j] * b.y;
+            sum[6] += w[j] * b.z;
+            sum[7] += w[j] * b.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (row[j] >= 0) sum[0] += w[j] * __ldcg(part + row[j] * c.hidden);
+    }
+    for (int j = kAhead; j < c.top_k; ++j) {
+        const int64_t more = __ldcg(place + j);
+        if (more < 0) continue;
+        const float v = __ldcg(weights + j);
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] += v * __ldcg(part + more * c.hidden + k);
+    }
+    if constexpr (N == 8) {
+        uint32_t o[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+            const float x = sum[2 * k] + r[2 * k], y = sum[2 * k + 1] + r[2 * k + 1];
             if (c.f16) {
-                const __half2 v = __floats2half2_rn(sum[2 * k], sum[2 * k + 1]);
-                w[k] = *reinterpret_cast<const uint32_t *>(&v);
+                const __half2 v = __floats2half2_rn(x, y);
+                o[k] = *reinterpret_cast<const uint32_t *>(&v);
             } else {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(sum[2 * k], sum[2 * k + 1]);
-                w[k] = *reinterpret_cast<const uint32_t *>(&v);
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+                o[k] = *reinterpret_cast<const uint32_t *>(&v);
             }
         }
         *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(c.y) + at) =
-            make_uint4(w[0], w[1], w[2], w[3]);
+            make_uint4(o[0], o[1], o[2], o[3]);
+    } else if (c.f16) {
+        static_cast<__half *>(c.y)[at] = __float2half_rn(sum[0] + r[0]);
     } else {
-        float v = sum[0];
-        if (c.residual) v += half_at(c.residual, from, c.f16);
-        if (c.f16) static_cast<__half *>(c.y)[at] = __float2half_rn(v);
-        else static_cast<__nv_bfloat16 *>(c.y)[at] = __float2bfloat16_rn(v);
+        static_cast<__nv_bfloat16 *>(c.y)[at] = __float2bfloat16_rn(sum[0] + r[0]);
     }
 }
 
@@ -268,7 +295,8 @@ __global__ void __launch_bounds__(kThreads) cfa_realign_kernel(const RealignArgs
     release();
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x)
         for (int64_t i = threadIdx.x; i < a.to_stride; i += kThreads)
-            a.to[r * a.to_stride + i] = i < a.cols ? a.from[r * a.from_stride + i] : (uint16_t)0;
+            a.to[r * a.to_stride + i] =
+                i < a.cols ? __ldcg(a.from + r * a.from_stride + i) : (uint16_t)0;
 }
 
 template <typename Args>
@@ -303,8 +331,8 @@ cudaError_t cfa_launch_sort(const cfa_sort *s, const void *x, int64_t x_stride, 
 {
     const size_t smem = sizeof(int32_t) * s->experts;
     PlaceArgs a = {*s, x, xs, x_stride, hidden, 0, (int32_t)cfa_sort_blocks(s->pairs), 0};
-    /* chunks of a power of two, so that they do not straddle blocks: about two per SM */
-    for (a.chunk = 1; a.chunk < kThreads && s->pairs > (int64_t)a.chunk * 512; a.chunk *= 2) {
+    /* chunks of a power of two, so that they do not straddle blocks: about one per SM */
+    for (a.chunk = 1; a.chunk < kThreads && s->pairs > (int64_t)a.chunk * 160; a.chunk *= 2) {
     }
     a.vec = (((uintptr_t)x | (uintptr_t)xs | (uint64_t)x_stride * 2 | (uint64_t)hidden * 2) & 15u) ==
             0;
