@@ -19,6 +19,11 @@
  * Gated: the stage holds 8 gate rows, then the 8 up rows that belong to them, and so on, so both
  * values of an output lie in one warp, 8 lanes apart.
  *
+ * exact: the tensor cores add in fp32, but cut each sum's last bits off where IEEE addition rounds, so
+ * that an fp32 result is off by half a unit in the last place per addition in the same direction
+ * (1e-6 after 64 of them: 1024 columns).  For fp32 results the accumulator therefore takes parts of
+ * 256 columns, which the epilogue adds with rounding in a third place of tensor memory.
+ *
  * Every wait has a limit.  One that runs out sets the status word that cfa_op_status reads; its CTA
  * then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
  * memory.
@@ -44,6 +49,7 @@ constexpr uint32_t kRowBytes = kDepth * 2;
 constexpr uint32_t kMaxStages = 32;      /* no more than a warp has lanes */
 constexpr uint32_t kSmem = 232448;       /* all that a CTA may have: one CTA per SM, so that the
                                             tensor memory is never asked for twice at once */
+constexpr uint32_t kPart = 4;            /* blocks per part of a sum that is kept exact (m.exact) */
 constexpr uint32_t kBand = 16;           /* token tiles that share a weight tile in turn */
 constexpr uint32_t kBoxes = 4;           /* heights of the loads of x */
 constexpr uint32_t kSpinLimit = 1u << 20;    /* polls of a wait */
@@ -63,6 +69,7 @@ struct Args {
     uint32_t wide;       /* a gated w has groups of 8 rows, or w is not gated */
     uint32_t whole;      /* whole blocks; the last of steps may lack columns */
     uint32_t steps;      /* blocks in all */
+    uint32_t acc_on;     /* columns of tensor memory from one accumulator to the next */
     uint32_t f_tiles;    /* feature tiles per group */
     int32_t total;       /* output tiles, of one group */
     uint32_t split;      /* log2 of the CTAs per output tile along the columns */
@@ -293,6 +300,19 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_store(uint32_t addr, const float (&v)[16])
+{
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n\t"
+                 "tcgen05.wait::st.sync.aligned;" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+                 : "memory");
+}
+
 /* Loads go past L1, which may hold what an older kernel read there: a launch can start before the one
  * before it has ended (cfa_launch_ctl), so that its start clears nothing written after it. */
 __device__ __forceinline__ float value(const void *p, int64_t i, int f16)
@@ -326,6 +346,18 @@ template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act
         for (int i = 0; i < N; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
         break;
     default: break;
+    }
+}
+
+/* 16 columns of the accumulator, and with `more` the sums of the parts before. */
+__device__ __forceinline__ void sum_load(uint32_t acc, uint32_t sum, bool more, float (&v)[16])
+{
+    tmem_load(acc, v);
+    if (more) {
+        float u[16];
+        tmem_load(sum, u);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] += u[j];
     }
 }
 
@@ -535,7 +567,7 @@ __device__ __forceinline__ void launch_wait(const Args &a)
     if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-template <bool PAIR, bool GATED>
+template <bool PAIR, bool GATED, bool EXACT>
 __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_constant__ Args a)
 {
     extern __shared__ uint8_t raw[];
@@ -647,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t k0 = PAIR ? 0 : rank * a.steps >> share;
     const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps >> share;
     const bool sync_tiles = !PAIR && share > 0;
-    const uint32_t deep = a.deep, stages = a.stages;
+    const uint32_t deep = a.deep, stages = a.stages, part = EXACT ? kPart : a.steps;
     const uint32_t at_once_to = a.wide ? a.whole : 0; /* blocks that a stage's loads can bring at once */
     bool ok = true;
     if (a.early_w && warp != kLoader) launch_wait(a);
@@ -750,7 +782,6 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     const uint32_t unit = PAIR ? 32u : 16u;
                     const uint32_t inst = instruction(m.f16, PAIR ? 256u : 128u,
                                                       ((uint32_t)o.rows + unit - 1) / unit * unit);
-                    const uint32_t d = tmem + buf * (a.tmem_cols / 2);
                     const uint32_t in_use = PAIR ? ((uint32_t)o.rows + 31u) / 32u * 16u
                                                  : (uint32_t)o.rows;
                     uint32_t box = 0;
@@ -759,35 +790,39 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     /* each stage's barrier is looked at before the products of the one before are
                      * issued, so that the look costs no time of its own */
                     bool there = mbar_try_wait(full + 8 * at, phase);
-                    ok = ok && mbar_wait(acc_empty + 8 * buf, buf_phase, s);
-                    fence_after();
-                    uint32_t add = 0; /* the first product of a tile overwrites */
-                    for (uint32_t k = k0; k < k1; k += deep) {
-                        ok = ok && (there || mbar_wait(full + 8 * at, phase, s));
-                        if (!ok) break;
+                    for (uint32_t k = k0; k < k1;) {
+                        const uint32_t d = tmem + buf * a.acc_on, stop = min(k1, k + part);
+                        ok = ok && mbar_wait(acc_empty + 8 * buf, buf_phase, s);
                         fence_after();
-                        uint32_t blocks = min(deep, k1 - k);
-                        uint32_t w = w_first + at * stage_on, x = x_first + at * stage_on;
-                                                const uint32_t done = empty + 8 * at;
-                        if (++at == stages) {
-                            at = 0;
-                            phase ^= 1;
-                        }
-                        there = k + deep < k1 && mbar_try_wait(full + 8 * at, phase);
-                        do {
-#pragma unroll
-                            for (uint32_t q = 0; q < kDepth / 16; ++q) { /* 32 bytes further */
-                                mma<PAIR>(d, w + q * 2, x + q * 2, inst, add);
-                                add = 1;
+                        uint32_t add = 0; /* the first product overwrites */
+                        for (; k < stop; k += deep) {
+                            ok = ok && (there || mbar_wait(full + 8 * at, phase, s));
+                            if (!ok) break;
+                            fence_after();
+                            uint32_t blocks = min(deep, k1 - k);
+                            uint32_t w = w_first + at * stage_on, x = x_first + at * stage_on;
+                            const uint32_t done = empty + 8 * at;
+                            if (++at == stages) {
+                                at = 0;
+                                phase ^= 1;
                             }
-                            w += w_on;
-                            x += x_on;
-                        } while (--blocks);
-                        commit<PAIR>(done);
+                            there = k + deep < k1 && mbar_try_wait(full + 8 * at, phase);
+                            do {
+#pragma unroll
+                                for (uint32_t q = 0; q < kDepth / 16; ++q) { /* 32 bytes further */
+                                    mma<PAIR>(d, w + q * 2, x + q * 2, inst, add);
+                                    add = 1;
+                                }
+                                w += w_on;
+                                x += x_on;
+                            } while (--blocks);
+                            commit<PAIR>(done);
+                        }
+                        if (!ok) break;
+                        commit<PAIR>(acc_full + 8 * buf);
+                        if (buf) buf_phase ^= 1;
+                        buf ^= 1;
                     }
-                    if (ok) commit<PAIR>(acc_full + 8 * buf);
-                    if (buf) buf_phase ^= 1;
-                    buf ^= 1;
                 }
                 if (sync_tiles) {
                     cluster_sync();
@@ -804,6 +839,20 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     } else {
         uint32_t buf = 0, buf_phase = 0;
         int32_t group = 0;
+        /* Gives an accumulator back once its sums have been read.  Relaxed: the stores of y need not
+         * have ended. */
+        const auto acc_release = [&](uint32_t &b, uint32_t &ph) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bar = acc_empty + 8 * b;
+                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                 PAIR ? map_to(bar, 0) : bar)
+                             : "memory");
+            }
+            if (b) ph ^= 1;
+            b ^= 1;
+        };
         const uint32_t lanes = s->tmem + ((uint32_t)warp * 32u << 16);
         float *partial = reinterpret_cast<float *>(
             raw + (ring - smem_addr(raw)) + a.stages * stage); /* [bn][128], split > 1 */
@@ -818,23 +867,42 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             if ((uint32_t)(warp * 32 + lane) >= a.fr) col = a.outs; /* a lane without a row */
             float bias = 0.0f; /* of the lane's weight row */
             if (m.bias && col < a.outs) {
-                const int64_t at = col + (GATED && (lane & 8) ? a.outs : 0);
+                const int64_t at = col + (GATED && (lane & 8) ? m.bias_up : 0);
                 bias = m.bias_f32 ? value(static_cast<const float *>(m.bias), at)
                                   : value(m.bias, at, m.f16);
             }
+            /* the parts before the last are added up in tensor memory */
+            bool more = false; /* a sum lies there */
             if (!dry) {
+                for (uint32_t k = k0 + part; EXACT && k < k1; k += part) {
+                    ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    fence_after();
+                    for (int32_t c = 0; ok && c < o.rows; c += 16) {
+                        float v[16], u[16];
+                        tmem_load(lanes + buf * a.acc_on + c, v);
+                        if (more) {
+                            tmem_load(lanes + 2 * a.acc_on + c, u);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] += u[j];
+                        }
+                        tmem_store(lanes + 2 * a.acc_on + c, v);
+                    }
+                    more = true;
+                    acc_release(buf, buf_phase);
+                }
                 ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 fence_after();
             }
-            const uint32_t src = lanes + buf * (a.tmem_cols / 2);
+            const uint32_t src = lanes + buf * a.acc_on, sum = lanes + 2 * a.acc_on;
             int32_t c0 = 0, c1 = o.rows;
             uint32_t sharers = 0;
             float v[16];
             if (sync_tiles) {
                 for (int32_t c = 0; ok && c < o.rows; c += 16) {
                     __syncwarp();
-                    tmem_load(src + c, v);
+                    sum_load(src + c, sum + c, EXACT && more, v);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         partial[(c + j) * kRows + warp * 32 + lane] = v[j];
@@ -852,7 +920,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             for (int32_t c = c0; ok && c < c1; c += 16) {
                 __syncwarp();
                 if (sharers == 0) {
-                    tmem_load(src + c, v);
+                    sum_load(src + c, sum + c, EXACT && more, v);
                 } else {
                     float p[4][16]; /* all on their way before the first is added */
 #pragma unroll
@@ -880,17 +948,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 dry = false;
                 continue;
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t bar = acc_empty + 8 * buf;
-                /* relaxed: the sums have been read, and the stores of y need not have ended */
-                asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                                 PAIR ? map_to(bar, 0) : bar)
-                             : "memory");
-            }
-            if (buf) buf_phase ^= 1;
-            buf ^= 1;
+            acc_release(buf, buf_phase);
             if (sync_tiles) cluster_done();
             t += stride;
         }
@@ -915,7 +973,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
 
 struct Device {
     std::atomic<int> sms;          /* 0: not asked yet */
-    std::atomic<int> clusters[2][9]; /* by gated and split: clusters that run at once, plus one */
+    std::atomic<int> clusters[8][3]; /* by kernel and split: clusters that run at once, plus one */
     std::atomic<unsigned> ready;   /* kernels whose shared memory is granted */
 };
 constexpr int kMaxDevices = 64;
@@ -953,13 +1011,16 @@ bool encode(CUtensorMap *map, int f16, const void *base, int rank, const cuuint6
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-const void *kernel_of(bool pair, bool gated)
+template <bool PAIR, bool GATED> const void *kernel_of(bool exact)
 {
-    if (pair)
-        return gated ? reinterpret_cast<const void *>(&cfa_matmul_kernel<true, true>)
-                     : reinterpret_cast<const void *>(&cfa_matmul_kernel<true, false>);
-    return gated ? reinterpret_cast<const void *>(&cfa_matmul_kernel<false, true>)
-                 : reinterpret_cast<const void *>(&cfa_matmul_kernel<false, false>);
+    return exact ? reinterpret_cast<const void *>(&cfa_matmul_kernel<PAIR, GATED, true>)
+                 : reinterpret_cast<const void *>(&cfa_matmul_kernel<PAIR, GATED, false>);
+}
+
+const void *kernel_of(bool pair, bool gated, bool exact)
+{
+    if (pair) return gated ? kernel_of<true, true>(exact) : kernel_of<true, false>(exact);
+    return gated ? kernel_of<false, true>(exact) : kernel_of<false, false>(exact);
 }
 
 struct Config {
@@ -986,15 +1047,15 @@ void configure(Config *c, unsigned grid, unsigned cluster, bool early, cudaStrea
     }
 }
 
-/* Clusters of `size` CTAs that the device runs at once. */
-cudaError_t clusters_of(Device &d, bool pair, bool gated, unsigned size, int *n)
+/* Clusters of 2^log CTAs that the device runs at once. */
+cudaError_t clusters_of(Device &d, const void *fn, unsigned kernel, unsigned log, int *n)
 {
-    std::atomic<int> &known = d.clusters[gated][pair ? 0 : size];
+    std::atomic<int> &known = d.clusters[kernel][log];
     int v = known.load();
     if (!v) {
         Config c;
-        configure(&c, size, size, false, nullptr);
-        const cudaError_t e = cudaOccupancyMaxActiveClusters(&v, kernel_of(pair, gated), &c.cfg);
+        configure(&c, 1u << log, 1u << log, false, nullptr);
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&v, fn, &c.cfg);
         if (e) return e;
         known.store(++v);
     }
@@ -1064,6 +1125,7 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
             uint32_t bn = (uint32_t)((room + unit - 1) / unit * unit);
             if (bn > 256) bn = 256;
             if (pair && bn < 96) break;
+            if (m->exact && bn > 128) continue; /* three of them in 512 columns */
             if (bn == last) continue;
             last = bn;
             for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += 16) {
@@ -1088,7 +1150,7 @@ Cut cut_of(const cfa_matmul *m, int sms)
 {
     struct Known {
         int64_t likely, w_rows, cols;
-        int32_t busy, gated, sms;
+        int32_t busy, gated, exact, sms;
         Cut cut;
     };
     static thread_local Known known[64] = {};
@@ -1097,8 +1159,8 @@ Cut cut_of(const cfa_matmul *m, int sms)
                          ((uint64_t)m->cols * 0x165667B19E3779F9ull) ^ (uint64_t)m->busy;
     Known &k = known[(key >> 40) & 63u];
     if (k.likely != m->likely || k.w_rows != m->w_rows || k.cols != m->cols || k.busy != m->busy ||
-        k.gated != m->gated || k.sms != sms)
-        k = {m->likely, m->w_rows, m->cols, m->busy, m->gated, sms,
+        k.gated != m->gated || k.exact != m->exact || k.sms != sms)
+        k = {m->likely, m->w_rows, m->cols, m->busy, m->gated, m->exact, sms,
              choose(m, m->gated ? m->w_rows / 2 : m->w_rows,
                     (uint32_t)((m->cols + kDepth - 1) / kDepth), sms)};
     return k.cut;
@@ -1141,20 +1203,21 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const uint32_t left = kSmem - shared_bytes(m->n_groups) - 1024u -
                           (partial > behind ? partial : behind);
     a.stages = left / stage < kMaxStages ? left / stage : kMaxStages;
-    for (a.tmem_cols = 32; a.tmem_cols < 2 * a.bn; a.tmem_cols *= 2) {
+    for (a.acc_on = 16; a.acc_on < a.bn; a.acc_on *= 2) {
     }
+    a.tmem_cols = m->exact ? 4 * a.acc_on : 2 * a.acc_on; /* a power of two */
 
-    const unsigned bit = 1u << ((pair ? 2 : 0) + (gated ? 1 : 0));
-    const void *fn = kernel_of(pair, gated);
-    if (!(d.ready.load() & bit)) {
+    const unsigned kernel = (pair ? 4u : 0u) + (gated ? 2u : 0u) + (m->exact ? 1u : 0u);
+    const void *fn = kernel_of(pair, gated, m->exact);
+    if (!(d.ready.load() & 1u << kernel)) {
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
         if (e) return e;
-        d.ready.fetch_or(bit);
+        d.ready.fetch_or(1u << kernel);
     }
-    const unsigned size = pair ? 2 : 1u << a.split;
+    const unsigned log = pair ? 1 : a.split, size = 1u << log;
     int clusters = sms;
-    if (size > 1) {
-        e = clusters_of(d, pair, gated, size, &clusters);
+    if (log) {
+        e = clusters_of(d, fn, kernel, log, &clusters);
         if (e) return e;
     }
     if (clusters > most) clusters = (int)most;

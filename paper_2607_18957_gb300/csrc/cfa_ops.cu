@@ -63,9 +63,15 @@ bool on_tma_grid(const void *p, int64_t rows, int64_t stride)
     return !off_grid(p, 16) && (rows <= 1 || stride % 8 == 0);
 }
 
+/* A weight off the grid is moved and multiplied in slices that stay in L2, through the same part of
+ * the workspace: moved as a whole it would be written to memory and read again. */
+constexpr uint64_t kSliceBytes = 72ull << 20;
+constexpr int64_t kSliceRows = 256; /* slices are multiples of this many columns of y */
+
 struct LinearPlan {
     bool move_x, move_w;
     int64_t row;          /* elements of a moved row */
+    int64_t slice;        /* columns of y per slice of a moved w (all of them if it stays) */
     uint64_t x_bytes, w_bytes;
 };
 
@@ -86,7 +92,15 @@ cfa_status linear_plan(const cfa_linear_args *a, LinearPlan *p)
     p->move_x = !on_tma_grid(a->x, a->tokens, a->x_stride);
     p->move_w = !on_tma_grid(a->w, a->rows, a->w_stride);
     p->x_bytes = p->move_x ? aligned((uint64_t)a->tokens * p->row * 2) : 0;
-    p->w_bytes = p->move_w ? aligned((uint64_t)a->rows * p->row * 2) : 0;
+    const int64_t halves = a->flags & CFA_LINEAR_GATED ? 2 : 1;
+    p->slice = (a->rows + halves - 1) / halves;
+    if (p->move_w) {
+        const int64_t fit = (int64_t)(kSliceBytes / ((uint64_t)p->row * 2 * halves)) / kSliceRows *
+                            kSliceRows;
+        if (p->slice > fit) p->slice = fit > kSliceRows ? fit : kSliceRows;
+        if (p->slice * halves > a->rows) p->slice = (a->rows + halves - 1) / halves;
+        p->w_bytes = aligned((uint64_t)(p->slice * halves) * p->row * 2);
+    }
     return CFA_OK;
 }
 
@@ -159,37 +173,49 @@ extern "C" cfa_status cfa_linear_async(const cfa_linear_args *a, cfa_stream stre
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     cfa_matmul m = {};
     m.x = a->x;
-    m.w = a->w;
     m.x_stride = a->x_stride;
-    m.w_stride = a->w_stride;
-    cudaError_t e = cudaSuccess;
-    uint8_t *ws = static_cast<uint8_t *>(a->workspace);
-    if (p.move_x) {
-        e = cfa_launch_realign(a->x, a->x_stride, a->tokens, a->cols, ws, p.row, stream);
-        m.x = ws;
-        m.x_stride = p.row;
-    }
-    if (p.move_w && !e) {
-        e = cfa_launch_realign(a->w, a->w_stride, a->rows, a->cols, ws + p.x_bytes, p.row, stream);
-        m.w = ws + p.x_bytes;
-        m.w_stride = p.row;
-    }
-    m.bias = a->bias;
-    m.residual = a->residual;
-    m.y = a->y;
-    m.tokens = a->tokens;
-    m.w_rows = a->rows;
+    m.tokens = m.likely = a->tokens;
     m.cols = a->cols;
     m.r_stride = a->residual_stride;
     m.y_stride = a->y_stride;
     m.n_groups = m.busy = 1;
-    m.likely = a->tokens;
     m.f16 = a->dtype == CFA_DTYPE_F16;
     m.bias_f32 = a->bias && a->bias_dtype == CFA_DTYPE_F32;
-    m.y_f32 = a->y_dtype == CFA_DTYPE_F32;
+    m.bias_up = outs;
+    m.y_f32 = m.exact = a->y_dtype == CFA_DTYPE_F32;
     m.act = a->activation;
     m.gated = gated;
-    if (!e) e = cfa_launch_matmul(&m, 1, 0, stream);
+    uint8_t *ws = static_cast<uint8_t *>(a->workspace), *wws = ws + p.x_bytes;
+    cudaError_t e = cudaSuccess;
+    for (int64_t c = 0; !e && c < outs; c += p.slice) {
+        const int64_t n = outs - c < p.slice ? outs - c : p.slice;
+        cfa_rows move[3];
+        int moves = 0;
+        if (p.move_x && c == 0) {
+            move[moves++] = {a->x, ws, a->x_stride, p.row, a->tokens, a->cols};
+            m.x = ws;
+            m.x_stride = p.row;
+        }
+        m.w = a->w;
+        m.w_stride = a->w_stride;
+        m.w_rows = a->rows;
+        if (p.move_w) {
+            const uint16_t *w = static_cast<const uint16_t *>(a->w);
+            move[moves++] = {w + c * a->w_stride, wws, a->w_stride, p.row, n, a->cols};
+            if (gated)
+                move[moves++] = {w + (outs + c) * a->w_stride, wws + n * p.row * 2, a->w_stride,
+                                 p.row, n, a->cols};
+            m.w = wws;
+            m.w_stride = p.row;
+            m.w_rows = gated ? 2 * n : n;
+        }
+        if (moves) e = cfa_launch_realign(move, moves, stream);
+        m.bias = a->bias ? static_cast<const uint8_t *>(a->bias) + c * (m.bias_f32 ? 4 : 2)
+                         : nullptr;
+        m.residual = a->residual ? static_cast<const uint8_t *>(a->residual) + c * ys : nullptr;
+        m.y = static_cast<uint8_t *>(a->y) + c * ys;
+        if (!e) e = cfa_launch_matmul(&m, 1, 0, stream);
+    }
     return cuda_result("cfa_linear", e);
 }
 

@@ -34,7 +34,9 @@ typedef struct cfa_matmul {
     int32_t n_groups;
     int32_t f16;      /* 1: binary16, 0: bf16 (x, w; bias, residual and y unless f32) */
     int32_t bias_f32, y_f32;
+    int64_t bias_up;  /* gated: where the up rows' bias starts, in elements */
     int32_t act, gated;
+    int32_t exact;    /* 1: the sums are rounded as fp32 results are to be */
     int32_t busy;     /* groups that can hold rows at all (host's bound) */
     int64_t likely;   /* rows to expect in all groups, at most `tokens` */
 } cfa_matmul;
@@ -71,8 +73,13 @@ typedef struct cfa_combine {
     int32_t top_k, f16;
 } cfa_combine;
 cudaError_t cfa_launch_combine(const cfa_combine *c, cudaStream_t stream);
-/* Rows of cols 2-byte elements onto rows of to_stride elements, the rest of each row zeros. */
-cudaError_t cfa_launch_realign(const void *from, int64_t from_stride, int64_t rows, int64_t cols,
-                               void *to, int64_t to_stride, cudaStream_t stream);
+/* Rows of cols 2-byte elements onto rows of to_stride (a multiple of 8) elements at a 16-byte aligned
+ * address, the rest of each row zeros: up to three matrices, none empty. */
+typedef struct cfa_rows {
+    const void *from;
+    void *to;
+    int64_t from_stride, to_stride, rows, cols;
+} cfa_rows;
+cudaError_t cfa_launch_realign(const cfa_rows *m, int n, cudaStream_t stream);
 
 #endif /* CFA_OPS_H */

@@ -283,20 +283,101 @@ __global__ void __launch_bounds__(kThreads) cfa_combine_kernel(const cfa_combine
     }
 }
 
-struct RealignArgs {
+struct RealignMatrix {
     const uint16_t *from;
     uint16_t *to;
     int64_t from_stride, to_stride, rows, cols;
 };
+struct RealignArgs {
+    RealignMatrix m[3];
+};
 
-__global__ void __launch_bounds__(kThreads) cfa_realign_kernel(const RealignArgs a)
+/* 16 bytes that start `phase` bytes (an even number) into the 32 of a and b. */
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, uint32_t phase)
+{
+    const bool half = phase & 2u;
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (phase & 8u) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (phase & 4u) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+/* Rows onto the 16-byte grid, zeros behind the last column.  A warp takes a row: every lane loads the
+ * aligned 16 bytes that its result starts in and has the next lane's for the rest.  Granules that are
+ * not wholly inside the matrix go element by element. */
+__global__ void __launch_bounds__(kThreads) cfa_realign_kernel(const RealignArgs all)
 {
     wait_before();
     release();
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x)
-        for (int64_t i = threadIdx.x; i < a.to_stride; i += kThreads)
-            a.to[r * a.to_stride + i] =
-                i < a.cols ? __ldcg(a.from + r * a.from_stride + i) : (uint16_t)0;
+    const RealignMatrix a = all.m[blockIdx.y];
+    const int lane = threadIdx.x & 31;
+    const int64_t warps = (int64_t)gridDim.x * (kThreads / 32);
+    const uintptr_t begin = (uintptr_t)a.from;
+    const uintptr_t end = begin + 2 * ((a.rows - 1) * a.from_stride + a.cols);
+    const auto granule = [&](uintptr_t at) {
+        if (at >= begin && at + 16 <= end) return __ldcg(reinterpret_cast<const uint4 *>(at));
+        uint32_t w[4] = {};
+        for (int i = 0; i < 8; ++i) {
+            const uintptr_t p = at + 2 * i;
+            if (p >= begin && p + 2 <= end)
+                w[i >> 1] |= (uint32_t)__ldcg(reinterpret_cast<const unsigned short *>(p))
+                             << (16 * (i & 1));
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    for (int64_t r = blockIdx.x * (int64_t)(kThreads / 32) + (threadIdx.x >> 5); r < a.rows;
+         r += warps) {
+        const uintptr_t row = (uintptr_t)(a.from + r * a.from_stride);
+        const uint32_t phase = (uint32_t)(row & 15u);
+        uint4 *to = reinterpret_cast<uint4 *>(a.to + r * a.to_stride);
+        const int64_t n = a.to_stride / 8;
+        for (int64_t c0 = 0; c0 < n; c0 += 4 * 32) {
+            uint4 g[5];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t c = c0 + u * 32 + lane;
+                g[u] = c < n ? granule(row - phase + 16 * c) : make_uint4(0, 0, 0, 0);
+            }
+            g[4] = make_uint4(0, 0, 0, 0);
+            if (phase && lane == 0 && c0 + 128 < n + 1) g[4] = granule(row - phase + 16 * (c0 + 128));
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t c = c0 + u * 32 + lane;
+                uint4 v = g[u];
+                if (phase) { /* the same for the whole warp */
+                    /* the granule behind the lane's: the next lane's, or lane 0's of the next round */
+                    const uint4 mine = lane == 0 ? g[u + 1] : g[u];
+                    uint4 next;
+                    next.x = __shfl_sync(kAll, mine.x, (lane + 1) & 31);
+                    next.y = __shfl_sync(kAll, mine.y, (lane + 1) & 31);
+                    next.z = __shfl_sync(kAll, mine.z, (lane + 1) & 31);
+                    next.w = __shfl_sync(kAll, mine.w, (lane + 1) & 31);
+                    if (c == n - 1) next = granule(row - phase + 16 * (c + 1));
+                    v = shifted(v, next, phase);
+                }
+                if (c >= n) continue;
+                const int64_t left = a.cols - c * 8;
+                if (left < 8) { /* zeros behind the last column */
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i >= left) w[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                to[c] = v;
+            }
+        }
+    }
 }
 
 template <typename Args>
@@ -352,10 +433,16 @@ cudaError_t cfa_launch_combine(const cfa_combine *c, cudaStream_t stream)
                 : launch(cfa_combine_kernel<1>, grid, 0, stream, *c);
 }
 
-cudaError_t cfa_launch_realign(const void *from, int64_t from_stride, int64_t rows, int64_t cols,
-                               void *to, int64_t to_stride, cudaStream_t stream)
+cudaError_t cfa_launch_realign(const cfa_rows *m, int n, cudaStream_t stream)
 {
-    const RealignArgs a = {static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to),
-                           from_stride, to_stride, rows, cols};
-    return launch(cfa_realign_kernel, dim3((unsigned)(rows < 4864 ? rows : 4864)), 0, stream, a);
+    RealignArgs a = {};
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        a.m[i] = {static_cast<const uint16_t *>(m[i].from), static_cast<uint16_t *>(m[i].to),
+                  m[i].from_stride, m[i].to_stride, m[i].rows, m[i].cols};
+        if (m[i].rows > most) most = m[i].rows;
+    }
+    const int64_t blocks = (most + kThreads / 32 - 1) / (kThreads / 32);
+    return launch(cfa_realign_kernel, dim3((unsigned)(blocks < 1216 ? blocks : 1216), (unsigned)n),
+                  0, stream, a);
 }

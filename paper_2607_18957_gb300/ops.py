@@ -191,7 +191,7 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
         need = _lib.ctypes.c_uint64()
         _check(_lib_c.cfa_linear_workspace(
             _LINEAR.pack(xp, wp, bp, rp, 0, 0, 0, t, n, k, xs, ws, rs, os_, code, bc, code, act,
-                         0, 0), _lib.ctypes.byref(need)))
+                         GATED if gated else 0, 0), _lib.ctypes.byref(need)))
         if need.value:
             workspace = _workspace(workspace, need.value, x.device)
             buf, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()

@@ -132,6 +132,32 @@ def test_linear_columns_off_the_grid(t, n, k):
     close(cfa.linear(x, w), *linear64(x, w, None, "none", False, None, BF16))
 
 
+@pytest.mark.parametrize("gated", [False, True])
+def test_linear_moves_a_large_weight_in_slices(gated):
+    """Rows of 8003 elements start at every 2-byte phase; 6000 of them are more than one slice."""
+    g = gen(21)
+    t, n, k = 3, 6000, 8003
+    x, w = normal(g, (t, k), BF16), normal(g, (n, k), BF16, k ** -0.5)
+    b = normal(g, (n,), BF16)
+    r = normal(g, (t, n // 2 if gated else n), BF16)
+    y = cfa.linear(x, w, b, activation="silu", gated=gated, residual=r)
+    close(y, *linear64(x, w, b, "silu", gated, r, BF16))
+
+
+@pytest.mark.parametrize("t,n,k", [(3, 200, 4096), (64, 8, 14336), (200, 260, 4096), (33, 64, 1000)])
+def test_fp32_results_are_rounded_as_fp32(t, n, k):
+    """Parts of 256 columns, 16 truncated additions of at most 2^-23 of the partial sum each, then one
+    rounding per part: far inside the bound of K of them."""
+    g = gen(k)
+    x, w = normal(g, (t, k), BF16), normal(g, (n, k), BF16, k ** -0.5)
+    y = cfa.linear(x, w, out_dtype="f32")
+    ref = x.double() @ w.double().t()
+    size = x.double().abs() @ w.double().abs().t()
+    adds = 16 + 2 + k // 256
+    assert bool(((y.double() - ref).abs() <= adds * 2.0 ** -23 * size).all())
+    assert ((y.double() - ref).norm() / ref.norm()).item() < 1e-6
+
+
 @pytest.mark.parametrize("lead,extra", [(0, 0), (8, 8), (8, 24), (1, 0), (0, 1), (3, 13), (4, 4)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_linear_inside_larger_buffers(lead, extra, gated):
