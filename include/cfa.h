@@ -697,8 +697,8 @@ cfa_status cfa_route_async(const cfa_route_args *args, cfa_stream stream);
  *   y_t = residual_t + sum over j of weights[t, j] * D_e act(G_e x_t) * (U_e x_t),  e = ids[t, j]
  * with [G_e; U_e] = w13[e - first_expert] and D_e = w2[e - first_expert]; without CFA_EXPERTS_GATED
  * w13 is [experts, inter, hidden] and the product with U_e falls away.  Ids outside
- * [first_expert, first_expert + experts) -- another expert-parallel rank's, or -1 -- add nothing and
- * their weights are not read; a token with no other ids gets its residual, or zeros.
+ * [first_expert, first_expert + experts) -- another expert-parallel rank's, or -1 -- add nothing,
+ * whatever their weights; a token with no other ids gets its residual, or zeros.
  *
  *   x         [tokens, hidden];  y, residual [tokens, hidden] of dtype
  *   w13       [experts, 2 * inter, hidden] ([experts, inter, hidden] when not gated), contiguous

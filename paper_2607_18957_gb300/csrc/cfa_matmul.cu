@@ -623,9 +623,16 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         if (m.ids) { /* counted from the pairs themselves */
             for (int32_t g = threadIdx.x; g < m.n_groups; g += kThreads) s->group[2 * g + 2] = 0;
             __syncthreads();
-            for (int32_t i = threadIdx.x; i < m.n_ids; i += kThreads) {
-                const int64_t g = (int64_t)__ldcg(m.ids + i) - m.first;
-                if (g >= 0 && g < m.n_groups) atomicAdd(&s->group[2 * g + 2], 1);
+            for (int32_t i0 = threadIdx.x; i0 < m.n_ids; i0 += 8 * kThreads) {
+                int64_t g[8]; /* eight loads under way at once */
+#pragma unroll
+                for (int32_t j = 0; j < 8; ++j) {
+                    const int32_t i = i0 + j * kThreads;
+                    g[j] = i < m.n_ids ? (int64_t)__ldcg(m.ids + i) - m.first : -1;
+                }
+#pragma unroll
+                for (int32_t j = 0; j < 8; ++j)
+                    if (g[j] >= 0 && g[j] < m.n_groups) atomicAdd(&s->group[2 * g[j] + 2], 1);
             }
             __syncthreads();
         }
@@ -1078,34 +1085,40 @@ uint32_t deep_of(bool pair, uint32_t bn, uint32_t fr)
     return deep;
 }
 
-/* Estimated microseconds of a product.  The CTA with the most tiles goes through its blocks at the
- * pace of their products and of their issue, or of what one SM can take in; a tile's epilogue runs
- * under the next tile's products, but for the last; and all CTAs together are held by L2 and memory.
+/* Estimated microseconds of a product.  The CTAs take their tiles in turns.  A turn takes the longer
+ * of a tile's blocks, at the pace of their products and their issue or of what one SM can take in, and
+ * of the turn's bytes, at the rate of L2 and of memory; the epilogue of a tile runs under the next
+ * tile's products, but for the last.  (Bytes by turns: a last turn of few CTAs cannot draw what memory
+ * gives.)
  * The constants are a fit to 13,800 timings: 182 sizes (1 to 4096 tokens, 256 to 28,672 rows, 1024 to
- * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.7 % longer than
- * the best of those on average, 42 % at the worst. */
+ * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.6 % longer than
+ * the best of those on average, 27 % at the worst. */
 double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int64_t rows, const Cut &c)
 {
-    const double kSplit[3] = {0.0, 3.4, 3.8}; /* one, two and four CTAs per tile */
+    const double kSplit[3] = {0.0, 2.1, 2.5}; /* one, two and four CTAs per tile */
     const uint32_t features = (c.pair ? 2 : 1) * (m->gated ? c.fr / 2 : c.fr);
     const int64_t n_tiles = (rows + c.bn - 1) / c.bn;
-    const double tiles = (double)(n_tiles * m->busy * ((outs + features - 1) / features));
+    const int64_t tiles = n_tiles * m->busy * ((outs + features - 1) / features);
     /* clusters of four leave some SMs out */
     const int64_t slots = c.pair || c.split == 1 ? sms / 2 : c.split == 2 ? sms * 9 / 38 : sms;
-    const double turns = (double)(((int64_t)tiles + slots - 1) / slots);
     const double blocks = (double)((steps + (1u << c.split) - 1) >> c.split);
     const double used = n_tiles == 1 ? (double)((rows + 15) / 16 * 16) : (double)c.bn;
     const double bytes = (double)(c.fr + (c.pair ? c.bn / 2 : c.bn)) * kRowBytes;
-    const double mma = used * (c.pair ? 0.00081 : 0.00085);
-    double step = (mma > 0.159 ? mma : 0.159) + 0.088 / deep_of(c.pair, c.bn, c.fr);
-    if (step < bytes / 133e3) step = bytes / 133e3;
+    const double mma = used * (c.pair ? 0.00091 : 0.00102);
+    double step = (mma > 0.152 ? mma : 0.152) + 0.077 / deep_of(c.pair, c.bn, c.fr);
+    if (step < bytes / 127e3) step = bytes / 127e3;
     const double tokens = (double)(rows < c.bn ? rows : c.bn);
-    const double epilogue = 0.026 * tokens / (1u << c.split), products = blocks * step;
-    const double chain = turns * ((products > epilogue ? products : epilogue) + 0.55) + epilogue;
-    const double l2 = tiles * steps * (c.pair ? 2 : 1) * bytes / 17.1e6;
-    const double mem = 2.0 * m->cols * ((double)m->w_rows * m->busy + (double)m->likely) / 6.6e6;
-    const double shared = (l2 > mem ? l2 : mem) + 1.2;
-    return 2.8 + kSplit[c.split] + (chain > shared ? chain : shared);
+    const double epilogue = 0.025 * tokens / (1u << c.split), products = blocks * step;
+    const double turn = (products > epilogue ? products : epilogue) + 0.6;
+    const double l2 = steps * (c.pair ? 2 : 1) * bytes / 18.1e6; /* per tile */
+    const double mem = 2.0 * m->cols * ((double)m->w_rows * m->busy + (double)m->likely) / 6.6e6 /
+                       (double)tiles;
+    const double share = l2 > mem ? l2 : mem;
+    const int64_t full = tiles / slots, left = tiles - full * slots;
+    double us = 2.8 + kSplit[c.split] + epilogue;
+    us += (double)full * (turn > (double)slots * share ? turn : (double)slots * share);
+    if (left) us += turn > (double)left * share ? turn : (double)left * share;
+    return us;
 }
 
 /* The cut with the least estimate.  Groups are taken as equally full, their number of rows being all
@@ -1130,7 +1143,7 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
             last = bn;
             for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += 16) {
                 for (uint32_t split = 0; split < 3; ++split) {
-                    if (split && (pair || bn > 128 || steps < 4u << split)) break;
+                    if (split && (pair || bn > 64 || steps < 4u << split)) break;
                     const Cut c = {pair != 0, bn, fr, split};
                     const double us = estimate(m, outs, steps, sms, rows, c);
                     if (us < least * 0.995) {

@@ -263,7 +263,7 @@ extern "C" cfa_status cfa_route_async(const cfa_route_args *a, cfa_stream stream
 
 namespace {
 
-constexpr int64_t kCounted = 1024; /* choices that the first product's CTAs count for themselves */
+constexpr int64_t kCounted = 4096; /* choices that the first product's CTAs count for themselves */
 
 struct ExpertsPlan {
     int64_t pairs;

@@ -180,13 +180,12 @@ __global__ void __launch_bounds__(kThreads) cfa_place_kernel(const PlaceArgs a)
             uint4 *o = reinterpret_cast<uint4 *>(to);
             const int64_t n = a.hidden / 8;
             int64_t h = lane;
-            for (; h + 96 < n; h += 128) {
-                const uint4 v0 = __ldcg(f + h), v1 = __ldcg(f + h + 32), v2 = __ldcg(f + h + 64),
-                            v3 = __ldcg(f + h + 96);
-                o[h] = v0;
-                o[h + 32] = v1;
-                o[h + 64] = v2;
-                o[h + 96] = v3;
+            for (; h + 7 * 32 < n; h += 8 * 32) {
+                uint4 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = __ldcg(f + h + u * 32);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) o[h + u * 32] = v[u];
             }
             for (; h < n; h += 32) o[h] = __ldcg(f + h);
         } else {
@@ -200,86 +199,100 @@ __device__ __forceinline__ float half_of(unsigned short b, int f16)
     return f16 ? __half2float(__ushort_as_half(b)) : __bfloat162float(__ushort_as_bfloat16(b));
 }
 
-/* A thread takes eight columns of one token, or one where y or the residual is off the 16-byte grid,
- * and adds the token's choices in their order, in fp32.  Where their rows lie, their weights and the
- * residual are read before the launch's wait: all that is there since the launch before last. */
-constexpr int kAhead = 8; /* choices read ahead */
-template <int N>
-__global__ void __launch_bounds__(kThreads) cfa_combine_kernel(const cfa_combine c)
-{
-    const int64_t per = c.hidden / N, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const bool in = i < c.tokens * per;
-    const int64_t t = in ? i / per : 0, h = in ? (i - t * per) * N : 0;
-    const int64_t at = t * c.y_stride + h, from = t * c.r_stride + h;
-    const int32_t *place = c.place + t * c.top_k;
-    const float *weights = c.weights + t * c.top_k;
+/* The rows and weights of up to kAhead choices of the token that piece i of `per` belongs to. */
+constexpr int kAhead = 4;
+struct Choices {
     int32_t row[kAhead];
-    float w[kAhead], sum[N] = {}, r[N] = {};
+    float w[kAhead];
+    int64_t t, h;
+};
+
+template <int N>
+__device__ __forceinline__ void choose(const cfa_combine &c, int64_t i, int64_t per, Choices &o)
+{
+    const bool in = i < c.tokens * per;
+    o.t = in ? i / per : 0;
+    o.h = in ? (i - o.t * per) * N : 0;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-        row[j] = in && j < c.top_k ? __ldcg(place + j) : -1;
-        w[j] = row[j] >= 0 ? __ldcg(weights + j) : 0.0f;
+        o.row[j] = in && j < c.top_k ? __ldcg(c.place + o.t * c.top_k + j) : -1;
+        o.w[j] = in && j < c.top_k ? __ldcg(c.weights + o.t * c.top_k + j) : 0.0f;
     }
-    if (in && c.residual) {
-        if constexpr (N == 8) {
-            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(
-                static_cast<const uint16_t *>(c.residual) + from));
-            const unsigned short *b = reinterpret_cast<const unsigned short *>(&v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = half_of(b[k], c.f16);
-        } else {
-            r[0] = half_of(__ldcg(static_cast<const unsigned short *>(c.residual) + from), c.f16);
-        }
-    }
-    wait_before();
-    if (!in) return;
-    const float *part = c.part + h;
+}
+
+template <int N>
+__device__ __forceinline__ void add_row(const cfa_combine &c, int64_t row, int64_t h, float w,
+                                        float (&sum)[N])
+{
     if constexpr (N == 8) {
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (row[j] < 0) continue;
-            const float4 *p = reinterpret_cast<const float4 *>(part + row[j] * c.hidden);
-            const float4 a = __ldcg(p), b = __ldcg(p + 1);
-            sum[0] += w[j] * a.x;
-            sum[1] += w[j] * a.y;
-            sum[2] += w[j] * a.z;
-            sum[3] += w[j] * a.w;
-            sum[4] += w[j] * b.x;
-            sum[5] += w[j] * b.y;
-            sum[6] += w[j] * b.z;
-            sum[7] += w[j] * b.w;
-        }
+        const float4 *p = reinterpret_cast<const float4 *>(c.part + row * c.hidden + h);
+        const float4 a = __ldcg(p), b = __ldcg(p + 1);
+        sum[0] += w * a.x;
+        sum[1] += w * a.y;
+        sum[2] += w * a.z;
+        sum[3] += w * a.w;
+        sum[4] += w * b.x;
+        sum[5] += w * b.y;
+        sum[6] += w * b.z;
+        sum[7] += w * b.w;
     } else {
+        sum[0] += w * __ldcg(c.part + row * c.hidden + h);
+    }
+}
+
+/* A thread takes eight columns of one token at a time, or one where y or the residual is off the 16-byte
+ * grid, and adds the token's choices in their order, in fp32.  Where their rows lie and their weights it
+ * reads a round ahead, and for the first before the launch's wait: both are there since the launch
+ * before last.  (One piece per thread, in as many blocks as there are pieces, took twice as long on
+ * 4096 tokens: every block waited for the two loads one after the other.) */
+template <int N>
+__global__ void __launch_bounds__(kThreads, 4) cfa_combine_kernel(const cfa_combine c)
+{
+    const int64_t per = c.hidden / N, all = c.tokens * per, step = (int64_t)gridDim.x * kThreads;
+    int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    Choices now;
+    choose<N>(c, i, per, now);
+    wait_before();
+    for (; i < all; i += step) {
+        float sum[N] = {};
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
-            if (row[j] >= 0) sum[0] += w[j] * __ldcg(part + row[j] * c.hidden);
-    }
-    for (int j = kAhead; j < c.top_k; ++j) {
-        const int64_t more = __ldcg(place + j);
-        if (more < 0) continue;
-        const float v = __ldcg(weights + j);
-#pragma unroll
-        for (int k = 0; k < N; ++k) sum[k] += v * __ldcg(part + more * c.hidden + k);
-    }
-    if constexpr (N == 8) {
-        uint32_t o[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float x = sum[2 * k] + r[2 * k], y = sum[2 * k + 1] + r[2 * k + 1];
-            if (c.f16) {
-                const __half2 v = __floats2half2_rn(x, y);
-                o[k] = *reinterpret_cast<const uint32_t *>(&v);
-            } else {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
-                o[k] = *reinterpret_cast<const uint32_t *>(&v);
-            }
+            if (now.row[j] >= 0) add_row<N>(c, now.row[j], now.h, now.w[j], sum);
+        const int64_t t = now.t, h = now.h;
+        choose<N>(c, i + step, per, now);
+        for (int j = kAhead; j < c.top_k; ++j) {
+            const int64_t row = __ldcg(c.place + t * c.top_k + j);
+            if (row >= 0) add_row<N>(c, row, h, __ldcg(c.weights + t * c.top_k + j), sum);
         }
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(c.y) + at) =
-            make_uint4(o[0], o[1], o[2], o[3]);
-    } else if (c.f16) {
-        static_cast<__half *>(c.y)[at] = __float2half_rn(sum[0] + r[0]);
-    } else {
-        static_cast<__nv_bfloat16 *>(c.y)[at] = __float2bfloat16_rn(sum[0] + r[0]);
+        const int64_t at = t * c.y_stride + h, from = t * c.r_stride + h;
+        if constexpr (N == 8) {
+            if (c.residual) {
+                const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(
+                    static_cast<const uint16_t *>(c.residual) + from));
+                const unsigned short *b = reinterpret_cast<const unsigned short *>(&v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] += half_of(b[k], c.f16);
+            }
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (c.f16) {
+                    const __half2 v = __floats2half2_rn(sum[2 * k], sum[2 * k + 1]);
+                    o[k] = *reinterpret_cast<const uint32_t *>(&v);
+                } else {
+                    const __nv_bfloat162 v = __floats2bfloat162_rn(sum[2 * k], sum[2 * k + 1]);
+                    o[k] = *reinterpret_cast<const uint32_t *>(&v);
+                }
+            }
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(c.y) + at) =
+                make_uint4(o[0], o[1], o[2], o[3]);
+        } else {
+            if (c.residual)
+                sum[0] += half_of(__ldcg(static_cast<const unsigned short *>(c.residual) + from),
+                                  c.f16);
+            if (c.f16) static_cast<__half *>(c.y)[at] = __float2half_rn(sum[0]);
+            else static_cast<__nv_bfloat16 *>(c.y)[at] = __float2bfloat16_rn(sum[0]);
+        }
     }
 }
 
@@ -412,8 +425,9 @@ cudaError_t cfa_launch_sort(const cfa_sort *s, const void *x, int64_t x_stride, 
 {
     const size_t smem = sizeof(int32_t) * s->experts;
     PlaceArgs a = {*s, x, xs, x_stride, hidden, 0, (int32_t)cfa_sort_blocks(s->pairs), 0};
-    /* chunks of a power of two, so that they do not straddle blocks: about one per SM */
-    for (a.chunk = 1; a.chunk < kThreads && s->pairs > (int64_t)a.chunk * 160; a.chunk *= 2) {
+    /* chunks of a power of two, so that they do not straddle blocks: two to four per SM, so that
+     * enough rows are under way */
+    for (a.chunk = 1; a.chunk < kThreads && s->pairs > (int64_t)a.chunk * 608; a.chunk *= 2) {
     }
     a.vec = (((uintptr_t)x | (uintptr_t)xs | (uint64_t)x_stride * 2 | (uint64_t)hidden * 2) & 15u) ==
             0;
@@ -427,8 +441,8 @@ cudaError_t cfa_launch_combine(const cfa_combine *c, cudaStream_t stream)
 {
     const bool wide = (((uintptr_t)c->y | (uintptr_t)c->residual | (uint64_t)c->y_stride * 2 |
                         (c->residual ? (uint64_t)c->r_stride * 2 : 0)) & 15u) == 0;
-    const int64_t threads = c->tokens * (c->hidden / (wide ? 8 : 1));
-    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
+    const int64_t blocks = (c->tokens * (c->hidden / (wide ? 8 : 1)) + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)(blocks < 608 ? blocks : 608)); /* four per SM */
     return wide ? launch(cfa_combine_kernel<8>, grid, 0, stream, *c)
                 : launch(cfa_combine_kernel<1>, grid, 0, stream, *c);
 }
