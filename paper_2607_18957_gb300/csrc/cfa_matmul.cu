@@ -1043,14 +1043,17 @@ void configure(Config *c, unsigned grid, unsigned cluster, bool early, cudaStrea
     c->cfg.dynamicSmemBytes = kSmem;
     c->cfg.stream = stream;
     c->cfg.attrs = c->attr;
-    c->attr[0].id = cudaLaunchAttributeClusterDimension;
-    c->attr[0].val.clusterDim.x = cluster;
-    c->attr[0].val.clusterDim.y = c->attr[0].val.clusterDim.z = 1;
-    c->cfg.numAttrs = 1;
+    c->cfg.numAttrs = 0;
+    if (cluster > 1) {
+        cudaLaunchAttribute &attr = c->attr[c->cfg.numAttrs++];
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = cluster;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    }
     if (early) {
-        c->attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        c->attr[1].val.programmaticStreamSerializationAllowed = 1;
-        c->cfg.numAttrs = 2;
+        cudaLaunchAttribute &attr = c->attr[c->cfg.numAttrs++];
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
     }
 }
 

@@ -26,6 +26,7 @@ torch = None
 _CODE = None    # torch dtype -> CFA_DTYPE_*
 _DTYPE = None   # dtype name -> torch dtype
 _lib_c = None
+_EXPERTS_BYTES = {}  # workspace bytes of experts by its sizes
 _raw_stream = _device = _grad = None
 
 
@@ -106,12 +107,8 @@ class _On:
 
 
 def _elsewhere(stream, device):
-    """The guard of a call that is not for the current device's current stream, or None."""
-    if stream is not None:
-        return _On(stream, device)
-    if device != _device():
-        return torch.cuda.device(device)
-    return None
+    """The guard of a call that is not for the current device's current stream."""
+    return torch.cuda.device(device) if stream is None else _On(stream, device)
 
 
 def _workspace(given, need, device):
@@ -139,20 +136,31 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
     if torch is None:
         _start()
     device = x.get_device()
-    _on(x, "x", device)
-    _on(weight, "weight", device)
-    guard = _elsewhere(stream, device)
-    if guard is not None:
-        with guard:
+    if device < 0 or weight.get_device() != device or (
+            _grad() and (x.requires_grad or weight.requires_grad)):
+        _on(x, "x", device)
+        _on(weight, "weight", device)
+    if stream is not None or device != _device():
+        with _elsewhere(stream, device):
             return linear(x, weight, bias, activation=activation, gated=gated, residual=residual,
                           out=out, out_dtype=out_dtype, workspace=workspace)
-    wshape = weight.shape
+    wshape, xshape = weight.shape, x.shape
     if len(wshape) != 2:
         raise ValueError(f"weight: shape {tuple(wshape)}")
     n, k = wshape
-    t, xs = _rows(x, "x", k)
+    ws, one = weight.stride()
+    if one != 1 and k > 1:
+        _on(weight, "weight", device)
+    if len(xshape) == 2 and xshape[1] == k:
+        t = xshape[0]
+        xs, one = x.stride()
+        if one != 1 and k > 1:
+            _on(x, "x", device)
+    else:
+        _on(x, "x", device)
+        t, xs = _rows(x, "x", k)
     dtype = x.dtype
-    code = _code(x, "x")
+    code = _CODE.get(dtype) or _code(x, "x")
     if weight.dtype is not dtype:
         raise ValueError(f"weight is {weight.dtype}, x {dtype}")
     act = _one_of(ACTIVATION, activation, "activation")
@@ -167,9 +175,11 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
         if bias.shape != (n,):
             raise ValueError(f"bias: shape {tuple(bias.shape)}, not ({n},)")
         bp, bc = bias.data_ptr(), _code(bias, "bias")
-    xshape = x.shape
     shape = (t, no) if len(xshape) == 2 else xshape[:-1] + (no,)
-    odtype = dtype if out_dtype is None else _one_of(_DTYPE, out_dtype, "out_dtype")
+    odtype, oc = dtype, code
+    if out_dtype is not None:
+        odtype = _one_of(_DTYPE, out_dtype, "out_dtype")
+        oc = _CODE[odtype]
     if out is None:
         out = torch.empty(shape, dtype=odtype, device=x.device)
         os_ = no
@@ -177,7 +187,7 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
         _on(out, "out", device)
         if out.shape != shape or (out_dtype is not None and out.dtype is not odtype):
             raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, not {tuple(shape)}")
-        odtype = out.dtype
+        odtype, oc = out.dtype, _code(out, "out")
         _, os_ = _rows(out, "out", no)
     if residual is not None:
         _on(residual, "residual", device)
@@ -186,7 +196,7 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
                              f"{tuple(shape)}")
         _, rs = _rows(residual, "residual", no)
         rp = residual.data_ptr()
-    xp, wp, ws = x.data_ptr(), weight.data_ptr(), weight.stride(0)
+    xp, wp = x.data_ptr(), weight.data_ptr()
     if (xp | wp | (xs | ws) * 2) & 15:
         need = _lib.ctypes.c_uint64()
         _check(_lib_c.cfa_linear_workspace(
@@ -197,7 +207,7 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
             buf, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     st = _lib_c.cfa_linear_async(
         _LINEAR.pack(xp, wp, bp, rp, out.data_ptr(), buf, size, t, n, k, xs, ws, rs, os_, code, bc,
-                     _code(out, "out"), act, GATED if gated else 0, 0), _raw_stream(device))
+                     oc, act, GATED if gated else 0, 0), _raw_stream(device))
     if st:
         _check(st)
     return out
@@ -219,15 +229,22 @@ def route(logits, top_k, *, scoring="softmax", bias=None, groups=1, top_groups=1
     if torch is None:
         _start()
     device = logits.get_device()
-    _on(logits, "logits", device)
-    guard = _elsewhere(stream, device)
-    if guard is not None:
-        with guard:
+    if device < 0 or (logits.requires_grad and _grad()):
+        _on(logits, "logits", device)
+    if stream is not None or device != _device():
+        with _elsewhere(stream, device):
             return route(logits, top_k, scoring=scoring, bias=bias, groups=groups,
                          top_groups=top_groups, renormalize=renormalize, scale=scale, out=out)
     lshape = logits.shape
-    e = lshape[-1] if lshape else 0
-    t, ls = _rows(logits, "logits", e)
+    if len(lshape) == 2 and lshape[1]:
+        t, e = lshape
+        ls, one = logits.stride()
+        if one != 1 and e > 1:
+            _on(logits, "logits", device)
+    else:
+        _on(logits, "logits", device)
+        e = lshape[-1] if lshape else 0
+        t, ls = _rows(logits, "logits", e)
     bp = 0
     if bias is not None:
         _on(bias, "bias", device)
@@ -238,11 +255,12 @@ def route(logits, top_k, *, scoring="softmax", bias=None, groups=1, top_groups=1
     if top_k < 1:
         raise ValueError(f"top_k is {top_k}")
     shape = (t, top_k) if len(lshape) == 2 else lshape[:-1] + (top_k,)
-    code = _code(logits, "logits")
+    code = _CODE.get(logits.dtype) or _code(logits, "logits")
     score = _one_of(SCORING, scoring, "scoring") if scoring != "softmax" else 0
     if out is None:
-        weights = torch.empty(shape, dtype=torch.float32, device=logits.device)
-        ids = torch.empty(shape, dtype=torch.int32, device=logits.device)
+        on = logits.device
+        weights = torch.empty(shape, dtype=torch.float32, device=on)
+        ids = torch.empty(shape, dtype=torch.int32, device=on)
     else:
         weights, ids = out
         for o, dt, name in ((weights, torch.float32, "weights"), (ids, torch.int32, "ids")):
@@ -272,38 +290,43 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
     if torch is None:
         _start()
     device = x.get_device()
-    _on(x, "x", device)
-    guard = _elsewhere(stream, device)
-    if guard is not None:
-        with guard:
+    if device < 0 or not (ids.get_device() == weights.get_device() == w13.get_device() ==
+                          w2.get_device() == device) or (
+            _grad() and (x.requires_grad or weights.requires_grad or w13.requires_grad or
+                         w2.requires_grad)):
+        for v, name in ((x, "x"), (ids, "ids"), (weights, "weights"), (w13, "w13"), (w2, "w2")):
+            _on(v, name, device)
+    if stream is not None or device != _device():
+        with _elsewhere(stream, device):
             return experts(x, ids, weights, w13, w2, activation=activation,
                            first_expert=first_expert, residual=residual, out=out,
                            workspace=workspace)
-    for v, name in ((ids, "ids"), (weights, "weights"), (w13, "w13"), (w2, "w2")):
-        _on(v, name, device)
-        if not v.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    if w13.dim() != 3 or w2.dim() != 3:
-        raise ValueError(f"w13 {tuple(w13.shape)} and w2 {tuple(w2.shape)} have three dimensions")
-    e, h, i = w2.shape
-    gated = w13.shape == (e, 2 * i, h)
-    if not gated and w13.shape != (e, i, h):
-        raise ValueError(f"w13 {tuple(w13.shape)} does not fit w2 {tuple(w2.shape)}")
+    if not (ids.is_contiguous() and weights.is_contiguous() and w13.is_contiguous() and
+            w2.is_contiguous()):
+        raise ValueError("ids, weights, w13 and w2 must be contiguous")
+    shape, ishape, w2shape, w13shape = x.shape, ids.shape, w2.shape, w13.shape
+    if len(w2shape) != 3 or len(w13shape) != 3:
+        raise ValueError(f"w13 {tuple(w13shape)} and w2 {tuple(w2shape)} have three dimensions")
+    e, h, i = w2shape
+    gated = w13shape[1] == 2 * i
+    if w13shape[0] != e or w13shape[2] != h or not (gated or w13shape[1] == i):
+        raise ValueError(f"w13 {tuple(w13shape)} does not fit w2 {tuple(w2shape)}")
     dtype = x.dtype
     if w13.dtype is not dtype or w2.dtype is not dtype:
         raise ValueError(f"w13 is {w13.dtype}, w2 {w2.dtype}, x {dtype}")
+    _on(x, "x", device)
     t, xs = _rows(x, "x", h)
-    shape, ishape = x.shape, ids.shape
     top_k = ishape[-1] if ishape else 0
     if (ishape[:-1] != shape[:-1] or weights.shape != ishape or ids.dtype is not torch.int32 or
             weights.dtype is not torch.float32):
         raise ValueError(f"ids {ids.dtype} {tuple(ishape)} and weights {weights.dtype} "
                          f"{tuple(weights.shape)} must be int32 and float32 {tuple(shape[:-1])} + "
                          "(top_k,)")
-    code = _code(x, "x")
-    act = _one_of(ACTIVATION, activation, "activation")
+    code = _CODE.get(dtype) or _code(x, "x")
+    act = 4 if activation == "silu" else _one_of(ACTIVATION, activation, "activation")
+    on = x.device
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out = torch.empty(shape, dtype=dtype, device=on)
         os_ = h
     else:
         _on(out, "out", device)
@@ -320,14 +343,27 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
         rp = residual.data_ptr()
     ptrs = (x.data_ptr(), w13.data_ptr(), w2.data_ptr(), rp, ids.data_ptr(), weights.data_ptr(),
             out.data_ptr())
-    rest = (t, h, i, xs, rs, os_, e, first_expert, top_k, code, act, GATED if gated else 0)
-    need = _lib.ctypes.c_uint64()
-    _check(_lib_c.cfa_experts_workspace(_EXPERTS.pack(*ptrs, 0, 0, *rest),
-                                        _lib.ctypes.byref(need)))
-    workspace = _workspace(workspace, need.value, x.device)
-    _check(_lib_c.cfa_experts_async(
-        _EXPERTS.pack(*ptrs, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                      *rest), _raw_stream(device)))
+    flags = GATED if gated else 0
+    sizes = (t, h, i, e, top_k)
+    need = _EXPERTS_BYTES.get(sizes)  # by the sizes alone
+    if need is None or code not in (2, 3):
+        size = _lib.ctypes.c_uint64()
+        _check(_lib_c.cfa_experts_workspace(
+            _EXPERTS.pack(*ptrs, 0, 0, t, h, i, xs, rs, os_, e, first_expert, top_k, code, act,
+                          flags), _lib.ctypes.byref(size)))
+        if len(_EXPERTS_BYTES) >= 1024:
+            _EXPERTS_BYTES.clear()
+        need = _EXPERTS_BYTES[sizes] = size.value
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=on)
+    else:
+        _workspace(workspace, need, on)
+    st = _lib_c.cfa_experts_async(
+        _EXPERTS.pack(*ptrs, workspace.data_ptr(), workspace.numel() * workspace.element_size(), t,
+                      h, i, xs, rs, os_, e, first_expert, top_k, code, act, flags),
+        _raw_stream(device))
+    if st:
+        _check(st)
     return out
 
 
