@@ -400,20 +400,6 @@ __device__ __forceinline__ Tile tile_at(const Args &a, const Shared *s, int32_t 
     return o;
 }
 
-/* One value of y: plus the residual, rounded. */
-__device__ __forceinline__ void store_one(const cfa_matmul &m, int64_t row, int64_t col, float v)
-{
-    if (m.residual) {
-        const int64_t at = row * m.r_stride + col;
-        v += m.y_f32 ? value(static_cast<const float *>(m.residual), at)
-                     : value(m.residual, at, m.f16);
-    }
-    const int64_t at = row * m.y_stride + col;
-    if (m.y_f32) static_cast<float *>(m.y)[at] = v;
-    else if (m.f16) static_cast<__half *>(m.y)[at] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16 *>(m.y)[at] = __float2bfloat16_rn(v);
-}
-
 __device__ __forceinline__ uint32_t pack(float lo, float hi, int f16)
 {
     if (f16) {
@@ -430,76 +416,126 @@ __device__ __forceinline__ float2 unpack(uint32_t v, int f16)
     return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&v));
 }
 
-/* N tokens' values of the lane's column: token i of the batch stands at row + i * step, if i * step
- * + 1 <= n.  Neighbouring lanes trade every second value, so that an even lane stores columns (c, c
- * + 1) of the tokens 0, 2, .. of the batch and an odd lane (c - 1, c) of the tokens 1, 3, ..; pairs
- * is false where y or the residual is off that grid. */
+/* What a lane stores of a batch of N tokens: token i of the batch stands at row + i * step, if i * step
+ * + 1 <= n.  With a.pairs, neighbouring lanes trade every second value, so that an even lane stores
+ * columns (c, c + 1) of the tokens 0, 2, .. of the batch and an odd lane (c - 1, c) of the tokens 1, 3,
+ * ..; without (y or the residual off that grid, or a last column on its own) each lane stores its own
+ * column of every token. */
+struct Place {
+    int64_t row, col;
+    int step, n;
+};
+
+__device__ __forceinline__ bool by_pairs(const Args &a, const Place &p)
+{
+    return a.pairs && (p.col | 1) < a.outs;
+}
+
+/* The residual where the lane will store. */
+struct Residual {
+    uint32_t lo[16], hi[8]; /* pairs of fp32 take both, one of a pair at a time */
+};
+
 template <int N>
-__device__ __forceinline__ void store(const Args &a, float (&v)[N], int64_t row, int step, int n,
-                                      int64_t col)
+__device__ __forceinline__ void fetch(const Args &a, const Place &p, Residual &r)
 {
     const cfa_matmul &m = a.m;
-    if (!a.pairs) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (col < a.outs && i * step < n) store_one(m, row + i * step, col, v[i]);
-        return;
-    }
-    const int odd = threadIdx.x & 1;
-    const bool in = (col | 1) < a.outs;         /* both columns of the pair */
-    const bool last = !in && !odd && col < a.outs; /* a last column on its own */
-    float2 o[N / 2];
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * i] : v[2 * i + 1], 1);
-        o[i] = odd ? make_float2(got, v[2 * i + 1]) : make_float2(v[2 * i], got);
-    }
-    if (last) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i * step < n) store_one(m, row + i * step, col, v[i]);
-    }
-    if (!in) return;
-    const int64_t c = col - odd;
-    const int first = odd * step; /* token of o[0] */
-    if (m.residual) {
-        const int64_t at = (row + first) * m.r_stride + c;
+    if (!m.residual) return;
+    if (by_pairs(a, p)) {
+        const int odd = threadIdx.x & 1, first = odd * p.step;
+        const int64_t at = (p.row + first) * m.r_stride + p.col - odd;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
-            if (first + 2 * i * step >= n) continue;
-            const int64_t from = at + 2 * i * step * m.r_stride;
-            const float2 r =
-                m.y_f32 ? __ldcg(reinterpret_cast<const float2 *>(
-                              static_cast<const float *>(m.residual) + from))
-                        : unpack(__ldcg(reinterpret_cast<const uint32_t *>(
-                                     static_cast<const uint16_t *>(m.residual) + from)), m.f16);
-            o[i].x += r.x;
-            o[i].y += r.y;
+            if (first + 2 * i * p.step >= p.n) continue;
+            const int64_t from = at + 2 * i * p.step * m.r_stride;
+            if (m.y_f32) {
+                const uint2 v = __ldcg(reinterpret_cast<const uint2 *>(
+                    static_cast<const float *>(m.residual) + from));
+                r.lo[i] = v.x;
+                r.hi[i] = v.y;
+            } else {
+                r.lo[i] = __ldcg(reinterpret_cast<const uint32_t *>(
+                    static_cast<const uint16_t *>(m.residual) + from));
+            }
+        }
+    } else if (p.col < a.outs) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i * p.step >= p.n) continue;
+            const int64_t from = (p.row + i * p.step) * m.r_stride + p.col;
+            if (m.y_f32) r.lo[i] = __ldcg(static_cast<const uint32_t *>(m.residual) + from);
+            else r.lo[i] = __ldcg(static_cast<const unsigned short *>(m.residual) + from);
         }
     }
-    const int64_t at = (row + first) * m.y_stride + c;
-    if (m.y_f32) {
-        float *to = static_cast<float *>(m.y) + at;
+}
+
+template <int N>
+__device__ __forceinline__ void store(const Args &a, float (&v)[N], const Place &p, const Residual &r)
+{
+    const cfa_matmul &m = a.m;
+    float2 o[N / 2];
+    const int odd = threadIdx.x & 1, first = odd * p.step;
+    if (a.pairs) { /* every lane trades */
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i)
-            if (first + 2 * i * step < n)
-                *reinterpret_cast<float2 *>(to + 2 * i * step * m.y_stride) = o[i];
-    } else {
-        uint16_t *to = static_cast<uint16_t *>(m.y) + at;
+        for (int i = 0; i < N / 2; ++i) {
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * i] : v[2 * i + 1], 1);
+            o[i] = odd ? make_float2(got, v[2 * i + 1]) : make_float2(v[2 * i], got);
+        }
+    }
+    if (by_pairs(a, p)) {
+        if (m.residual) {
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i)
-            if (first + 2 * i * step < n)
-                *reinterpret_cast<uint32_t *>(to + 2 * i * step * m.y_stride) =
-                    pack(o[i].x, o[i].y, m.f16);
+            for (int i = 0; i < N / 2; ++i) {
+                const float2 x = m.y_f32 ? make_float2(__uint_as_float(r.lo[i]),
+                                                       __uint_as_float(r.hi[i]))
+                                         : unpack(r.lo[i], m.f16);
+                o[i].x += x.x;
+                o[i].y += x.y;
+            }
+        }
+        const int64_t at = (p.row + first) * m.y_stride + p.col - odd;
+        if (m.y_f32) {
+            float *to = static_cast<float *>(m.y) + at;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                if (first + 2 * i * p.step < p.n)
+                    *reinterpret_cast<float2 *>(to + 2 * i * p.step * m.y_stride) = o[i];
+        } else {
+            uint16_t *to = static_cast<uint16_t *>(m.y) + at;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                if (first + 2 * i * p.step < p.n)
+                    *reinterpret_cast<uint32_t *>(to + 2 * i * p.step * m.y_stride) =
+                        pack(o[i].x, o[i].y, m.f16);
+        }
+    } else if (p.col < a.outs) {
+        const int64_t at = p.row * m.y_stride + p.col;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i * p.step >= p.n) continue;
+            float x = v[i];
+            const int64_t to = at + i * p.step * m.y_stride;
+            if (m.residual)
+                x += m.y_f32 ? __uint_as_float(r.lo[i]) : unpack(r.lo[i], m.f16).x;
+            if (m.y_f32) static_cast<float *>(m.y)[to] = x;
+            else static_cast<uint16_t *>(m.y)[to] = (uint16_t)pack(x, 0.0f, m.f16);
+        }
     }
 }
 
 /* N of 16 tokens' sums of the lane's weight row, of which n are in the tile: bias, activation, store.
  * Gated: of 16 lanes, 8 hold gate values and the next 8 the up values of the same columns; of two tokens
  * the gate's lanes finish the first and the others the second. */
+template <bool GATED>
+__device__ __forceinline__ Place place_of(int64_t row, int n, int64_t col)
+{
+    const int upper = GATED && (threadIdx.x & 8) ? 1 : 0;
+    return {row + upper, col, GATED ? 2 : 1, n - upper};
+}
+
 template <bool GATED, int N>
-__device__ __forceinline__ void finish(const Args &a, float (&all)[16], int64_t row, int n, int64_t col,
-                                       float bias)
+__device__ __forceinline__ void finish(const Args &a, float (&all)[16], const Place &p, float bias,
+                                       const Residual &r)
 {
     const cfa_matmul &m = a.m;
     float v[N];
@@ -517,10 +553,10 @@ __device__ __forceinline__ void finish(const Args &a, float (&all)[16], int64_t 
         activate(gate, m.act);
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) gate[j] *= up[j];
-        store<N / 2>(a, gate, row + (upper ? 1 : 0), 2, n - (upper ? 1 : 0), col);
+        store<N / 2>(a, gate, p, r);
     } else {
         activate(v, m.act);
-        store<N>(a, v, row, 1, n, col);
+        store<N>(a, v, p, r);
     }
 }
 
@@ -878,6 +914,15 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 bias = m.bias_f32 ? value(static_cast<const float *>(m.bias), at)
                                   : value(m.bias, at, m.f16);
             }
+            int32_t c0 = 0, c1 = o.rows; /* the tokens that this CTA finishes */
+            if (sync_tiles) {            /* of a cluster, each its share */
+                const int32_t even = (((o.rows - 1) >> share) + 2) & ~1;
+                c0 = (int32_t)rank * even;
+                c1 = min(o.rows, c0 + even);
+            }
+            Residual next; /* of the next batch, on its way since the one before */
+            if (!dry && c0 < c1)
+                fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c0, c1 - c0, col), next);
             /* the parts before the last are added up in tensor memory */
             bool more = false; /* a sum lies there */
             if (!dry) {
@@ -903,7 +948,6 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 fence_after();
             }
             const uint32_t src = lanes + buf * a.acc_on, sum = lanes + 2 * a.acc_on;
-            int32_t c0 = 0, c1 = o.rows;
             uint32_t sharers = 0;
             float v[16];
             if (sync_tiles) {
@@ -915,10 +959,6 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                         partial[(c + j) * kRows + warp * 32 + lane] = v[j];
                 }
                 if (!dry) cluster_sync();
-                /* each CTA of the cluster finishes its share of the tokens */
-                const int32_t even = (((o.rows - 1) >> share) + 2) & ~1;
-                c0 = (int32_t)rank * even;
-                c1 = min(o.rows, c0 + even);
                 sharers = dry ? 1u : 1u << share;
             }
             const bool few = c1 - c0 <= 4;
@@ -947,9 +987,12 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     for (int j = 0; j < 16; ++j)
                         v[j] = ((p[0][j] + p[1][j]) + p[2][j]) + p[3][j];
                 }
-                const int n = dry ? 0 : c1 - c;
-                if (few) finish<GATED, 4>(a, v, o.row + c, n, col, bias);
-                else finish<GATED, 16>(a, v, o.row + c, n, col, bias);
+                const Place p = place_of<GATED>(o.row + c, dry ? 0 : c1 - c, col);
+                const Residual r = next;
+                if (c + 16 < c1)
+                    fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c + 16, c1 - c - 16, col), next);
+                if (few) finish<GATED, 4>(a, v, p, bias, r);
+                else finish<GATED, 16>(a, v, p, bias, r);
             }
             if (dry) {
                 dry = false;
