@@ -66,8 +66,9 @@ struct Args {
     uint32_t fr;         /* weight rows per CTA: a multiple of 8, gated of 16 */
     uint32_t stages;
     uint32_t deep;       /* blocks of kDepth columns per stage */
-    uint32_t wide;       /* a gated w has groups of 8 rows, or w is not gated */
     uint32_t whole;      /* whole blocks; the last of steps may lack columns */
+    int32_t f_whole;     /* gated, with a last group of fewer than 8 rows: the features before it, which
+                            a tile at once has to stay inside; otherwise INT32_MAX */
     uint32_t steps;      /* blocks in all */
     uint32_t acc_on;     /* columns of tensor memory from one accumulator to the next */
     uint32_t f_tiles;    /* feature tiles per group */
@@ -723,7 +724,6 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps >> share;
     const bool sync_tiles = !PAIR && share > 0;
     const uint32_t deep = a.deep, stages = a.stages, part = EXACT ? kPart : a.steps;
-    const uint32_t at_once_to = a.wide ? a.whole : 0; /* blocks that a stage's loads can bring at once */
     bool ok = true;
     if (a.early_w && warp != kLoader) launch_wait(a);
 
@@ -749,6 +749,8 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 const CUtensorMap *const xmap = a.xmap + box, *const xtail = a.xtail + box;
                 const uint32_t x_one = a.x_box[box] * kRowBytes;
                 const uint32_t w_loaded = deep * w_bytes, all = w_loaded + deep * x_one;
+                /* blocks that a stage's loads can bring at once */
+                const uint32_t at_once_to = f + (int32_t)per_cta <= a.f_whole ? a.whole : 0;
                 /* Stages of the first tile get their w before the launch's wait, as many as there are,
                  * and then their x. */
                 uint32_t ahead = 0;
@@ -1253,8 +1255,8 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const uint32_t block = (a.fr + x_rows) * kRowBytes;
     a.deep = deep_of(pair, a.bn, a.fr);
     const uint32_t stage = block * a.deep;
-    a.wide = !gated || a.outs % 8 == 0;
     a.whole = (uint32_t)(m->cols / kDepth);
+    a.f_whole = gated && a.outs % 8 ? (int32_t)(a.outs / 8 * 8) : INT32_MAX;
     /* the products read kRows rows of each block of w, whatever lies behind the a.fr of them */
     const uint32_t after = a.fr + a.deep * x_rows;
     const uint32_t behind = kRows > after ? (kRows - after) * kRowBytes : 0;
@@ -1289,7 +1291,7 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     const cuuint64_t on = kRowBytes, groups = (cuuint64_t)m->n_groups, blocks = a.whole;
     const cuuint64_t outs = (cuuint64_t)a.outs, rows = (cuuint64_t)m->w_rows;
     const cuuint64_t tokens = (cuuint64_t)m->tokens;
-    if (a.wide && blocks) {
+    if (blocks && a.f_whole) {
         if (gated) { /* 64 columns, 8 rows, gate or up of each group, the next 8 rows, block */
             const cuuint64_t dim[5] = {kDepth, 8, 2 * groups, outs / 8, blocks};
             const cuuint64_t stride[4] = {wld, wld * outs, wld * 8, on};
@@ -1308,7 +1310,7 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
             fine = encode(&a.xmap[i], m->f16, m->x, 3, dim, stride, box);
         }
     }
-    if (fine && (!a.wide || a.steps > a.whole)) {
+    if (fine && (a.f_whole != INT32_MAX || a.steps > a.whole)) {
         if (gated) {
             const cuuint64_t dim[4] = {k, outs, 2, groups};
             const cuuint64_t stride[3] = {wld, wld * outs, wld * outs * 2};

@@ -125,6 +125,17 @@ def test_linear_epilogue(t, n, k, act, gated):
         close(y, *linear64(x, w, b, act, gated, r, y.dtype))
 
 
+@pytest.mark.parametrize("t,n,k", [(3, 16, 128), (70, 144, 128), (300, 2000, 320), (5, 24, 64),
+                                   (9, 14, 192), (200, 310, 256), (600, 1030, 128), (2, 2, 64),
+                                   (40, 6, 72)])
+def test_linear_gated_rows_that_do_not_fill_their_tiles(t, n, k):
+    """Halves of whole groups of 8 rows and others, whole blocks of 64 columns and others."""
+    g = gen(n * 3 + k)
+    x, w = normal(g, (t, k), F16), normal(g, (n, k), F16, k ** -0.5)
+    close(cfa.linear(x, w, activation="silu", gated=True),
+          *linear64(x, w, None, "silu", True, None, F16))
+
+
 @pytest.mark.parametrize("t,n,k", [(1, 5, 3), (5, 33, 7), (19, 130, 1001), (150, 64, 250)])
 def test_linear_columns_off_the_grid(t, n, k):
     g = gen(k)
