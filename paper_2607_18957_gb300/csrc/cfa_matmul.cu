@@ -7,8 +7,8 @@
  * memory speed, ragged groups only shorten N, and a warp of the epilogue holds 32 neighbouring
  * output columns of one token, which it stores side by side.
  *
- * A CTA has six warps: four for the epilogue (each owns 32 lanes of tensor memory), one that asks
- * the TMA for tiles of 64 columns of w and x, and one that issues the products.  Tiles come in a ring
+ * A CTA has ten warps: eight for the epilogue (two take turns at each 32 lanes of tensor memory), one
+ * that asks the TMA for tiles of 64 columns of w and x, and one that issues the products.  Tiles come in a ring
  * of shared-memory stages; the accumulator is double buffered, so that the epilogue of one output
  * tile runs under the products of the next.  CTAs are persistent and take output tiles in turn.
  *
@@ -39,8 +39,9 @@
 
 namespace {
 
-constexpr int kThreads = 192;
-constexpr int kLoader = 4, kIssuer = 5;  /* warps; 0 to 3 are the epilogue's */
+constexpr int kThreads = 320;
+constexpr int kLoader = 8, kIssuer = 9;  /* warps; 0 to 7 are the epilogue's, two for each 32 lanes */
+constexpr int32_t kBatch = 16, kRound = 32; /* columns that one of the two takes at a time, and both */
 constexpr uint32_t kRows = 128;          /* weight rows per CTA, at most */
 constexpr uint32_t kDepth = 64;          /* columns of w and x per block: one 128-byte swizzle row */
 constexpr uint32_t kDeepBytes = 65536;   /* a stage takes more than one block up to this (of a pair,
@@ -630,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         }
         if (lane < 2) {
             mbar_init(acc_full + 8 * lane, 1);
-            mbar_init(acc_empty + 8 * lane, PAIR ? 8 : 4);
+            mbar_init(acc_empty + 8 * lane, PAIR ? 16 : 8);
         }
         if (lane == 0) {
             s->dead = 0;
@@ -898,7 +899,9 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             if (b) ph ^= 1;
             b ^= 1;
         };
-        const uint32_t lanes = s->tmem + ((uint32_t)warp * 32u << 16);
+        const int quarter = warp & 3; /* of the lanes; the warp's batches start at `from` */
+        const int32_t from = (warp >> 2) * kBatch;
+        const uint32_t lanes = s->tmem + ((uint32_t)quarter * 32u << 16);
         float *partial = reinterpret_cast<float *>(
             raw + (ring - smem_addr(raw)) + a.stages * stage); /* [bn][128], split > 1 */
         /* The first tile is gone through twice: first without a wait, without rows and so without
@@ -906,10 +909,10 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         bool dry = true;
         for (int32_t t = begin; t < total;) {
             const Tile o = tile_at(a, s, t, &group, features);
-            int64_t col = o.feature + (GATED ? warp * 16 + (lane >> 4) * 8 + (lane & 7)
-                                             : warp * 32 + lane);
+            int64_t col = o.feature + (GATED ? quarter * 16 + (lane >> 4) * 8 + (lane & 7)
+                                             : quarter * 32 + lane);
             if constexpr (PAIR) col += rank * per_cta;
-            if ((uint32_t)(warp * 32 + lane) >= a.fr) col = a.outs; /* a lane without a row */
+            if ((uint32_t)(quarter * 32 + lane) >= a.fr) col = a.outs; /* a lane without a row */
             float bias = 0.0f; /* of the lane's weight row */
             if (m.bias && col < a.outs) {
                 const int64_t at = col + (GATED && (lane & 8) ? m.bias_up : 0);
@@ -923,8 +926,9 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 c1 = min(o.rows, c0 + even);
             }
             Residual next; /* of the next batch, on its way since the one before */
-            if (!dry && c0 < c1)
-                fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c0, c1 - c0, col), next);
+            if (!dry && c0 + from < c1)
+                fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c0 + from, c1 - c0 - from, col),
+                                      next);
             /* the parts before the last are added up in tensor memory */
             bool more = false; /* a sum lies there */
             if (!dry) {
@@ -932,7 +936,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     ok = ok && mbar_wait(acc_full + 8 * buf, buf_phase, s);
                     ok = __all_sync(0xFFFFFFFFu, ok);
                     fence_after();
-                    for (int32_t c = 0; ok && c < o.rows; c += 16) {
+                    for (int32_t c = from; ok && c < o.rows; c += kRound) {
                         float v[16], u[16];
                         tmem_load(lanes + buf * a.acc_on + c, v);
                         if (more) {
@@ -953,20 +957,20 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             uint32_t sharers = 0;
             float v[16];
             if (sync_tiles) {
-                for (int32_t c = 0; ok && c < o.rows; c += 16) {
+                for (int32_t c = from; ok && c < o.rows; c += kRound) {
                     __syncwarp();
                     sum_load(src + c, sum + c, EXACT && more, v);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        partial[(c + j) * kRows + warp * 32 + lane] = v[j];
+                        partial[(c + j) * kRows + quarter * 32 + lane] = v[j];
                 }
                 if (!dry) cluster_sync();
                 sharers = dry ? 1u : 1u << share;
             }
             const bool few = c1 - c0 <= 4;
-            const uint32_t base = smem_addr(partial) + (uint32_t)(warp * 32 + lane) * 4u;
+            const uint32_t base = smem_addr(partial) + (uint32_t)(quarter * 32 + lane) * 4u;
             if (dry) c1 = min(c1, c0 + 1);
-            for (int32_t c = c0; ok && c < c1; c += 16) {
+            for (int32_t c = c0 + from; ok && c < c1; c += kRound) {
                 __syncwarp();
                 if (sharers == 0) {
                     sum_load(src + c, sum + c, EXACT && more, v);
@@ -991,8 +995,9 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 }
                 const Place p = place_of<GATED>(o.row + c, dry ? 0 : c1 - c, col);
                 const Residual r = next;
-                if (c + 16 < c1)
-                    fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c + 16, c1 - c - 16, col), next);
+                if (c + kRound < c1)
+                    fetch<GATED ? 8 : 16>(
+                        a, place_of<GATED>(o.row + c + kRound, c1 - c - kRound, col), next);
                 if (few) finish<GATED, 4>(a, v, p, bias, r);
                 else finish<GATED, 16>(a, v, p, bias, r);
             }
