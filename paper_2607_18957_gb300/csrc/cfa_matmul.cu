@@ -32,6 +32,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <math.h>
+
 #include <atomic>
 
 #include "cfa_device.cuh"
@@ -1144,11 +1146,11 @@ uint32_t deep_of(bool pair, uint32_t bn, uint32_t fr)
  * tile's products, but for the last.  (Bytes by turns: a last turn of few CTAs cannot draw what memory
  * gives.)
  * The constants are a fit to 13,800 timings: 182 sizes (1 to 4096 tokens, 256 to 28,672 rows, 1024 to
- * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.6 % longer than
- * the best of those on average, 27 % at the worst. */
+ * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.4 % longer than
+ * the best of those on average, 25 % at the worst. */
 double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int64_t rows, const Cut &c)
 {
-    const double kSplit[3] = {0.0, 2.1, 2.5}; /* one, two and four CTAs per tile */
+    const double kSplit[3] = {0.0, 1.84, 2.68}; /* one, two and four CTAs per tile */
     const uint32_t features = (c.pair ? 2 : 1) * (m->gated ? c.fr / 2 : c.fr);
     const int64_t n_tiles = (rows + c.bn - 1) / c.bn;
     const int64_t tiles = n_tiles * m->busy * ((outs + features - 1) / features);
@@ -1157,18 +1159,18 @@ double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int6
     const double blocks = (double)((steps + (1u << c.split) - 1) >> c.split);
     const double used = n_tiles == 1 ? (double)((rows + 15) / 16 * 16) : (double)c.bn;
     const double bytes = (double)(c.fr + (c.pair ? c.bn / 2 : c.bn)) * kRowBytes;
-    const double mma = used * (c.pair ? 0.00091 : 0.00102);
-    double step = (mma > 0.152 ? mma : 0.152) + 0.077 / deep_of(c.pair, c.bn, c.fr);
-    if (step < bytes / 127e3) step = bytes / 127e3;
+    const double mma = used * (c.pair ? 0.00078 : 0.0008);
+    double step = (mma > 0.149 ? mma : 0.149) + 0.09 / deep_of(c.pair, c.bn, c.fr);
+    if (step < bytes / 138e3) step = bytes / 138e3;
     const double tokens = (double)(rows < c.bn ? rows : c.bn);
-    const double epilogue = 0.025 * tokens / (1u << c.split), products = blocks * step;
+    const double epilogue = 0.018 * tokens / (1u << c.split), products = blocks * step;
     const double turn = (products > epilogue ? products : epilogue) + 0.6;
-    const double l2 = steps * (c.pair ? 2 : 1) * bytes / 18.1e6; /* per tile */
+    const double l2 = steps * (c.pair ? 2 : 1) * bytes / 19.9e6; /* per tile */
     const double mem = 2.0 * m->cols * ((double)m->w_rows * m->busy + (double)m->likely) / 6.6e6 /
                        (double)tiles;
     const double share = l2 > mem ? l2 : mem;
     const int64_t full = tiles / slots, left = tiles - full * slots;
-    double us = 2.8 + kSplit[c.split] + epilogue;
+    double us = 2.8 + kSplit[c.split] + (c.split ? 0.01 * tokens : 0.0) + epilogue;
     us += (double)full * (turn > (double)slots * share ? turn : (double)slots * share);
     if (left) us += turn > (double)left * share ? turn : (double)left * share;
     return us;
@@ -1186,8 +1188,10 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
         uint32_t last = 0;
         for (int64_t parts = (rows + 255) / 256; parts < (rows + 255) / 256 + 64; ++parts) {
             const int64_t even = (rows + parts - 1) / parts;
-            /* uneven groups: room for half as much again where that saves a second tile */
-            const int64_t room = busy > 1 && parts == 1 ? even + even / 2 : even;
+            /* uneven groups: room for two standard deviations of evenly drawn choices, so that most
+             * have one tile */
+            const int64_t room = busy > 1 && parts == 1 ? even + 2 + (int64_t)(2.0 * sqrt((double)even))
+                                                        : even;
             uint32_t bn = (uint32_t)((room + unit - 1) / unit * unit);
             if (bn > 256) bn = 256;
             if (pair && bn < 96) break;
@@ -1196,7 +1200,7 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
             last = bn;
             for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += 16) {
                 for (uint32_t split = 0; split < 3; ++split) {
-                    if (split && (pair || bn > 64 || steps < 4u << split)) break;
+                    if (split && (pair || bn > 128 || steps < 4u << split)) break;
                     const Cut c = {pair != 0, bn, fr, split};
                     const double us = estimate(m, outs, steps, sms, rows, c);
                     if (us < least * 0.995) {
