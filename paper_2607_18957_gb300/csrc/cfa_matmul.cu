@@ -1199,8 +1199,13 @@ Cut choose(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms)
             if (bn == last) continue;
             last = bn;
             for (uint32_t fr = pair ? kRows : 32; fr <= kRows; fr += 16) {
+                const uint32_t features = (pair ? 2 : 1) * (m->gated ? fr / 2 : fr);
+                const int64_t tiles = (rows + bn - 1) / bn * busy * ((outs + features - 1) / features);
                 for (uint32_t split = 0; split < 3; ++split) {
-                    if (split && (pair || bn > 128 || steps < 4u << split)) break;
+                    /* only while there is an SM for each: clusters go through their tiles one after the
+                     * other, and with more turns took 175 us where single CTAs take 109 */
+                    if (split && (pair || bn > 128 || steps < 4u << split || tiles << split > sms))
+                        break;
                     const Cut c = {pair != 0, bn, fr, split};
                     const double us = estimate(m, outs, steps, sms, rows, c);
                     if (us < least * 0.995) {
