@@ -739,6 +739,15 @@ cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
  */
 cfa_status cfa_op_status(void);
 
+/*
+ * Self-test of those waits, like cfa_selftest_wait_timeout: on `device` (-1 = current) one product is
+ * launched whose loader asks for nothing, so that its other waits run out.  *status_word receives the
+ * word that it left: 1 when every wait ended and the kernel returned; the record is cleared again.  The
+ * CUDA context stays usable.  Allocates and frees 17 KiB of device memory; synchronizes the device.
+ * Errors: CFA_ERR_INVAL (status_word NULL), CFA_ERR_CUDA.
+ */
+cfa_status cfa_selftest_op_timeout(int device, int *status_word);
+
 /* Zeroes the plan's checksum buffer on `stream`. */
 cfa_status cfa_reset_checksums(cfa_plan *plan, cfa_stream stream);
 

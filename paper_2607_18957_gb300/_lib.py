@@ -128,6 +128,7 @@ SIGNATURES = {
     "cfa_experts_workspace": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_experts_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_op_status": (ctypes.c_int, []),
+    "cfa_selftest_op_timeout": (ctypes.c_int, [ctypes.c_int, _P]),
 }
 
 _lib = None

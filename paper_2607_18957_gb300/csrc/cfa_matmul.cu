@@ -79,6 +79,8 @@ struct Args {
     uint32_t split;      /* log2 of the CTAs per output tile along the columns */
     uint32_t tmem_cols;
     uint32_t release;
+    uint32_t polls;      /* of a wait, before it gives up */
+    uint32_t lose;       /* self-test: the loader asks for nothing */
     uint32_t early_w;    /* w, and what tells the groups' rows, is there before the launch's wait */
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
@@ -90,6 +92,7 @@ struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem;
+    uint32_t polls;
     int dead;
     int32_t total;   /* output tiles */
     int32_t group[]; /* output tiles before each group's, and rows of x before each group's, in turn */
@@ -132,7 +135,8 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
 /* Waits for phase `parity`; false if the limit ran out here or in another warp of the CTA. */
 __device__ __noinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, Shared *s)
 {
-    for (uint32_t k = 0; k < kSpinLimit; ++k) {
+    const uint32_t polls = s->polls;
+    for (uint32_t k = 0; k < polls; ++k) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((k & 1023u) == 1023u && *(volatile int *)&s->dead) return false;
     }
@@ -637,6 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         }
         if (lane == 0) {
             s->dead = 0;
+            s->polls = a.polls;
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap[0]) : "memory");
         }
@@ -737,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             int32_t group = 0;
             asm volatile("fence.proxy.async.global;" ::: "memory");
             bool waited = !a.early_w;
-            for (int32_t t = begin; t < total; t += stride) {
+            for (int32_t t = a.lose ? total : begin; t < total; t += stride) {
                 const Tile o = tile_at(a, s, t, &group, features);
                 /* rows of x for this CTA: of a pair, each holds half of the columns in use */
                 uint32_t half = 0;
@@ -1251,6 +1256,8 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     a.outs = gated ? m->w_rows / 2 : m->w_rows;
     a.steps = (uint32_t)((m->cols + kDepth - 1) / kDepth);
     a.release = (uint32_t)release;
+    a.polls = m->lose ? 4096 : kSpinLimit;
+    a.lose = m->lose;
     a.early_w = m->w_ready && !pair;
     a.bn = cut.bn;
     a.fr = cut.fr;
@@ -1374,4 +1381,27 @@ cudaError_t cfa_matmul_status(int *word)
     const int zero = 0;
     const cudaError_t e = cudaMemcpyFromSymbol(word, g_status, sizeof *word);
     return e || !*word ? e : cudaMemcpyToSymbol(g_status, &zero, sizeof zero);
+}
+
+/* A product of one token whose loader asks for nothing, on the default stream: its waits run out after
+ * 4096 polls each.  *word receives the status word that this leaves, which is then cleared. */
+cudaError_t cfa_matmul_selftest(int *word)
+{
+    uint8_t *buf = nullptr;
+    const size_t w_bytes = 128 * 64 * 2, x_bytes = 64 * 2, y_bytes = 128 * 2;
+    cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&buf), w_bytes + x_bytes + y_bytes);
+    if (e) return e;
+    e = cudaMemset(buf, 0, w_bytes + x_bytes + y_bytes);
+    cfa_matmul m = {};
+    m.w = buf;
+    m.x = buf + w_bytes;
+    m.y = buf + w_bytes + x_bytes;
+    m.tokens = m.likely = m.n_groups = m.busy = m.lose = 1;
+    m.w_rows = m.y_stride = 128;
+    m.cols = m.x_stride = m.w_stride = 64;
+    if (!e) e = cfa_launch_matmul(&m, 0, 0, nullptr);
+    if (!e) e = cudaDeviceSynchronize();
+    if (!e) e = cfa_matmul_status(word);
+    const cudaError_t freed = cudaFree(buf);
+    return e ? e : freed;
 }

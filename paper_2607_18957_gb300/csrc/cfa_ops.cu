@@ -449,3 +449,16 @@ extern "C" cfa_status cfa_op_status(void)
                   word == 1 ? "a product's wait ran out: its result is not valid"
                             : "a product's wait ran out, and loads in flight did not end");
 }
+
+extern "C" cfa_status cfa_selftest_op_timeout(int device, int *status_word)
+{
+    if (!status_word) return refuse(CFA_ERR_INVAL, "cfa_selftest_op_timeout: NULL output");
+    int prev = 0;
+    cudaError_t e = cudaGetDevice(&prev);
+    if (!e && device >= 0) e = cudaSetDevice(device);
+    if (!e) {
+        e = cfa_matmul_selftest(status_word);
+        if (device >= 0) cudaSetDevice(prev);
+    }
+    return cuda_result("cfa_selftest_op_timeout", e);
+}

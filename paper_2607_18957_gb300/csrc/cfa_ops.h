@@ -37,6 +37,7 @@ typedef struct cfa_matmul {
     int64_t bias_up;  /* gated: where the up rows' bias starts, in elements */
     int32_t act, gated;
     int32_t exact;    /* 1: the sums are rounded as fp32 results are to be */
+    int32_t lose;     /* 1: self-test, the kernel's loads are not issued */
     int32_t busy;     /* groups that can hold rows at all (host's bound) */
     int64_t likely;   /* rows to expect in all groups, at most `tokens` */
 } cfa_matmul;
@@ -56,6 +57,7 @@ typedef struct cfa_sort {
 cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream);
 /* The current device's word of waits that ran out (0: none), cleared. */
 cudaError_t cfa_matmul_status(int *word);
+cudaError_t cfa_matmul_selftest(int *word);
 cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream);
 /* Rows of hist that the sort of so many pairs needs. */
 int64_t cfa_sort_blocks(int64_t pairs);

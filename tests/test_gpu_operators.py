@@ -487,6 +487,43 @@ def test_experts_repeat_bit_for_bit_in_place_and_in_a_graph():
     assert torch.equal(z, cfa.experts(x, ids, w, w13, w2))
 
 
+@pytest.mark.parametrize("t,e,top_k", [(5000, 4, 4), (4100, 16, 8), (300, 1024, 8)])
+def test_experts_of_many_pairs_and_of_many_experts(t, e, top_k):
+    """More pairs than one block of the sort counts for itself, and the most experts there can be."""
+    x, ids, w, w13, w2 = expert_operands(t, 64, 32, e, top_k, e, BF16, t + e)
+    close(cfa.experts(x, ids, w, w13, w2), *experts64(x, ids, w, w13, w2, "silu", 0, None))
+
+
+def test_offsets_past_32_bits():
+    """A result and stacked weights of more than 2^31 elements."""
+    g = gen(31)
+    x, w = normal(g, (65600, 64), BF16), normal(g, (32800, 64), BF16, 0.125)
+    y = cfa.linear(x, w)
+    for rows in (slice(0, 40), slice(65472, 65600)):
+        close(y[rows], *linear64(x[rows], w, None, "none", False, None, BF16))
+    del y
+    w13 = torch.empty(20, 28672, 4096, dtype=BF16, device="cuda")  # the others are never read
+    w2 = torch.empty(20, 4096, 14336, dtype=BF16, device="cuda")
+    w13[19] = normal(g, (28672, 4096), BF16, 4096 ** -0.5)
+    w2[19] = normal(g, (4096, 14336), BF16, 14336 ** -0.5)
+    x = normal(g, (9, 4096), BF16)
+    ids = torch.full((9, 1), 19, dtype=torch.int32, device="cuda")
+    weights = torch.rand(9, 1, generator=g, device="cuda")
+    close(cfa.experts(x, ids, weights, w13, w2),
+          *experts64(x, ids - 19, weights, w13[19:], w2[19:], "silu", 0, None))
+
+
+def test_a_wait_that_runs_out_ends_and_is_reported():
+    import ctypes
+    from paper_2607_18957_gb300 import _lib
+    word = ctypes.c_int(-1)
+    assert _lib.load().cfa_selftest_op_timeout(-1, ctypes.byref(word)) == 0
+    assert word.value == 1
+    cfa.op_status()  # cleared
+    x = normal(gen(1), (3, 64), BF16)  # and the context is as usable as before
+    close(cfa.linear(x, x), *linear64(x, x, None, "none", False, None, BF16))
+
+
 # ---- refusals -----------------------------------------------------------------------------------
 
 def test_python_refusals():

@@ -136,6 +136,10 @@ def test_null_arguments(lib):
         assert f(None, None) == INVAL
 
 
+def test_selftest_refuses_a_null_output(lib):
+    assert lib.cfa_selftest_op_timeout(-1, None) == INVAL
+
+
 def test_no_tokens_need_no_pointers(lib):
     assert lib.cfa_linear_async(linear(tokens=0, x=0, w=0, y=0), None) == 0
     assert lib.cfa_route_async(route(tokens=0, logits=0, weights=0, ids=0), None) == 0
