@@ -8,9 +8,9 @@
  * output columns of one token, which it stores side by side.
  *
  * A CTA has ten warps: eight for the epilogue (two take turns at each 32 lanes of tensor memory), one
- * that asks the TMA for tiles of 64 columns of w and x, and one that issues the products.  Tiles come in a ring
- * of shared-memory stages; the accumulator is double buffered, so that the epilogue of one output
- * tile runs under the products of the next.  CTAs are persistent and take output tiles in turn.
+ * that asks the TMA for tiles of 64 columns of w and x, and one that issues the products.  Tiles come
+ * in a ring of shared-memory stages; the accumulator is double buffered, so that the epilogue of one
+ * output tile runs under the products of the next.  CTAs are persistent and take output tiles in turn.
  *
  * PAIR: two CTAs work on one tile of 256 weight rows (cta_group::2): each holds half of the rows and
  * half of the tokens, so each operand is loaded once per pair.
@@ -18,11 +18,31 @@
  * the partial sums meet in shared memory and are added in the order of the CTAs.
  * Gated: the stage holds 8 gate rows, then the 8 up rows that belong to them, and so on, so both
  * values of an output lie in one warp, 8 lanes apart.
+ * Of these, and of the heights of the tiles, `choose` takes those that a fit to timings puts first.
+ *
+ * What bounds it, and what it takes on one GB300 (bf16, weights from memory, not from L2):
+ *   many tokens: the tensor cores.  2048 tokens, gated 28,672 x 4096: the tensor pipe is active in 95 %
+ *     of the cycles, 4096 tokens take 480 us (2.0 PFLOP/s) in a burst and 550 (1.75) under the power
+ *     limit, as cuBLAS does.
+ *   few tokens: memory, 128 weight rows a stage and 150 to 200 KiB a CTA on their way.  One token,
+ *     gated 28,672 x 4096 (235 MB): 37.5 us (6.3 TB/s); 57,344 x 4096: 70 us (6.7 TB/s).
+ *   few tokens and a small weight: start and end.  A launch of one block takes 3.0 us, 50 MB
+ *     12.4 us (7.4 at the rate of memory), 117 MB 22 us (17).
+ * What made the difference, in the order it was found: stores of pairs of columns without a branch
+ * between them (1078 -> 562 us on 4096 x 28,672 x 4096); one elected lane for loads and for products,
+ * which lets the compiler keep their operands in uniform registers (0.31 -> 0.18 us a block), and a
+ * look at the next stage's barrier before the products of this one (0.25 -> 0.21); one load for all
+ * blocks of a stage instead of one or, gated, four per block (627 -> 447 us on the gate/up product);
+ * loads before the tensor memory is there and the epilogue's code warmed up under them (4.0 -> 3.0 us
+ * for one block); eight epilogue warps instead of four (88 -> 65 us on 2247 tokens, gated 16,384 x
+ * 1280 with SiLU).
  *
  * exact: the tensor cores add in fp32, but cut each sum's last bits off where IEEE addition rounds, so
  * that an fp32 result is off by half a unit in the last place per addition in the same direction
  * (1e-6 after 64 of them: 1024 columns).  For fp32 results the accumulator therefore takes parts of
- * 256 columns, which the epilogue adds with rounding in a third place of tensor memory.
+ * 256 columns, which the epilogue adds with rounding in a third place of tensor memory (2.3e-7 at 4096
+ * columns, as a product in plain fp32 has).  Results of 16 bits, whose own rounding is a thousand times
+ * that, are summed in one go.
  *
  * Every wait has a limit.  One that runs out sets the status word that cfa_op_status reads; its CTA
  * then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor

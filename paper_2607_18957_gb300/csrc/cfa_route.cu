@@ -5,9 +5,11 @@
  * the best of its own, and only the lane that has just given its best looks for the next one.  Equal
  * keys go to the lowest index.
  *
- * Up to a few thousand tokens this is bound by the launch and by the chain of loads, exponentials and
- * top_k warp reductions of one token; the bytes (4 KiB read and written per token of 256 fp32 logits
- * at the most) would take a tenth of that.
+ * Bound by the launch and by the chain of loads, exponentials and top_k warp reductions of one token,
+ * and beyond some thousand tokens by the instructions of that chain; the bytes would take a tenth.
+ * One token over 8 experts 1.5 us, 4099 tokens over 256 experts in 8 groups with a bias 10.7 us (0.42
+ * TB/s), 10,801 tokens over 128 experts 9.6 us.  Every 32nd logit to a lane and group ranks by one lane
+ * per group took 13.8 us on the second without its bias, 8.1 this way.
  */
 #include <math.h>
 
