@@ -2,14 +2,20 @@
  * Choice of experts.  One warp a token: each lane holds R neighbouring logits, so that a group of
  * experts lies in a few neighbouring lanes.  The top_k come out one at a time as the warp's largest
  * key, a key being the fp32 value mapped onto unsigned integers of the same order; every lane keeps
- * the best of its own, and only the lane that has just given its best looks for the next one.  Equal
- * keys go to the lowest index.
+ * the best of its own.  Equal keys go to the lowest index.
+ *
+ * The lane that has just given its best needs the next one.  With few logits per lane it goes through
+ * them alone; from kShared on its keys, which lie in shared memory, go one to a lane and the warp takes
+ * their largest: the others would wait for that lane's loop anyway (4096 tokens over 128 experts, eight
+ * choices: 4.9 -> 4.2 us; 256 experts 7.3 -> 5.3).
  *
  * Bound by the launch and by the chain of loads, exponentials and top_k warp reductions of one token,
  * and beyond some thousand tokens by the instructions of that chain; the bytes would take a tenth.
- * One token over 8 experts 1.5 us, 4099 tokens over 256 experts in 8 groups with a bias 10.7 us (0.42
- * TB/s), 10,801 tokens over 128 experts 9.6 us.  Every 32nd logit to a lane and group ranks by one lane
- * per group took 13.8 us on the second without its bias, 8.1 this way.
+ * One token over 8 experts 1.5 us beside the launch, 4099 tokens over 256 experts in 8 groups with a
+ * bias 6.7 us, 16,384 tokens over 128 experts 10.0 us.  What made the difference there: neighbouring
+ * logits in a lane instead of every 32nd (13.8 -> 8.1 us without a bias), the bias through L1 (3.2 us
+ * less), and a warp brought together again before its shuffles (1.1 us less: lanes that a branch has
+ * parted trade values one by one).
  */
 #include <math.h>
 
@@ -146,21 +152,64 @@ __device__ __forceinline__ void keep_groups(const cfa_route_args &a, float (&key
     }
 }
 
+/* The bias comes through L1, behind a fence that clears what L1 held before the launch's wait was over:
+ * every warp reads the same few lines, which L2 hands out at 64 bytes a clock. */
+template <int R>
+__device__ __forceinline__ void load_bias(const float *bias, int first, int n, float (&b)[R])
+{
+    if (R % 4 == 0 && n == 32 * R && ((uintptr_t)bias & 15u) == 0) {
+#pragma unroll
+        for (int r = 0; r + 3 < R; r += 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(bias + first + r);
+            b[r] = q.x;
+            b[r + 1] = q.y;
+            b[r + 2] = q.z;
+            b[r + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) b[r] = first + r < n ? bias[first + r] : 0.0f;
+    }
+}
+
+/* The lane's R values side by side in shared memory. */
+template <int R, typename T> __device__ __forceinline__ void put(T *to, const T (&v)[R])
+{
+    if constexpr (R % 4 == 0) {
+        struct alignas(16) Four {
+            T v[4];
+        };
+#pragma unroll
+        for (int r = 0; r < R; r += 4)
+            *reinterpret_cast<Four *>(to + r) = {v[r], v[r + 1], v[r + 2], v[r + 3]};
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) to[r] = v[r];
+    }
+}
+
+constexpr int kShared = 4; /* from so many logits per lane on, keys and logits lie in shared memory too */
+
 /* R: logits per lane. */
 template <int R>
 __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_args a)
 {
-    extern __shared__ float s_key[]; /* [warps][experts], with groups only */
+    /* of each warp: [32 R] keys and [32 R] logits from kShared on; below, [experts] keys with groups */
+    extern __shared__ __align__(16) uint32_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t *const s_key = smem + warp * (R >= kShared ? 64 * R : a.experts);
+    float *const s_logit = reinterpret_cast<float *>(s_key + 32 * R);
     const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.bias) __threadfence();
     if (t >= a.tokens) return;
 
     const int es = a.dtype == CFA_DTYPE_F32 ? 4 : 2;
     const uint8_t *row = static_cast<const uint8_t *>(a.logits) + t * a.logits_stride * es;
     const bool vec = a.experts == 32 * R && ((uintptr_t)row & (uintptr_t)(4 * es - 1)) == 0;
-    float v[R], key[R];
+    float v[R], key[R], b[R];
     load<R>(a.dtype, a.experts, row, lane * R, vec, v);
+    if (a.bias) load_bias<R>(a.bias, lane * R, a.experts, b);
     float top = -INFINITY;
     bool nan = false;
 #pragma unroll
@@ -181,21 +230,24 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
             norm = nan ? NAN : warp_add(sum);
         }
     }
-    if (a.bias) {
-        float b[R];
-        load<R>(CFA_DTYPE_F32, a.experts, a.bias, lane * R,
-                a.experts == 32 * R && ((uintptr_t)a.bias & 15u) == 0, b);
+    if (!softmax) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            key[r] = (softmax ? expf(v[r] - top) / norm : 1.0f / (1.0f + expf(-v[r]))) + b[r];
+        for (int r = 0; r < R; ++r) key[r] = 1.0f / (1.0f + expf(-v[r]));
+    } else if (a.bias) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = expf(v[r] - top) / norm;
     } else {
 #pragma unroll
-        for (int r = 0; r < R; ++r) key[r] = softmax ? v[r] : 1.0f / (1.0f + expf(-v[r]));
+        for (int r = 0; r < R; ++r) key[r] = v[r];
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] += b[r];
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (!(v[r] > -INFINITY)) key[r] = -INFINITY;
-    if (a.groups > 1) keep_groups<R>(a, key, s_key + warp * a.experts, lane, !softmax);
+    if (a.groups > 1) keep_groups<R>(a, key, reinterpret_cast<float *>(s_key), lane, !softmax);
 
     uint32_t k[R], best = 0; /* the lane's best key, its place and its logit */
     int at = 0;
@@ -211,10 +263,31 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
     }
     float chosen = -INFINITY; /* lane j: the logit of choice j */
     int id = -1;
+    if constexpr (R >= kShared) {
+        __syncwarp();
+        put<R>(s_key + lane * R, k);
+        put<R>(s_logit + lane * R, v);
+        __syncwarp();
+    }
     for (int j = 0; j < a.top_k; ++j) {
         const uint32_t most = __reduce_max_sync(kAll, best);
         if (most == 0) break; /* nothing left to choose */
         const int win = __ffs(__ballot_sync(kAll, best == most)) - 1;
+        if constexpr (R >= kShared) {
+            /* the winner's keys, one to a lane, which alone reads and writes it: the best that is left */
+            const int gone = __shfl_sync(kAll, at, win);
+            if (lane == j) id = win * R + gone;
+            const int own = win * R + (lane < R ? lane : 0);
+            uint32_t left = lane < R && lane != gone ? s_key[own] : 0;
+            if (lane == gone) s_key[own] = 0;
+            const uint32_t next = __reduce_max_sync(kAll, left);
+            const int place = __ffs(__ballot_sync(kAll, left == next)) - 1;
+            if (lane == win) {
+                best = next;
+                at = place;
+            }
+            continue;
+        }
         const int e = __shfl_sync(kAll, lane * R + at, win);
         const float logit = __shfl_sync(kAll, z, win);
         if (lane == j) {
@@ -235,6 +308,9 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
             }
         }
     }
+
+    if constexpr (R >= kShared) chosen = id >= 0 ? s_logit[id < 0 ? 0 : id] : -INFINITY;
+    __syncwarp(); /* the lanes together, for the shuffles below */
 
     float w = 0.0f;
     if (softmax) {
@@ -261,7 +337,8 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
 template <int R> cudaError_t launch(const cfa_route_args &a, cudaStream_t stream)
 {
     const unsigned grid = (unsigned)((a.tokens + kWarps - 1) / kWarps);
-    const size_t smem = a.groups > 1 ? sizeof(float) * kWarps * a.experts : 0;
+    const size_t smem = sizeof(float) * kWarps *
+                        (R >= kShared ? 64 * R : a.groups > 1 ? a.experts : 0);
     cfa_launch_ctl ctl = {};
     ctl.flags = CFA_LAUNCH_EARLY;
     void *p[] = {const_cast<cfa_route_args *>(&a)};
