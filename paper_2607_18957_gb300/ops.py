@@ -26,7 +26,7 @@ torch = None
 _CODE = None    # torch dtype -> CFA_DTYPE_*
 _DTYPE = None   # dtype name -> torch dtype
 _lib_c = None
-_EXPERTS_BYTES = {}  # workspace bytes of experts by its sizes
+_LINEAR_BYTES, _EXPERTS_BYTES = {}, {}  # workspace bytes by a call's sizes
 _raw_stream = _device = _grad = None
 
 
@@ -198,12 +198,19 @@ def linear(x, weight, bias=None, *, activation="none", gated=False, residual=Non
         rp = residual.data_ptr()
     xp, wp = x.data_ptr(), weight.data_ptr()
     if (xp | wp | (xs | ws) * 2) & 15:
-        need = _lib.ctypes.c_uint64()
-        _check(_lib_c.cfa_linear_workspace(
-            _LINEAR.pack(xp, wp, bp, rp, 0, 0, 0, t, n, k, xs, ws, rs, os_, code, bc, code, act,
-                         GATED if gated else 0, 0), _lib.ctypes.byref(need)))
-        if need.value:
-            workspace = _workspace(workspace, need.value, x.device)
+        sizes = (t, n, k, xs, ws, xp & 15, wp & 15, gated)
+        need = _LINEAR_BYTES.get(sizes)  # by the sizes and the alignment alone
+        if need is None:
+            size = _lib.ctypes.c_uint64()
+            _check(_lib_c.cfa_linear_workspace(
+                _LINEAR.pack(xp, wp, bp, rp, 0, 0, 0, t, n, k, xs, ws, rs, os_, code, bc, code,
+                             act, GATED if gated else 0, 0), _lib.ctypes.byref(size)))
+            if len(_LINEAR_BYTES) >= 1024:
+                _LINEAR_BYTES.clear()
+            need = _LINEAR_BYTES[sizes] = size.value
+        size = 0
+        if need:
+            workspace = _workspace(workspace, need, x.device)
             buf, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     st = _lib_c.cfa_linear_async(
         _LINEAR.pack(xp, wp, bp, rp, out.data_ptr(), buf, size, t, n, k, xs, ws, rs, os_, code, bc,
