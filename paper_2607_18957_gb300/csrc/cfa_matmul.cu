@@ -35,7 +35,10 @@
  * blocks of a stage instead of one or, gated, four per block (627 -> 447 us on the gate/up product);
  * loads before the tensor memory is there and the epilogue's code warmed up under them (4.0 -> 3.0 us
  * for one block); eight epilogue warps instead of four (88 -> 65 us on 2247 tokens, gated 16,384 x
- * 1280 with SiLU).
+ * 1280 with SiLU); tiles turned round in shared memory and stored 16 bytes at a time, or 4 where rows
+ * lie off that grid, by kernels that hold no other way to store (62 -> 56 there; 2206 tokens x 6359 x
+ * 392 with a residual 81 -> 37, x 6360 42 -> 27); rings of three stages or more beside a cluster's sums
+ * (256 tokens x 4096 x 14,336 47 -> 37).
  *
  * exact: the tensor cores add in fp32, but cut each sum's last bits off where IEEE addition rounds, so
  * that an fp32 result is off by half a unit in the last place per addition in the same direction
@@ -77,6 +80,19 @@ constexpr uint32_t kBand = 16;           /* token tiles that share a weight tile
 constexpr uint32_t kBoxes = 4;           /* heights of the loads of x */
 constexpr uint32_t kSpinLimit = 1u << 20;    /* polls of a wait */
 constexpr uint32_t kDrainLimit = 1u << 16;   /* polls for loads in flight after one ran out */
+
+/* What a kernel is made for.  An epilogue that holds what other products need (other ways to store,
+ * functions that are not called) no longer fits the instruction caches: with all in one kernel, 2206
+ * tokens x 6360 x 64 took 30 us where 18 do. */
+enum : int {
+    kPair = 1,
+    kGated = 2,
+    kF32 = 4,     /* y */
+    kExact = 8,   /* see above; with kF32 */
+    kWide = 16,   /* tiles are stored by way of shared memory, 16 bytes at a time .. */
+    kNarrow = 32, /* .. or 4, y or the residual being off the 16-byte grid; neither: from registers */
+    kCurves = 64, /* the activations with erf and tanh too */
+};
 
 struct Args {
     CUtensorMap wmap, xmap[kBoxes]; /* a stage's blocks of w and of x at once, whole blocks only */
@@ -352,8 +368,15 @@ __device__ __forceinline__ float value(const void *p, int64_t i, int f16)
 __device__ __forceinline__ float value(const float *p, int64_t i) { return __ldcg(p + i); }
 
 /* One switch for a batch of values, so that they run side by side. */
-template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
+template <int KIND, int N> __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
+    if (!(KIND & kCurves) && act != CFA_ACT_SILU) {
+        if (act == CFA_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+        }
+        return;
+    }
     switch (act) {
     case CFA_ACT_RELU:
 #pragma unroll
@@ -371,7 +394,10 @@ template <int N> __device__ __forceinline__ void activate(float (&v)[N], int act
         break;
     case CFA_ACT_SILU:
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
+        for (int i = 0; i < N; ++i)
+            /* both fast forms are off by some units in the last place of fp32: the quotient by two,
+             * which fp32 results may be, the exponential by |v|, which 16 bits do not show */
+            v[i] = __fdividef(v[i], 1.0f + (KIND & kExact ? expf(-v[i]) : __expf(-v[i])));
         break;
     default: break;
     }
@@ -464,7 +490,7 @@ struct Residual {
     uint32_t lo[16], hi[8]; /* pairs of fp32 take both, one of a pair at a time */
 };
 
-template <int N>
+template <bool F32, int N>
 __device__ __forceinline__ void fetch(const Args &a, const Place &p, Residual &r)
 {
     const cfa_matmul &m = a.m;
@@ -476,7 +502,7 @@ __device__ __forceinline__ void fetch(const Args &a, const Place &p, Residual &r
         for (int i = 0; i < N / 2; ++i) {
             if (first + 2 * i * p.step >= p.n) continue;
             const int64_t from = at + 2 * i * p.step * m.r_stride;
-            if (m.y_f32) {
+            if (F32) {
                 const uint2 v = __ldcg(reinterpret_cast<const uint2 *>(
                     static_cast<const float *>(m.residual) + from));
                 r.lo[i] = v.x;
@@ -491,13 +517,13 @@ __device__ __forceinline__ void fetch(const Args &a, const Place &p, Residual &r
         for (int i = 0; i < N; ++i) {
             if (i * p.step >= p.n) continue;
             const int64_t from = (p.row + i * p.step) * m.r_stride + p.col;
-            if (m.y_f32) r.lo[i] = __ldcg(static_cast<const uint32_t *>(m.residual) + from);
+            if (F32) r.lo[i] = __ldcg(static_cast<const uint32_t *>(m.residual) + from);
             else r.lo[i] = __ldcg(static_cast<const unsigned short *>(m.residual) + from);
         }
     }
 }
 
-template <int N>
+template <bool F32, int N>
 __device__ __forceinline__ void store(const Args &a, float (&v)[N], const Place &p, const Residual &r)
 {
     const cfa_matmul &m = a.m;
@@ -514,7 +540,7 @@ __device__ __forceinline__ void store(const Args &a, float (&v)[N], const Place 
         if (m.residual) {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                const float2 x = m.y_f32 ? make_float2(__uint_as_float(r.lo[i]),
+                const float2 x = F32 ? make_float2(__uint_as_float(r.lo[i]),
                                                        __uint_as_float(r.hi[i]))
                                          : unpack(r.lo[i], m.f16);
                 o[i].x += x.x;
@@ -522,7 +548,7 @@ __device__ __forceinline__ void store(const Args &a, float (&v)[N], const Place 
             }
         }
         const int64_t at = (p.row + first) * m.y_stride + p.col - odd;
-        if (m.y_f32) {
+        if (F32) {
             float *to = static_cast<float *>(m.y) + at;
 #pragma unroll
             for (int i = 0; i < N / 2; ++i)
@@ -544,8 +570,8 @@ __device__ __forceinline__ void store(const Args &a, float (&v)[N], const Place 
             float x = v[i];
             const int64_t to = at + i * p.step * m.y_stride;
             if (m.residual)
-                x += m.y_f32 ? __uint_as_float(r.lo[i]) : unpack(r.lo[i], m.f16).x;
-            if (m.y_f32) static_cast<float *>(m.y)[to] = x;
+                x += F32 ? __uint_as_float(r.lo[i]) : unpack(r.lo[i], m.f16).x;
+            if (F32) static_cast<float *>(m.y)[to] = x;
             else static_cast<uint16_t *>(m.y)[to] = (uint16_t)pack(x, 0.0f, m.f16);
         }
     }
@@ -561,15 +587,16 @@ __device__ __forceinline__ Place place_of(int64_t row, int n, int64_t col)
     return {row + upper, col, GATED ? 2 : 1, n - upper};
 }
 
-template <bool GATED, int N>
+template <int KIND, int N>
 __device__ __forceinline__ void finish(const Args &a, float (&all)[16], const Place &p, float bias,
                                        const Residual &r)
 {
+    constexpr bool F32 = KIND & kF32;
     const cfa_matmul &m = a.m;
     float v[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = m.bias ? all[j] + bias : all[j];
-    if constexpr (GATED) {
+    if constexpr ((KIND & kGated) != 0) {
         const bool upper = threadIdx.x & 8;
         float gate[N / 2], up[N / 2];
 #pragma unroll
@@ -578,13 +605,251 @@ __device__ __forceinline__ void finish(const Args &a, float (&all)[16], const Pl
             gate[j] = upper ? got : v[2 * j];
             up[j] = upper ? v[2 * j + 1] : got;
         }
-        activate(gate, m.act);
+        activate<KIND>(gate, m.act);
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) gate[j] *= up[j];
-        store<N / 2>(a, gate, p, r);
+        store<F32, N / 2>(a, gate, p, r);
     } else {
-        activate(v, m.act);
-        store<N>(a, v, p, r);
+        activate<KIND>(v, m.act);
+        store<F32, N>(a, v, p, r);
+    }
+}
+
+/* A batch of 16 tokens by way of shared memory, in which token j's sums of the warp's 32 weight rows lie
+ * side by side from word j * kStageRow on (four words more than they are, so that 16-byte reads of
+ * neighbouring tokens meet different banks).  The registers hold 16 tokens of one column: stored from
+ * there, each store writes 64 bytes of two tokens at most, after an exchange with the next lane.  A lane takes 16 bytes of y at a time: 8 columns of 2 bytes
+ * or 4 of 4, of the tokens lane / CHUNKS + i * STEP. */
+constexpr int kStageRow = 36;
+constexpr uint32_t kStageBytes = 8 * kBatch * kStageRow * 4;
+
+template <bool GATED, bool F32> struct Wide {
+    static constexpr int COLS = F32 ? 4 : 8, CHUNKS = (GATED ? 16 : 32) / COLS;
+    static constexpr int ITEMS = kBatch * CHUNKS / 32, STEP = 32 / CHUNKS;
+};
+
+__device__ __forceinline__ uint4 pack16(const float (&v)[8], int f16)
+{
+    uint32_t o[4];
+    if (f16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = pack(v[2 * i], v[2 * i + 1], 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = pack(v[2 * i], v[2 * i + 1], 0);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ uint4 pack16(const float (&v)[4], int)
+{
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                      __float_as_uint(v[3]));
+}
+__device__ __forceinline__ void add16(float (&v)[8], uint4 r, int f16)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    if (f16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 x = unpack(w[i], 1);
+            v[2 * i] += x.x;
+            v[2 * i + 1] += x.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 x = unpack(w[i], 0);
+            v[2 * i] += x.x;
+            v[2 * i + 1] += x.y;
+        }
+    }
+}
+__device__ __forceinline__ void add16(float (&v)[4], uint4 r, int)
+{
+    v[0] += __uint_as_float(r.x);
+    v[1] += __uint_as_float(r.y);
+    v[2] += __uint_as_float(r.z);
+    v[3] += __uint_as_float(r.w);
+}
+
+/* The residual of a batch of n tokens from `row` on, in columns [col, limit) of which the lane takes its
+ * chunk. */
+template <bool GATED, bool F32>
+__device__ __forceinline__ void fetch_wide(const Args &a, int64_t row, int n, int64_t col, int64_t limit,
+                                           uint4 (&r)[4])
+{
+    typedef Wide<GATED, F32> W;
+    const int lane = threadIdx.x & 31, token = lane / W::CHUNKS;
+    col += lane % W::CHUNKS * W::COLS;
+    if (!a.m.residual || col + W::COLS > limit) return;
+    const uint8_t *from = static_cast<const uint8_t *>(a.m.residual) +
+                          ((row + token) * a.m.r_stride + col) * (16 / W::COLS);
+#pragma unroll
+    for (int i = 0; i < W::ITEMS; ++i)
+        if (token + i * W::STEP < n)
+            r[i] = __ldcg(reinterpret_cast<const uint4 *>(
+                from + i * W::STEP * a.m.r_stride * (16 / W::COLS)));
+}
+
+template <int KIND>
+__device__ __forceinline__ void finish_wide(const Args &a, const float *stage, int64_t row, int n,
+                                            int64_t col, int64_t limit, const uint4 (&r)[4])
+{
+    constexpr bool GATED = KIND & kGated, F32 = KIND & kF32;
+    typedef Wide<GATED, F32> W;
+    const cfa_matmul &m = a.m;
+    const int lane = threadIdx.x & 31, token = lane / W::CHUNKS, at = lane % W::CHUNKS * W::COLS;
+    float v[W::ITEMS][W::COLS];
+#pragma unroll
+    for (int i = 0; i < W::ITEMS; ++i) {
+        /* gated: 8 gate rows, then their 8 up rows */
+        const float *from = stage + (token + i * W::STEP) * kStageRow +
+                            (GATED ? at / 8 * 16 + at % 8 : at);
+        float up[W::COLS];
+#pragma unroll
+        for (int j = 0; j < W::COLS; j += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(from + j);
+            v[i][j] = x.x;
+            v[i][j + 1] = x.y;
+            v[i][j + 2] = x.z;
+            v[i][j + 3] = x.w;
+            if constexpr (GATED) {
+                const float4 u = *reinterpret_cast<const float4 *>(from + j + 8);
+                up[j] = u.x;
+                up[j + 1] = u.y;
+                up[j + 2] = u.z;
+                up[j + 3] = u.w;
+            }
+        }
+        activate<KIND>(v[i], m.act);
+        if constexpr (GATED) {
+#pragma unroll
+            for (int j = 0; j < W::COLS; ++j) v[i][j] *= up[j];
+        }
+    }
+    col += at;
+    const int64_t first = (row + token) * m.y_stride + col;
+    if (col + W::COLS <= limit) {
+        uint8_t *to = static_cast<uint8_t *>(m.y) + first * (16 / W::COLS);
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i) {
+            if (m.residual) add16(v[i], r[i], m.f16);
+            const uint4 o = pack16(v[i], m.f16);
+            if (token + i * W::STEP < n)
+                *reinterpret_cast<uint4 *>(to + i * W::STEP * m.y_stride * (16 / W::COLS)) = o;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i)
+#pragma unroll
+            for (int j = 0; j < W::COLS; ++j) {
+                if (token + i * W::STEP >= n || col + j >= limit) continue;
+                const int64_t to = first + i * W::STEP * m.y_stride + j;
+                float x = v[i][j];
+                if (m.residual) {
+                    const int64_t from = (row + token + i * W::STEP) * m.r_stride + col + j;
+                    x += F32 ? value(static_cast<const float *>(m.residual), from)
+                             : value(m.residual, from, m.f16);
+                }
+                if (F32) static_cast<float *>(m.y)[to] = x;
+                else static_cast<uint16_t *>(m.y)[to] = (uint16_t)pack(x, 0.0f, m.f16);
+            }
+    }
+}
+
+/* The same where y or the residual is off the 16-byte grid, for y of 2 bytes: a lane takes 4 bytes of y
+ * of the tokens lane / WORDS + i * STEP.  Where a token's columns start between two words, its first
+ * lane stores the first and the last of them by themselves. */
+template <bool GATED> struct Narrow {
+    static constexpr int COLS = GATED ? 16 : 32, WORDS = COLS / 2, STEP = 32 / WORDS;
+    static constexpr int ITEMS = kBatch / STEP;
+};
+
+/* The two columns of the lane in row `row` of y, and in every second row from there: of them the first
+ * lies at a word's address, unless they are the first lane's two of a row that starts between words. */
+template <bool GATED>
+__device__ __forceinline__ void narrow_columns(const Args &a, int64_t row, int64_t col, int &c0, int &c1)
+{
+    const int word = (int)(threadIdx.x & 31) % Narrow<GATED>::WORDS;
+    const int odd = (int)(((uintptr_t)a.m.y >> 1) + row * a.m.y_stride + col) & 1;
+    c1 = 2 * word + 1 - odd;
+    c0 = c1 ? c1 - 1 : Narrow<GATED>::COLS - 1;
+}
+
+template <bool GATED>
+__device__ __forceinline__ void fetch_narrow(const Args &a, int64_t row, int n, int64_t col,
+                                             int64_t limit, uint32_t (&r)[16])
+{
+    typedef Narrow<GATED> W;
+    if (!a.m.residual) return;
+    const int token = (int)(threadIdx.x & 31) / W::WORDS;
+    int c0, c1;
+    narrow_columns<GATED>(a, row + token, col, c0, c1);
+    const unsigned short *from = static_cast<const unsigned short *>(a.m.residual) +
+                                 (row + token) * a.m.r_stride + col;
+    const int in0 = col + c0 < limit ? n - token : 0, in1 = col + c1 < limit ? n - token : 0;
+#pragma unroll
+    for (int i = 0; i < W::ITEMS; ++i) {
+        if (i * W::STEP < in0) r[2 * i] = __ldcg(from + c0);
+        if (i * W::STEP < in1) r[2 * i + 1] = __ldcg(from + c1);
+        from += W::STEP * a.m.r_stride;
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ void finish_narrow(const Args &a, const float *stage, int64_t row, int n,
+                                              int64_t col, int64_t limit, const uint32_t (&r)[16])
+{
+    constexpr bool GATED = KIND & kGated;
+    typedef Narrow<GATED> W;
+    const cfa_matmul &m = a.m;
+    const int token = (int)(threadIdx.x & 31) / W::WORDS;
+    int c0, c1;
+    narrow_columns<GATED>(a, row + token, col, c0, c1);
+    float v[2 * W::ITEMS], up[GATED ? 2 * W::ITEMS : 1];
+    /* gated: 8 gate rows, then their 8 up rows */
+    const float *const from0 = stage + token * kStageRow + (GATED ? c0 + (c0 & 8) : c0);
+    const float *const from1 = stage + token * kStageRow + (GATED ? c1 + (c1 & 8) : c1);
+#pragma unroll
+    for (int i = 0; i < W::ITEMS; ++i) {
+        v[2 * i] = from0[i * W::STEP * kStageRow];
+        v[2 * i + 1] = from1[i * W::STEP * kStageRow];
+        if constexpr (GATED) {
+            up[2 * i] = from0[i * W::STEP * kStageRow + 8];
+            up[2 * i + 1] = from1[i * W::STEP * kStageRow + 8];
+        }
+    }
+    activate<KIND>(v, m.act);
+    if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < 2 * W::ITEMS; ++i) v[i] *= up[i];
+    }
+    if (m.residual) {
+#pragma unroll
+        for (int i = 0; i < 2 * W::ITEMS; ++i) v[i] += unpack(r[i], m.f16).x;
+    }
+    uint32_t o[W::ITEMS];
+    if (m.f16) {
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i) o[i] = pack(v[2 * i], v[2 * i + 1], 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i) o[i] = pack(v[2 * i], v[2 * i + 1], 0);
+    }
+    uint16_t *to = static_cast<uint16_t *>(m.y) + (row + token) * m.y_stride + col;
+    const int64_t step = W::STEP * m.y_stride;
+    const int in0 = col + c0 < limit ? n - token : 0, in1 = col + c1 < limit ? n - token : 0;
+    if (c0 < c1 && in0 == in1) {
+        to += c0;
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i)
+            if (i * W::STEP < in0) *reinterpret_cast<uint32_t *>(to + i * step) = o[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::ITEMS; ++i) {
+            if (i * W::STEP < in0) to[i * step + c0] = (uint16_t)o[i];
+            if (i * W::STEP < in1) to[i * step + c1] = (uint16_t)(o[i] >> 16);
+        }
     }
 }
 
@@ -631,9 +896,11 @@ __device__ __forceinline__ void launch_wait(const Args &a)
     if (a.release) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-template <bool PAIR, bool GATED, bool EXACT>
+template <int KIND>
 __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_constant__ Args a)
 {
+    constexpr bool PAIR = KIND & kPair, GATED = KIND & kGated, F32 = KIND & kF32;
+    constexpr bool EXACT = KIND & kExact, WIDE = KIND & kWide, NARROW = KIND & kNarrow;
     extern __shared__ uint8_t raw[];
     Shared *s = reinterpret_cast<Shared *>(raw);
     const uint32_t ring = (smem_addr(raw) + shared_bytes(a.m.n_groups) + 1023u) & ~1023u;
@@ -934,6 +1201,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
         /* The first tile is gone through twice: first without a wait, without rows and so without
          * stores, which brings the code into the instruction cache while the sums are under way. */
         bool dry = true;
+        float *const staging = partial + warp * (kBatch * kStageRow); /* kWide, kNarrow */
         for (int32_t t = begin; t < total;) {
             const Tile o = tile_at(a, s, t, &group, features);
             int64_t col = o.feature + (GATED ? quarter * 16 + (lane >> 4) * 8 + (lane & 7)
@@ -952,10 +1220,22 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 c0 = (int32_t)rank * even;
                 c1 = min(o.rows, c0 + even);
             }
-            Residual next; /* of the next batch, on its way since the one before */
-            if (!dry && c0 + from < c1)
-                fetch<GATED ? 8 : 16>(a, place_of<GATED>(o.row + c0 + from, c1 - c0 - from, col),
-                                      next);
+            /* the warp's columns of y, and the end of those that there are */
+            const int64_t first = o.feature + (PAIR ? rank * per_cta : 0) + quarter * (GATED ? 16 : 32);
+            const int32_t lanes_in = (int32_t)a.fr - quarter * 32;
+            int64_t limit = first + (GATED ? lanes_in / 2 : lanes_in);
+            if (limit > a.outs) limit = a.outs;
+            /* the residual of the next batch, on its way since the one before */
+            uint4 wide[4];
+            uint32_t narrow[16];
+            Residual next;
+            if (!dry && c0 + from < c1) {
+                const int64_t row = o.row + c0 + from;
+                const int n = c1 - c0 - from;
+                if constexpr (WIDE) fetch_wide<GATED, F32>(a, row, n, first, limit, wide);
+                else if constexpr (NARROW) fetch_narrow<GATED>(a, row, n, first, limit, narrow);
+                else fetch<F32, GATED ? 8 : 16>(a, place_of<GATED>(row, n, col), next);
+            }
             /* the parts before the last are added up in tensor memory */
             bool more = false; /* a sum lies there */
             if (!dry) {
@@ -997,36 +1277,64 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             const bool few = c1 - c0 <= 4;
             const uint32_t base = smem_addr(partial) + (uint32_t)(quarter * 32 + lane) * 4u;
             if (dry) c1 = min(c1, c0 + 1);
-            for (int32_t c = c0 + from; ok && c < c1; c += kRound) {
-                __syncwarp();
-                if (sharers == 0) {
+            if constexpr (WIDE || NARROW) {
+                for (int32_t c = from; ok && c < c1; c += kRound) {
+                    __syncwarp();
                     sum_load(src + c, sum + c, EXACT && more, v);
-                } else {
-                    float p[4][16]; /* all on their way before the first is added */
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const uint32_t from = map_to(base, dry ? rank : (uint32_t)r % sharers) +
-                                              (uint32_t)c * (kRows * 4u);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            p[r][j] = 0.0f;
-                            if (r < sharers && j < c1 - c)
-                                asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                                             : "=f"(p[r][j])
-                                             : "r"(from + (uint32_t)j * (kRows * 4u)));
-                        }
-                    }
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        v[j] = ((p[0][j] + p[1][j]) + p[2][j]) + p[3][j];
+                        staging[j * kStageRow + lane] = m.bias ? v[j] + bias : v[j];
+                    __syncwarp();
+                    const int64_t row = o.row + c;
+                    const int n = dry ? 0 : c1 - c;
+                    if constexpr (WIDE) {
+                        uint4 r[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) r[j] = wide[j];
+                        if (c + kRound < c1)
+                            fetch_wide<GATED, F32>(a, row + kRound, n - kRound, first, limit, wide);
+                        finish_wide<KIND>(a, staging, row, n, first, limit, r);
+                    } else {
+                        uint32_t r[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) r[j] = narrow[j];
+                        if (c + kRound < c1)
+                            fetch_narrow<GATED>(a, row + kRound, n - kRound, first, limit, narrow);
+                        finish_narrow<KIND>(a, staging, row, n, first, limit, r);
+                    }
                 }
-                const Place p = place_of<GATED>(o.row + c, dry ? 0 : c1 - c, col);
-                const Residual r = next;
-                if (c + kRound < c1)
-                    fetch<GATED ? 8 : 16>(
-                        a, place_of<GATED>(o.row + c + kRound, c1 - c - kRound, col), next);
-                if (few) finish<GATED, 4>(a, v, p, bias, r);
-                else finish<GATED, 16>(a, v, p, bias, r);
+            } else {
+                for (int32_t c = c0 + from; ok && c < c1; c += kRound) {
+                    __syncwarp();
+                    if (sharers == 0) {
+                        sum_load(src + c, sum + c, EXACT && more, v);
+                    } else {
+                        float p[4][16]; /* all on their way before the first is added */
+    #pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint32_t from = map_to(base, dry ? rank : (uint32_t)r % sharers) +
+                                                  (uint32_t)c * (kRows * 4u);
+    #pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                p[r][j] = 0.0f;
+                                if (r < sharers && j < c1 - c)
+                                    asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                                                 : "=f"(p[r][j])
+                                                 : "r"(from + (uint32_t)j * (kRows * 4u)));
+                            }
+                        }
+    #pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            v[j] = ((p[0][j] + p[1][j]) + p[2][j]) + p[3][j];
+                    }
+                    const Place p = place_of<GATED>(o.row + c, dry ? 0 : c1 - c, col);
+                    const Residual r = next;
+                    if (c + kRound < c1)
+                        fetch<F32, GATED ? 8 : 16>(
+                            a, place_of<GATED>(o.row + c + kRound, c1 - c - kRound, col), next);
+                    if (few) finish<KIND, 4>(a, v, p, bias, r);
+                    else finish<KIND, 16>(a, v, p, bias, r);
+                }
             }
             if (dry) {
                 dry = false;
@@ -1057,8 +1365,8 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
 
 struct Device {
     std::atomic<int> sms;          /* 0: not asked yet */
-    std::atomic<int> clusters[8][3]; /* by kernel and split: clusters that run at once, plus one */
-    std::atomic<unsigned> ready;   /* kernels whose shared memory is granted */
+    std::atomic<int> clusters[64][3]; /* by kernel and split: clusters that run at once, plus one */
+    std::atomic<uint64_t> ready;   /* kernels whose shared memory is granted */
 };
 constexpr int kMaxDevices = 64;
 Device g_device[kMaxDevices];
@@ -1095,17 +1403,54 @@ bool encode(CUtensorMap *map, int f16, const void *base, int rank, const cuuint6
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, bool GATED> const void *kernel_of(bool exact)
-{
-    return exact ? reinterpret_cast<const void *>(&cfa_matmul_kernel<PAIR, GATED, true>)
-                 : reinterpret_cast<const void *>(&cfa_matmul_kernel<PAIR, GATED, false>);
-}
-
-const void *kernel_of(bool pair, bool gated, bool exact)
-{
-    if (pair) return gated ? kernel_of<true, true>(exact) : kernel_of<true, false>(exact);
-    return gated ? kernel_of<false, true>(exact) : kernel_of<false, false>(exact);
-}
+/* The kernels that there are.  The second product of the experts alone takes kF32 without kExact, with
+ * y on the 16-byte grid and no activation. */
+struct Kernel {
+    int kind;
+    const void *fn;
+};
+template <int KIND> Kernel kernel() { return {KIND, reinterpret_cast<const void *>(&cfa_matmul_kernel<KIND>)}; }
+constexpr int kHalf = 0, kSingle = kF32 | kExact;
+const Kernel g_kernel[] = {
+    kernel<kWide>(),
+    kernel<kWide | kCurves>(),
+    kernel<kWide | kGated>(),
+    kernel<kWide | kGated | kCurves>(),
+    kernel<kWide | kPair>(),
+    kernel<kWide | kPair | kCurves>(),
+    kernel<kWide | kPair | kGated>(),
+    kernel<kWide | kPair | kGated | kCurves>(),
+    kernel<kWide | kF32>(),
+    kernel<kWide | kF32 | kPair>(),
+    kernel<kWide | kSingle>(),
+    kernel<kWide | kSingle | kCurves>(),
+    kernel<kWide | kSingle | kGated | kCurves>(),
+    kernel<kWide | kSingle | kPair>(),
+    kernel<kWide | kSingle | kPair | kCurves>(),
+    kernel<kWide | kSingle | kPair | kGated | kCurves>(),
+    kernel<kNarrow | kCurves>(),
+    kernel<kNarrow | kCurves | kGated>(),
+    kernel<kNarrow | kCurves | kPair>(),
+    kernel<kNarrow | kCurves | kPair | kGated>(),
+    kernel<kHalf>(),
+    kernel<kCurves>(),
+    kernel<kGated>(),
+    kernel<kGated | kCurves>(),
+    kernel<kF32>(),
+    kernel<kF32 | kPair>(),
+    kernel<kPair>(),
+    kernel<kPair | kGated>(),
+    kernel<kPair | kCurves>(),
+    kernel<kPair | kGated | kCurves>(),
+    kernel<kSingle>(),
+    kernel<kSingle | kCurves>(),
+    kernel<kSingle | kGated | kCurves>(),
+    kernel<kSingle | kPair>(),
+    kernel<kSingle | kPair | kCurves>(),
+    kernel<kSingle | kPair | kGated | kCurves>(),
+};
+constexpr int kKernels = sizeof g_kernel / sizeof g_kernel[0];
+static_assert(kKernels <= 64, "a bit each in Device");
 
 struct Config {
     cudaLaunchConfig_t cfg;
@@ -1156,12 +1501,16 @@ struct Cut {
     uint32_t bn, fr, split; /* split: log2 */
 };
 
-/* Bytes of one stage's blocks that may be taken together, and how many blocks that makes. */
-uint32_t deep_of(bool pair, uint32_t bn, uint32_t fr)
+/* Blocks of a stage: as many as kDeepBytes hold (of a pair, whose products take longer, half of it), if
+ * the ring then has three stages or more (with two, 256 tokens x 4096 x 14,336 took 47 us where 37 do). */
+uint32_t deep_of(const Cut &c)
 {
-    const uint32_t block = (fr + (pair ? bn / 2 : bn)) * kRowBytes;
+    const uint32_t block = (c.fr + (c.pair ? c.bn / 2 : c.bn)) * kRowBytes;
+    const uint32_t ring = kSmem - 4096u - (c.split ? c.bn * kRows * 4u : kStageBytes);
     uint32_t deep = 4;
-    while (deep > 1 && block * deep > (pair ? kDeepBytes / 2 : kDeepBytes)) deep /= 2;
+    while (deep > 1 && (block * deep > (c.pair ? kDeepBytes / 2 : kDeepBytes) ||
+                        block * deep * 3 > ring))
+        deep /= 2;
     return deep;
 }
 
@@ -1169,13 +1518,13 @@ uint32_t deep_of(bool pair, uint32_t bn, uint32_t fr)
  * of a tile's blocks, at the pace of their products and their issue or of what one SM can take in, and
  * of the turn's bytes, at the rate of L2 and of memory; the epilogue of a tile runs under the next
  * tile's products, but for the last.  (Bytes by turns: a last turn of few CTAs cannot draw what memory
- * gives.)
- * The constants are a fit to 13,800 timings: 182 sizes (1 to 4096 tokens, 256 to 28,672 rows, 1024 to
- * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 2.4 % longer than
- * the best of those on average, 25 % at the worst. */
+ * gives.)  Tiles whose rows of y do not fill lines of 128 bytes take longer to store.
+ * The constants are a fit to 16,100 timings: 224 sizes (1 to 4096 tokens, 256 to 28,672 rows, 384 to
+ * 14,336 columns), each cut in up to 130 ways.  The cut that this puts first takes 1.9 % longer than
+ * the best of those on average, 20 % at the worst. */
 double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int64_t rows, const Cut &c)
 {
-    const double kSplit[3] = {0.0, 1.84, 2.68}; /* one, two and four CTAs per tile */
+    const double kSplit[3] = {0.0, 1.67, 2.51}; /* one, two and four CTAs per tile */
     const uint32_t features = (c.pair ? 2 : 1) * (m->gated ? c.fr / 2 : c.fr);
     const int64_t n_tiles = (rows + c.bn - 1) / c.bn;
     const int64_t tiles = n_tiles * m->busy * ((outs + features - 1) / features);
@@ -1184,18 +1533,19 @@ double estimate(const cfa_matmul *m, int64_t outs, uint32_t steps, int sms, int6
     const double blocks = (double)((steps + (1u << c.split) - 1) >> c.split);
     const double used = n_tiles == 1 ? (double)((rows + 15) / 16 * 16) : (double)c.bn;
     const double bytes = (double)(c.fr + (c.pair ? c.bn / 2 : c.bn)) * kRowBytes;
-    const double mma = used * (c.pair ? 0.00078 : 0.0008);
-    double step = (mma > 0.149 ? mma : 0.149) + 0.09 / deep_of(c.pair, c.bn, c.fr);
-    if (step < bytes / 138e3) step = bytes / 138e3;
+    const double mma = used * (c.pair ? 0.00075 : 0.00087);
+    double step = (mma > 0.152 ? mma : 0.152) + 0.078 / deep_of(c);
+    if (step < bytes / 166e3) step = bytes / 166e3;
     const double tokens = (double)(rows < c.bn ? rows : c.bn);
-    const double epilogue = 0.018 * tokens / (1u << c.split), products = blocks * step;
+    const bool lines = (m->gated ? c.fr / 2 : c.fr) * (m->y_f32 ? 4 : 2) % 128 == 0;
+    const double epilogue = (lines ? 0.0146 : 0.0194) * tokens / (1u << c.split), products = blocks * step;
     const double turn = (products > epilogue ? products : epilogue) + 0.6;
-    const double l2 = steps * (c.pair ? 2 : 1) * bytes / 19.9e6; /* per tile */
+    const double l2 = steps * (c.pair ? 2 : 1) * bytes / 20e6; /* per tile */
     const double mem = 2.0 * m->cols * ((double)m->w_rows * m->busy + (double)m->likely) / 6.6e6 /
                        (double)tiles;
     const double share = l2 > mem ? l2 : mem;
     const int64_t full = tiles / slots, left = tiles - full * slots;
-    double us = 2.8 + kSplit[c.split] + (c.split ? 0.01 * tokens : 0.0) + epilogue;
+    double us = 2.8 + kSplit[c.split] + (c.split ? 0.006 * tokens : 0.0) + epilogue;
     us += (double)full * (turn > (double)slots * share ? turn : (double)slots * share);
     if (left) us += turn > (double)left * share ? turn : (double)left * share;
     return us;
@@ -1250,7 +1600,7 @@ Cut cut_of(const cfa_matmul *m, int sms)
 {
     struct Known {
         int64_t likely, w_rows, cols;
-        int32_t busy, gated, exact, sms;
+        int32_t busy, gated, y_f32, exact, sms;
         Cut cut;
     };
     static thread_local Known known[64] = {};
@@ -1259,8 +1609,8 @@ Cut cut_of(const cfa_matmul *m, int sms)
                          ((uint64_t)m->cols * 0x165667B19E3779F9ull) ^ (uint64_t)m->busy;
     Known &k = known[(key >> 40) & 63u];
     if (k.likely != m->likely || k.w_rows != m->w_rows || k.cols != m->cols || k.busy != m->busy ||
-        k.gated != m->gated || k.exact != m->exact || k.sms != sms)
-        k = {m->likely, m->w_rows, m->cols, m->busy, m->gated, m->exact, sms,
+        k.gated != m->gated || k.y_f32 != m->y_f32 || k.exact != m->exact || k.sms != sms)
+        k = {m->likely, m->w_rows, m->cols, m->busy, m->gated, m->y_f32, m->exact, sms,
              choose(m, m->gated ? m->w_rows / 2 : m->w_rows,
                     (uint32_t)((m->cols + kDepth - 1) / kDepth), sms)};
     return k.cut;
@@ -1294,32 +1644,52 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     if (m->offs) /* ragged groups: half as high, a quarter, an eighth */
         for (uint32_t i = 1; i < kBoxes && x_rows >> i >= 16; ++i) a.x_box[i] = (x_rows >> i) / 8 * 8;
     const uint32_t block = (a.fr + x_rows) * kRowBytes;
-    a.deep = deep_of(pair, a.bn, a.fr);
+    a.deep = deep_of(cut);
     const uint32_t stage = block * a.deep;
     a.whole = (uint32_t)(m->cols / kDepth);
     a.f_whole = gated && a.outs % 8 ? (int32_t)(a.outs / 8 * 8) : INT32_MAX;
     /* the products read kRows rows of each block of w, whatever lies behind the a.fr of them */
     const uint32_t after = a.fr + a.deep * x_rows;
     const uint32_t behind = kRows > after ? (kRows - after) * kRowBytes : 0;
-    const uint32_t partial = a.split ? a.bn * kRows * 4u : 0u;
-    const uint32_t left = kSmem - shared_bytes(m->n_groups) - 1024u -
-                          (partial > behind ? partial : behind);
-    a.stages = left / stage < kMaxStages ? left / stage : kMaxStages;
+    const auto stages_beside = [&](uint32_t bytes) {
+        const uint32_t left = kSmem - shared_bytes(m->n_groups) - 1024u - (bytes > behind ? bytes : behind);
+        return left / stage < kMaxStages ? left / stage : kMaxStages;
+    };
+    /* Clusters have their sums in shared memory anyway, and a few tokens are stored as fast from the
+     * registers.  So are those of low tiles where the staging would cost the ring a stage: they wait for
+     * memory. */
+    int kind = (pair ? kPair : 0) | (gated ? kGated : 0);
+    if (m->exact) kind |= kSingle;
+    else if (m->y_f32) kind |= kF32;
+    a.stages = stages_beside(a.split ? a.bn * kRows * 4u : 0u);
+    const uint32_t staged = stages_beside(kStageBytes);
+    if (!a.split && m->tokens > 4 && (a.bn > 128 || staged == a.stages || !a.pairs)) {
+        if ((((uintptr_t)m->y | (uintptr_t)m->residual) & 15u) == 0 &&
+            m->y_stride * (int64_t)(two / 2) % 16 == 0 &&
+            (!m->residual || m->r_stride * (int64_t)(two / 2) % 16 == 0))
+            kind |= kWide;
+        else if (!m->y_f32)
+            kind |= kNarrow | kCurves;
+        if (kind & (kWide | kNarrow)) a.stages = staged;
+    }
+    if (m->act == CFA_ACT_GELU || m->act == CFA_ACT_GELU_TANH || (m->exact && gated)) kind |= kCurves;
+    int kernel = 0;
+    while (kernel < kKernels && g_kernel[kernel].kind != kind) ++kernel;
+    if (kernel == kKernels) return cudaErrorInvalidValue;
+    const void *fn = g_kernel[kernel].fn;
     for (a.acc_on = 16; a.acc_on < a.bn; a.acc_on *= 2) {
     }
     a.tmem_cols = m->exact ? 4 * a.acc_on : 2 * a.acc_on; /* a power of two */
 
-    const unsigned kernel = (pair ? 4u : 0u) + (gated ? 2u : 0u) + (m->exact ? 1u : 0u);
-    const void *fn = kernel_of(pair, gated, m->exact);
-    if (!(d.ready.load() & 1u << kernel)) {
+    if (!(d.ready.load() & 1ull << kernel)) {
         e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
         if (e) return e;
-        d.ready.fetch_or(1u << kernel);
+        d.ready.fetch_or(1ull << kernel);
     }
     const unsigned log = pair ? 1 : a.split, size = 1u << log;
     int clusters = sms;
     if (log) {
-        e = clusters_of(d, fn, kernel, log, &clusters);
+        e = clusters_of(d, fn, (unsigned)kernel, log, &clusters);
         if (e) return e;
     }
     if (clusters > most) clusters = (int)most;
