@@ -330,8 +330,9 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, uint32_t phase)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-/* Rows onto the 16-byte grid, zeros behind the last column.  A warp takes a row: every lane loads the
- * aligned 16 bytes that its result starts in and has the next lane's for the rest.  Granules that are
+/* Rows onto the 16-byte grid, zeros behind the last column.  A warp takes 128 granules of a row at a
+ * time, so that few long rows keep as many warps busy as many short ones: every lane loads the aligned
+ * 16 bytes that its result starts in and has the next lane's for the rest.  Granules that are
  * not wholly inside the matrix go element by element. */
 __global__ void __launch_bounds__(kThreads) cfa_realign_kernel(const RealignArgs all)
 {
@@ -353,47 +354,46 @@ __global__ void __launch_bounds__(kThreads) cfa_realign_kernel(const RealignArgs
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     };
-    for (int64_t r = blockIdx.x * (int64_t)(kThreads / 32) + (threadIdx.x >> 5); r < a.rows;
-         r += warps) {
+    const int64_t n = a.to_stride / 8, chunks = (n + 127) / 128;
+    for (int64_t i = blockIdx.x * (int64_t)(kThreads / 32) + (threadIdx.x >> 5); i < a.rows * chunks;
+         i += warps) {
+        const int64_t r = i / chunks, c0 = (i - r * chunks) * 128;
         const uintptr_t row = (uintptr_t)(a.from + r * a.from_stride);
         const uint32_t phase = (uint32_t)(row & 15u);
         uint4 *to = reinterpret_cast<uint4 *>(a.to + r * a.to_stride);
-        const int64_t n = a.to_stride / 8;
-        for (int64_t c0 = 0; c0 < n; c0 += 4 * 32) {
-            uint4 g[5];
+        uint4 g[5];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t c = c0 + u * 32 + lane;
-                g[u] = c < n ? granule(row - phase + 16 * c) : make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < 4; ++u) {
+            const int64_t c = c0 + u * 32 + lane;
+            g[u] = c < n ? granule(row - phase + 16 * c) : make_uint4(0, 0, 0, 0);
+        }
+        g[4] = make_uint4(0, 0, 0, 0);
+        if (phase && lane == 0 && c0 + 128 < n + 1) g[4] = granule(row - phase + 16 * (c0 + 128));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t c = c0 + u * 32 + lane;
+            uint4 v = g[u];
+            if (phase) { /* the same for the whole warp */
+                /* the granule behind the lane's: the next lane's, or lane 0's of the next round */
+                const uint4 mine = lane == 0 ? g[u + 1] : g[u];
+                uint4 next;
+                next.x = __shfl_sync(kAll, mine.x, (lane + 1) & 31);
+                next.y = __shfl_sync(kAll, mine.y, (lane + 1) & 31);
+                next.z = __shfl_sync(kAll, mine.z, (lane + 1) & 31);
+                next.w = __shfl_sync(kAll, mine.w, (lane + 1) & 31);
+                if (c == n - 1) next = granule(row - phase + 16 * (c + 1));
+                v = shifted(v, next, phase);
             }
-            g[4] = make_uint4(0, 0, 0, 0);
-            if (phase && lane == 0 && c0 + 128 < n + 1) g[4] = granule(row - phase + 16 * (c0 + 128));
+            if (c >= n) continue;
+            const int64_t left = a.cols - c * 8;
+            if (left < 8) { /* zeros behind the last column */
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t c = c0 + u * 32 + lane;
-                uint4 v = g[u];
-                if (phase) { /* the same for the whole warp */
-                    /* the granule behind the lane's: the next lane's, or lane 0's of the next round */
-                    const uint4 mine = lane == 0 ? g[u + 1] : g[u];
-                    uint4 next;
-                    next.x = __shfl_sync(kAll, mine.x, (lane + 1) & 31);
-                    next.y = __shfl_sync(kAll, mine.y, (lane + 1) & 31);
-                    next.z = __shfl_sync(kAll, mine.z, (lane + 1) & 31);
-                    next.w = __shfl_sync(kAll, mine.w, (lane + 1) & 31);
-                    if (c == n - 1) next = granule(row - phase + 16 * (c + 1));
-                    v = shifted(v, next, phase);
-                }
-                if (c >= n) continue;
-                const int64_t left = a.cols - c * 8;
-                if (left < 8) { /* zeros behind the last column */
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i >= left) w[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                to[c] = v;
+                for (int i = 0; i < 8; ++i)
+                    if (i >= left) w[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                v = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            to[c] = v;
         }
     }
 }
@@ -459,7 +459,8 @@ cudaError_t cfa_launch_realign(const cfa_rows *m, int n, cudaStream_t stream)
     for (int i = 0; i < n; ++i) {
         a.m[i] = {static_cast<const uint16_t *>(m[i].from), static_cast<uint16_t *>(m[i].to),
                   m[i].from_stride, m[i].to_stride, m[i].rows, m[i].cols};
-        if (m[i].rows > most) most = m[i].rows;
+        const int64_t pieces = m[i].rows * ((m[i].to_stride / 8 + 127) / 128);
+        if (pieces > most) most = pieces;
     }
     const int64_t blocks = (most + kThreads / 32 - 1) / (kThreads / 32);
     return launch(cfa_realign_kernel, dim3((unsigned)(blocks < 1216 ? blocks : 1216), (unsigned)n),
