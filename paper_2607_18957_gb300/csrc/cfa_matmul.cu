@@ -1437,11 +1437,6 @@ const Kernel g_kernel[] = {
     kernel<kGated>(),
     kernel<kGated | kCurves>(),
     kernel<kF32>(),
-    kernel<kF32 | kPair>(),
-    kernel<kPair>(),
-    kernel<kPair | kGated>(),
-    kernel<kPair | kCurves>(),
-    kernel<kPair | kGated | kCurves>(),
     kernel<kSingle>(),
     kernel<kSingle | kCurves>(),
     kernel<kSingle | kGated | kCurves>(),
@@ -1657,13 +1652,13 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     };
     /* Clusters have their sums in shared memory anyway, and a few tokens are stored as fast from the
      * registers.  So are those of low tiles where the staging would cost the ring a stage: they wait for
-     * memory. */
+     * memory (64 tokens through all of 8 experts of 14,336 x 4096: 428 us, 414 from registers). */
     int kind = (pair ? kPair : 0) | (gated ? kGated : 0);
     if (m->exact) kind |= kSingle;
     else if (m->y_f32) kind |= kF32;
     a.stages = stages_beside(a.split ? a.bn * kRows * 4u : 0u);
     const uint32_t staged = stages_beside(kStageBytes);
-    if (!a.split && m->tokens > 4 && (a.bn > 128 || staged == a.stages || !a.pairs)) {
+    if (!a.split && m->tokens > 4 && (pair || a.bn > 128 || staged == a.stages || !a.pairs)) {
         if ((((uintptr_t)m->y | (uintptr_t)m->residual) & 15u) == 0 &&
             m->y_stride * (int64_t)(two / 2) % 16 == 0 &&
             (!m->residual || m->r_stride * (int64_t)(two / 2) % 16 == 0))

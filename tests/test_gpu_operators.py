@@ -125,6 +125,33 @@ def test_linear_epilogue(t, n, k, act, gated):
         close(y, *linear64(x, w, b, act, gated, r, y.dtype))
 
 
+@pytest.mark.parametrize("t,n,k,gated,act,out", [
+    (171, 11200, 648, False, "none", None), (161, 10104, 784, False, "gelu", None),
+    (161, 5440, 648, True, "silu", None), (197, 5064, 792, True, "gelu_tanh", None),
+    (162, 11033, 720, False, "relu", None), (172, 5433, 680, True, "silu", None),
+    (900, 6359, 392, False, "gelu_tanh", None), (900, 6362, 392, False, "silu", None),
+    (2372, 904, 2560, False, "none", "f32"), (4808, 448, 2832, False, "gelu_tanh", "f32"),
+    (4747, 196, 2248, True, "silu", "f32"), (4767, 386, 2544, False, "relu", "f32"),
+    (4787, 462, 3104, False, "gelu", "f32"), (4821, 230, 2264, True, "silu", "f32"),
+    (2438, 8, 32, False, "none", "f32"), (5, 5000, 32, False, "gelu", "f32"),
+    (17, 16, 144, True, "gelu", None), (7, 18, 144, True, "silu", None)])
+def test_linear_of_every_kind_of_tile(t, n, k, gated, act, out):
+    """Tiles of one SM and of two, results of 2 and of 4 bytes on the 16-byte grid, off it and between
+    words; n columns of results."""
+    dtype = F16 if n % 3 else BF16
+    g = gen(t + n + k)
+    x = normal(g, (t, k), dtype)
+    w = normal(g, (2 * n if gated else n, k), dtype, k ** -0.5)
+    b = normal(g, (w.shape[0],), dtype)
+    odt = F32 if out else dtype
+    r = normal(g, (t, n), odt)
+    for residual in (None, r):
+        buf, y = inside(t, n, odt)
+        assert cfa.linear(x, w, b, activation=act, gated=gated, residual=residual, out=y) is y
+        close(y, *linear64(x, w, b, act, gated, residual, odt))
+        assert bool(torch.isnan(buf[t * n:]).all())
+
+
 @pytest.mark.parametrize("t,n,k", [(3, 16, 128), (70, 144, 128), (300, 2000, 320), (5, 24, 64),
                                    (9, 14, 192), (200, 310, 256), (600, 1030, 128), (2, 2, 64),
                                    (40, 6, 72)])
@@ -412,6 +439,14 @@ def test_experts(t, h, i, e, top_k, dtype):
     x, ids, w, w13, w2 = expert_operands(t, h, i, e, top_k, e, dtype, t + h + e)
     y = cfa.experts(x, ids, w, w13, w2)
     close(y, *experts64(x, ids, w, w13, w2, "silu", 0, None))
+
+
+@pytest.mark.parametrize("t,h,i,e,top_k", [(1300, 624, 480, 48, 2), (900, 1000, 416, 6, 3)])
+def test_experts_of_many_tokens_each(t, h, i, e, top_k):
+    x, ids, w, w13, w2 = expert_operands(t, h, i, e, top_k, e, BF16, t + h)
+    r = normal(gen(t), (t, h), BF16)
+    y = cfa.experts(x, ids, w, w13, w2, residual=r)
+    close(y, *experts64(x, ids, w, w13, w2, "silu", 0, r))
 
 
 @pytest.mark.parametrize("t", [1, 70, 3000])
