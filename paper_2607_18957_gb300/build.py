@@ -30,7 +30,7 @@ def _nvcc():
 
 def _sources():
     return [os.path.join(CSRC, f) for f in CU_SOURCES + C_SOURCES +
-            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h"]] + \
+            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h", "cfa_tiles.h"]] + \
         [os.path.join(INCLUDE, "cfa.h")]
 
 
