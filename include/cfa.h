@@ -661,7 +661,9 @@ cfa_status cfa_linear_async(const cfa_linear_args *args, cfa_stream stream);
  *            (the same order, and no two logits tie by rounding)
  *   groups   with groups > 1 the experts form that many groups of neighbours, and only those of
  *            the top_groups best groups can be chosen.  A group's rank is its best key with
- *            softmax, the sum of its two best keys with sigmoid (groups of one: the key)
+ *            softmax, the sum of its two best keys with sigmoid (one key where the group has only
+ *            one).  Only the keys of available experts count: masking an expert takes it out of
+ *            its group's rank, and a group without any left comes last
  *   choice   the top_k largest keys in descending order; of equal ones (keys, groups) the lowest
  *            index comes first
  *   weights  the scores (without bias) of the chosen experts; with CFA_ROUTE_RENORMALIZE divided by

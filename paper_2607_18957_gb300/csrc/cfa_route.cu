@@ -105,6 +105,14 @@ __device__ __forceinline__ void merge(float &first, float &second, float a, floa
     second = fmaxf(fmaxf(second, b), low);
 }
 
+/* A group's place among the others by its two best keys.  An expert that cannot be chosen counts for
+ * nothing in its group: the sum of the two best is the one key where only one expert is left (with -inf
+ * in the sum the group would rank behind all others), and a group without any is last. */
+__device__ __forceinline__ uint32_t rank_of(float first, float second, bool sum_two)
+{
+    return order_of(sum_two && second > -INFINITY ? first + second : first);
+}
+
 /* Which lanes' keys lie in a group that is kept; by lanes where every lane's keys lie in one group of
  * 2^n neighbouring lanes, otherwise through shared memory. */
 template <int R>
@@ -118,7 +126,7 @@ __device__ __forceinline__ void keep_groups(const cfa_route_args &a, float (&key
         for (int r = 0; r < R; ++r) merge(first, second, key[r], -INFINITY);
         for (int o = 1; o < lanes; o <<= 1)
             merge(first, second, __shfl_xor_sync(kAll, first, o), __shfl_xor_sync(kAll, second, o));
-        const uint32_t best = order_of(sum_two && size > 1 ? first + second : first);
+        const uint32_t best = rank_of(first, second, sum_two);
         const int group = lane / lanes;
         int before = 0;
         for (int g = 0; g < a.groups; ++g) {
@@ -138,7 +146,7 @@ __device__ __forceinline__ void keep_groups(const cfa_route_args &a, float (&key
     float first = -INFINITY, second = -INFINITY;
     if (lane < a.groups)
         for (int i = 0; i < size; ++i) merge(first, second, mine[lane * size + i], -INFINITY);
-    const uint32_t best = order_of(sum_two && size > 1 ? first + second : first);
+    const uint32_t best = rank_of(first, second, sum_two);
     int before = 0;
     for (int g = 0; g < a.groups; ++g) {
         const uint32_t other = __shfl_sync(kAll, best, g);

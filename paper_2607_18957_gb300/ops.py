@@ -227,7 +227,8 @@ def route(logits, top_k, *, scoring="softmax", bias=None, groups=1, top_groups=1
     logits    [..., E] bf16, fp16 or fp32;  scoring "softmax" or "sigmoid"
     bias      [E] fp32, added to the scores for the choice alone
     groups    only experts of the top_groups best of `groups` groups of neighbours can be chosen; a
-              group goes by its best key (softmax) or the sum of its two best (sigmoid)
+              group goes by its best key (softmax) or the sum of its two best (sigmoid), of the
+              experts that can be chosen at all
     renormalize  divides the chosen scores by their sum;  scale multiplies them
     out       (weights, ids) to write into
     Equal keys go to the lowest index; an expert whose logit or key is -inf or NaN is never chosen,

@@ -1,4 +1,7 @@
-"""Edges of the operators on the loaded layout: many tokens with fp32 results."""
+"""Edges of the operators on the loaded layout: many tokens with fp32 results, groups of experts of which
+some cannot be chosen."""
+import math
+
 import pytest
 import torch
 
@@ -47,3 +50,101 @@ def test_fp32_results_of_many_tokens(t, n, k, gated):
     assert y.dtype == F32 and y.shape == (t, n)
     worst = ((y.double() - ref).abs() - bound).max().item()
     assert worst <= 0, f"off by {worst:g} more than the bound"
+
+
+# ---- groups of experts --------------------------------------------------------------------------
+
+def route_row(row, bias, top_k, scoring, groups, top_groups):
+    """(ids, weights, margin) of one token from the definition, in 64 bits; margin: how far apart the
+    closest two groups and the closest two keys lie that are told apart."""
+    n, size = len(row), len(row) // groups
+    top = max(row)
+    if scoring == "softmax":
+        norm = sum(math.exp(v - top) for v in row) if top > -math.inf else 1.0
+        score = [math.exp(v - top) / norm if v > -math.inf else 0.0 for v in row]
+    else:
+        score = [1 / (1 + math.exp(-v)) if v > -math.inf else 0.0 for v in row]
+    key = row if bias is None and scoring == "softmax" else [
+        s + (0.0 if bias is None else b) for s, b in zip(score, bias or score)]
+    free = [v > -math.inf and k == k and k > -math.inf for v, k in zip(row, key)]
+    rank = []
+    for q in range(groups):
+        left = sorted((key[e] for e in range(q * size, (q + 1) * size) if free[e]), reverse=True)
+        count = 2 if scoring == "sigmoid" else 1
+        rank.append(sum(left[:count]) if left else -math.inf)
+    order = sorted(range(groups), key=lambda q: (-rank[q], q))
+    kept, margin = order[:top_groups], math.inf
+    if top_groups < groups and rank[order[top_groups]] > -math.inf:
+        margin = rank[order[top_groups - 1]] - rank[order[top_groups]]
+    left = sorted((e for e in range(n) if free[e] and e // size in kept), key=lambda e: (-key[e], e))
+    for a, b in zip(left[:top_k], left[1:]):
+        margin = min(margin, key[a] - key[b])
+    ids = left[:top_k]
+    w = [score[e] for e in ids]
+    if scoring == "softmax":
+        w = [math.exp(row[e] - max(row[i] for i in ids)) for e in ids]
+    total = sum(w)
+    w = [v / total if total else 0.0 for v in w]
+    pad = top_k - len(ids)
+    return ids + [-1] * pad, w + [0.0] * pad, margin
+
+
+def check_groups(z, top_k, scoring, bias, groups, top_groups):
+    """Keys without a bias are fp32 values below 1, at most three units of 2^-24 off, their sums seven: choices
+    that are 2^-20 apart have to be the definition's, and with a bias (below 4) those 2^-18 apart."""
+    near = 2.0 ** -20 if bias is None else 2.0 ** -18
+    w, i = cfa.route(z, top_k, scoring=scoring, bias=bias, groups=groups, top_groups=top_groups)
+    b = None if bias is None else bias.double().cpu().tolist()
+    clear = 0
+    for row, gi, gw in zip(z.double().cpu().tolist(), i.cpu().tolist(), w.cpu().tolist()):
+        ids, weights, margin = route_row(row, b, top_k, scoring, groups, top_groups)
+        if margin < near:
+            continue
+        clear += 1
+        assert gi == ids
+        assert all(abs(x - y) <= 2.0 ** -19 * y for x, y in zip(gw, weights))
+    assert clear >= 0.75 * z.shape[0]
+
+
+def masked(z, groups, how, seed):
+    t, e = z.shape
+    part = z.view(t, groups, e // groups)
+    r = torch.rand(part.shape, generator=torch.Generator(device="cuda").manual_seed(seed),
+                   device="cuda")
+    rank = r.argsort(dim=2).argsort(dim=2)
+    if how == "one of each":
+        part[rank == 0] = -math.inf
+    elif how == "all but one":
+        part[rank != 0] = -math.inf
+    elif how == "a group":
+        part[torch.arange(t), torch.arange(t) % groups] = -math.inf
+    elif how == "half":
+        part[r < 0.5] = -math.inf
+    elif how == "nearly all":
+        part[r < 0.95] = -math.inf
+    return z
+
+
+GROUPS = [(8, 4, 2, 2), (16, 4, 2, 3), (64, 8, 4, 8), (60, 4, 2, 6), (96, 32, 5, 8), (256, 8, 4, 8),
+          (1024, 2, 1, 32)]
+HOW = ["none", "one of each", "all but one", "a group", "half", "nearly all"]
+
+
+@pytest.mark.parametrize("e,groups,top_groups,top_k", GROUPS)
+@pytest.mark.parametrize("how", HOW)
+@pytest.mark.parametrize("scoring,biased", [("softmax", False), ("sigmoid", False),
+                                            ("sigmoid", True), ("softmax", True)])
+def test_groups_with_masked_experts(e, groups, top_groups, top_k, how, scoring, biased):
+    z = masked(normal(e, (40, e), F32, 1.5), groups, how, e + 1)
+    bias = normal(e + 2, (e,), F32, 0.3) if biased else None
+    check_groups(z, top_k, scoring, bias, groups, top_groups)
+
+
+def test_a_masked_expert_leaves_its_group_its_rank():
+    z = torch.tensor([[5.0, -math.inf, -3.0, -3.0]], device="cuda")
+    w, i = cfa.route(z, 1, scoring="sigmoid", groups=2, top_groups=1)
+    assert i.tolist() == [[0]] and w.tolist() == [[1.0]]
+    z = torch.tensor([[-math.inf, -math.inf, -3.0, -math.inf]], device="cuda")
+    bias = torch.tensor([4.0, 4.0, -2.0, 4.0], device="cuda")  # of experts that cannot be chosen
+    w, i = cfa.route(z, 1, scoring="sigmoid", bias=bias, groups=2, top_groups=1)
+    assert i.tolist() == [[2]] and w.tolist() == [[1.0]]
