@@ -148,3 +148,29 @@ def test_a_masked_expert_leaves_its_group_its_rank():
     bias = torch.tensor([4.0, 4.0, -2.0, 4.0], device="cuda")  # of experts that cannot be chosen
     w, i = cfa.route(z, 1, scoring="sigmoid", bias=bias, groups=2, top_groups=1)
     assert i.tolist() == [[2]] and w.tolist() == [[1.0]]
+
+
+@pytest.mark.parametrize("e,groups,top_groups,top_k", GROUPS)
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("what", [math.nan, -math.inf])
+def test_groups_with_a_bias_that_takes_experts_out(e, groups, top_groups, top_k, scoring, what):
+    bias = normal(e + 3, (e,), F32, 0.3)
+    bias[::5] = what
+    check_groups(normal(e, (40, e), F32, 1.5), top_k, scoring, bias, groups, top_groups)
+
+
+@pytest.mark.parametrize("size", [2, 3, 4, 8, 16])
+def test_a_nan_in_the_bias_does_not_count_its_group_twice(size):
+    """Two groups; the first has one key of 0.6 and NaN, the second two keys of 0.4: 0.6 < 0.8, whatever
+    place the NaN has."""
+    for at in range(1, size):
+        z = torch.full((1, 2 * size), -30.0, device="cuda")
+        z[0, 0] = math.log(0.6 / 0.4)
+        z[0, size:size + 2] = -math.log(0.6 / 0.4)
+        bias = torch.zeros(2 * size, device="cuda")
+        bias[at] = math.nan
+        for pad in (1, 8, 16):  # groups without a chance, so that a lane holds several keys
+            zz = torch.cat([z, torch.full((1, 2 * size * (pad - 1)), -30.0, device="cuda")], dim=1)
+            bb = torch.cat([bias, torch.zeros(2 * size * (pad - 1), device="cuda")])
+            w, i = cfa.route(zz, 1, scoring="sigmoid", bias=bb, groups=2 * pad, top_groups=1)
+            assert i.tolist() == [[size]] and w.tolist() == [[1.0]]
