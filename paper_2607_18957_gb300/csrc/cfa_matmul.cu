@@ -390,9 +390,15 @@ template <int KIND, int N> __device__ __forceinline__ void activate(float (&v)[N
     case CFA_ACT_SILU:
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            /* both fast forms are off by some units in the last place of fp32: the quotient by two,
-             * which fp32 results may be, the exponential by |v|, which 16 bits do not show */
-            v[i] = __fdividef(v[i], 1.0f + (KIND & kExact ? expf(-v[i]) : __expf(-v[i])));
+        {
+            /* Both fast forms are off by some units in the last place of fp32: the quotient by two,
+             * which fp32 results may be, the exponential by |v|, which 16 bits do not show.  The fast
+             * quotient is 0 for divisors above 2^126, which 1 + exp(-v) is from v = -87.4 on, with
+             * the value at -9e-37; a quarter of both sides of it stays below to where exp(-v) leaves
+             * fp32 (-88.7). */
+            const float e = KIND & kExact ? expf(-v[i]) : __expf(-v[i]);
+            v[i] = __fdividef(0.25f * v[i], fmaf(0.25f, e, 0.25f));
+        }
         break;
     default: break;
     }

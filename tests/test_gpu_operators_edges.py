@@ -1,5 +1,5 @@
-"""Edges of the operators on the loaded layout: many tokens with fp32 results, groups of experts of which
-some cannot be chosen."""
+"""Edges of the operators on the loaded layout: many tokens with fp32 results, SiLU where exp(-v) leaves
+fp32, groups of experts of which some cannot be chosen."""
 import math
 
 import pytest
@@ -50,6 +50,27 @@ def test_fp32_results_of_many_tokens(t, n, k, gated):
     assert y.dtype == F32 and y.shape == (t, n)
     worst = ((y.double() - ref).abs() - bound).max().item()
     assert worst <= 0, f"off by {worst:g} more than the bound"
+
+
+@pytest.mark.parametrize("t", [1, 40, 300])
+@pytest.mark.parametrize("dtype,out", [(BF16, "f32"), (F16, "f32"), (BF16, None)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_silu_of_arguments_far_below_zero(t, dtype, out, gated):
+    """-77, -77.5, .. -88.5, where exp(-v) is just inside fp32 and the value a normal number of fp32
+    and bf16.  The exponential is off by two units in the last place for fp32 results and by 2 + 1.173
+    |v| for others, the sum by half a unit, the quotient by two; bf16's rounding by 2^-8."""
+    v = -77.0 - 0.5 * torch.arange(24, device="cuda")
+    x = torch.zeros(t, 16, dtype=dtype, device="cuda")
+    x[:, 3] = 1.0
+    w = torch.zeros(48 if gated else 24, 16, dtype=dtype, device="cuda")
+    w[:24, 3] = v.to(dtype)
+    if gated:
+        w[24:, 3] = 1.0
+    assert torch.equal(w[:24, 3].float(), v)
+    y = cfa.linear(x, w, activation="silu", gated=gated, out_dtype=out).double()
+    ref = (v.double() / (1 + torch.exp(-v.double()))).expand(t, 24)
+    units = 5 if out else 5 + 1.173 * 88.5
+    assert bool(((y - ref).abs() <= (units * 2.0 ** -23 + (0 if out else 2.0 ** -8)) * ref.abs()).all())
 
 
 # ---- groups of experts --------------------------------------------------------------------------
