@@ -734,18 +734,20 @@ cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
 
 /*
  * The products wait for their own loads and for one another inside a kernel, each time with a limit.
- * Returns CFA_OK if no wait has run out on the current device since the last call, CFA_ERR_DEVICE if
- * one has (the results since then are not valid), CFA_ERR_SUSPECT if loads in flight did not end
- * either (see there); then clears the record.  Call it after the streams in question have been
- * waited for; it reads one word from the device.
+ * Returns CFA_OK if no wait has run out on the current device since the calling thread's last call
+ * there, CFA_ERR_DEVICE if one has (the results since then are not valid), CFA_ERR_SUSPECT if loads in
+ * flight did not end either (see there).  The device only counts: every thread is told of every wait
+ * that ran out, once, whichever stream or thread it belongs to, and a thread's first call of all that
+ * there have been.  Call it after the streams in question have been waited for; it reads two words
+ * from the device.
  */
 cfa_status cfa_op_status(void);
 
 /*
  * Self-test of those waits, like cfa_selftest_wait_timeout: on `device` (-1 = current) one product is
- * launched whose loader asks for nothing, so that its other waits run out.  *status_word receives the
- * word that it left: 1 when every wait ended and the kernel returned; the record is cleared again.  The
- * CUDA context stays usable.  Allocates and frees 17 KiB of device memory; synchronizes the device.
+ * launched whose loader asks for nothing, so that its other waits run out.  *status_word receives 1 when
+ * every wait ended and the kernel returned; cfa_op_status is told nothing of it.  The CUDA context stays
+ * usable.  Allocates and frees 17 KiB of device memory; synchronizes the device.
  * Errors: CFA_ERR_INVAL (status_word NULL), CFA_ERR_CUDA.
  */
 cfa_status cfa_selftest_op_timeout(int device, int *status_word);

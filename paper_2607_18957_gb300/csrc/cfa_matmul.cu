@@ -47,7 +47,7 @@
  * columns, as a product in plain fp32 has).  Results of 16 bits, whose own rounding is a thousand times
  * that, are summed in one go.
  *
- * Every wait has a limit.  One that runs out sets the status word that cfa_op_status reads; its CTA
+ * Every wait has a limit.  One that runs out is counted in what cfa_op_status reads; its CTA
  * then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
  * memory.
  */
@@ -116,7 +116,7 @@ struct Args {
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
 
-__device__ int g_status; /* 1: a wait ran out, 2: and so did the wait for the loads in flight */
+__device__ cfa_op_counts g_counts[2]; /* of waits that ran out; [1]: the self-test's */
 
 /* What precedes the stages in shared memory. */
 struct Shared {
@@ -856,15 +856,15 @@ __device__ __forceinline__ void finish_narrow(const Args &a, const float *stage,
  * first CTA's barriers count the loads of both; the second only gives its own the same time. */
 __device__ void drain(const Args &a, Shared *s, uint32_t issued, bool second)
 {
-    int word = 1;
+    bool ended = true;
     const uint32_t most = issued < a.stages ? issued : a.stages;
     for (uint32_t l = issued - most; l < issued; ++l) {
         bool done = false;
         for (uint32_t k = 0; !done && k < kDrainLimit; ++k)
             done = mbar_try_wait(smem_addr(s->full + l % a.stages), (l / a.stages) & 1u);
-        if (!done && !second) word = 2;
+        if (!done && !second) ended = false;
     }
-    atomicMax(&g_status, word);
+    if (!ended) atomicAdd(&g_counts[a.lose].in_flight, 1u);
 }
 
 /* A stage's blocks of w, from block k on. */
@@ -1347,7 +1347,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
 
     fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *(volatile int *)&s->dead) atomicMax(&g_status, 1);
+    if (threadIdx.x == 0 && *(volatile int *)&s->dead) atomicAdd(&g_counts[a.lose].ran_out, 1u);
     if constexpr (PAIR) cluster_sync();
     if (warp == kIssuer) {
         const uint32_t tmem = s->tmem;
@@ -1662,20 +1662,29 @@ cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaS
     return launch(m, d, sms, cut_of(m, sms), early, release, stream);
 }
 
+/* Every thread has its own record of what it has been told: one that asks takes nothing from another,
+ * and nothing that is counted between two of its calls is lost. */
 cudaError_t cfa_matmul_status(int *word)
 {
-    const int zero = 0;
-    const cudaError_t e = cudaMemcpyFromSymbol(word, g_status, sizeof *word);
-    return e || !*word ? e : cudaMemcpyToSymbol(g_status, &zero, sizeof zero);
+    static thread_local cfa_op_counts seen[kMaxDevices] = {};
+    cfa_op_counts now;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (!e && (dev < 0 || dev >= kMaxDevices)) e = cudaErrorInvalidDevice;
+    if (!e) e = cudaMemcpyFromSymbol(&now, g_counts, sizeof now);
+    if (!e) *word = cfa_op_news(seen + dev, now);
+    return e;
 }
 
 /* A product of one token whose loader asks for nothing, on the default stream: its waits run out after
- * 4096 polls each.  *word receives the status word that this leaves, which is then cleared. */
+ * 4096 polls each.  *word receives what this has been counted as, in counts of its own. */
 cudaError_t cfa_matmul_selftest(int *word)
 {
     uint8_t *buf = nullptr;
     const size_t w_bytes = 128 * 64 * 2, x_bytes = 64 * 2, y_bytes = 128 * 2;
-    cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&buf), w_bytes + x_bytes + y_bytes);
+    cfa_op_counts before, after;
+    cudaError_t e = cudaMemcpyFromSymbol(&before, g_counts, sizeof before, sizeof before);
+    if (!e) e = cudaMalloc(reinterpret_cast<void **>(&buf), w_bytes + x_bytes + y_bytes);
     if (e) return e;
     e = cudaMemset(buf, 0, w_bytes + x_bytes + y_bytes);
     cfa_matmul m = {};
@@ -1687,7 +1696,8 @@ cudaError_t cfa_matmul_selftest(int *word)
     m.cols = m.x_stride = m.w_stride = 64;
     if (!e) e = cfa_launch_matmul(&m, 0, 0, nullptr);
     if (!e) e = cudaDeviceSynchronize();
-    if (!e) e = cfa_matmul_status(word);
+    if (!e) e = cudaMemcpyFromSymbol(&after, g_counts, sizeof after, sizeof after);
+    if (!e) *word = cfa_op_news(&before, after);
     const cudaError_t freed = cudaFree(buf);
     return e ? e : freed;
 }

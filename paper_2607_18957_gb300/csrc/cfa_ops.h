@@ -55,7 +55,22 @@ typedef struct cfa_sort {
 /* All of these enqueue on `stream` and return a CUDA error. `early`: may start before the kernel
  * before it on the stream has ended, and waits inside; `release`: its dependents may do so. */
 cudaError_t cfa_launch_matmul(const cfa_matmul *m, int early, int release, cudaStream_t stream);
-/* The current device's word of waits that ran out (0: none), cleared. */
+/* CTAs in which a wait has run out, and those of them whose loads in flight did not end either: counted
+ * up on the device and never set back, so that no reader takes anything from another. */
+typedef struct cfa_op_counts {
+    uint32_t ran_out, in_flight;
+} cfa_op_counts;
+/* What has been counted since *seen, which becomes `now`: 0 nothing, 1 waits that ran out, 2 loads in
+ * flight too.  Lower counts than those seen are a new start of the device's. */
+static inline int cfa_op_news(cfa_op_counts *seen, cfa_op_counts now)
+{
+    if ((int32_t)(now.ran_out - seen->ran_out) < 0 || (int32_t)(now.in_flight - seen->in_flight) < 0)
+        seen->ran_out = seen->in_flight = 0;
+    const int word = now.in_flight != seen->in_flight ? 2 : now.ran_out != seen->ran_out ? 1 : 0;
+    *seen = now;
+    return word;
+}
+/* The current device's news since the calling thread last asked. */
 cudaError_t cfa_matmul_status(int *word);
 cudaError_t cfa_matmul_selftest(int *word);
 cudaError_t cfa_launch_route(const cfa_route_args *a, cudaStream_t stream);

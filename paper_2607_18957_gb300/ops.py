@@ -377,5 +377,6 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
 
 def op_status():
     """Raises CfaError if a wait inside a product's kernel has run out on the current device since the
-    last call (the results since then are not valid).  Call it after waiting for the streams."""
+    calling thread's last call (the results since then are not valid), whichever thread or stream it
+    belongs to.  Call it after waiting for the streams."""
     _check(_lib.load().cfa_op_status())

@@ -1,6 +1,8 @@
 """Edges of the operators on the loaded layout: many tokens with fp32 results, SiLU where exp(-v) leaves
-fp32, groups of experts of which some cannot be chosen."""
+fp32, groups of experts of which some cannot be chosen, threads that ask for waits that ran out."""
+import ctypes
 import math
+import threading
 
 import pytest
 import torch
@@ -195,3 +197,32 @@ def test_a_nan_in_the_bias_does_not_count_its_group_twice(size):
             bb = torch.cat([bias, torch.zeros(2 * size * (pad - 1), device="cuda")])
             w, i = cfa.route(zz, 1, scoring="sigmoid", bias=bb, groups=2 * pad, top_groups=1)
             assert i.tolist() == [[size]] and w.tolist() == [[1.0]]
+
+
+# ---- waits that ran out -------------------------------------------------------------------------
+
+def test_a_thread_that_asks_takes_nothing_from_another():
+    """The self-test's waits run out (and end) in one thread while another asks all the time: the first
+    is told of them every time and the other never."""
+    from paper_2607_18957_gb300 import _lib
+    lib = _lib.load()
+    over, told = threading.Event(), []
+
+    def ask():
+        torch.cuda.set_device(0)
+        while not over.is_set():
+            told.append(lib.cfa_op_status())
+
+    other = threading.Thread(target=ask)
+    other.start()
+    words = []
+    try:
+        for _ in range(40):
+            word = ctypes.c_int(-1)
+            assert lib.cfa_selftest_op_timeout(-1, ctypes.byref(word)) == 0
+            words.append(word.value)
+    finally:
+        over.set()
+        other.join()
+    assert words == [1] * 40
+    assert told and set(told) == {0}
