@@ -744,10 +744,11 @@ cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
 cfa_status cfa_op_status(void);
 
 /*
- * Self-test of those waits, like cfa_selftest_wait_timeout: on `device` (-1 = current) one product is
- * launched whose loader asks for nothing, so that its other waits run out.  *status_word receives 1 when
- * every wait ended and the kernel returned; cfa_op_status is told nothing of it.  The CUDA context stays
- * usable.  Allocates and frees 17 KiB of device memory; synchronizes the device.
+ * Self-test of those waits, like cfa_selftest_wait_timeout: on `device` (-1 = current) products are
+ * launched whose loaders ask for nothing, so that their other waits run out: by single CTAs, by clusters
+ * and by pairs.  *status_word receives 1 when every wait ended, every kernel returned and each was counted;
+ * cfa_op_status is told nothing of them.  The CUDA context stays usable.  Allocates and frees 532 KiB of
+ * device memory; synchronizes the device.
  * Errors: CFA_ERR_INVAL (status_word NULL), CFA_ERR_CUDA.
  */
 cfa_status cfa_selftest_op_timeout(int device, int *status_word);

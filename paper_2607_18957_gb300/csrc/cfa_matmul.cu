@@ -47,9 +47,10 @@
  * columns, as a product in plain fp32 has).  Results of 16 bits, whose own rounding is a thousand times
  * that, are summed in one go.
  *
- * Every wait has a limit.  One that runs out is counted in what cfa_op_status reads; its CTA
- * then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
- * memory.
+ * Every wait on an mbarrier has a limit.  One that runs out is counted in what cfa_op_status reads; its
+ * CTA then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
+ * memory.  The barriers of a cluster have none: they end because every thread goes through all of its
+ * CTA's tiles and arrives at each one's barriers, whether or not a wait of its has run out.
  */
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -59,9 +60,9 @@
 
 #include <atomic>
 
-#include "cfa_tiles.h"
 #include "cfa_device.cuh"
 #include "cfa_ops.h"
+#include "cfa_tiles.h"
 
 namespace {
 
@@ -111,7 +112,7 @@ struct Args {
     uint32_t tmem_cols;
     uint32_t release;
     uint32_t polls;      /* of a wait, before it gives up */
-    uint32_t lose;       /* self-test: the loader asks for nothing */
+    uint32_t lose;       /* self-test: the loader asks for nothing, but goes through its tiles */
     uint32_t early_w;    /* w, and what tells the groups' rows, is there before the launch's wait */
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
@@ -1028,7 +1029,8 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             int32_t group = 0;
             asm volatile("fence.proxy.async.global;" ::: "memory");
             bool waited = !a.early_w;
-            for (int32_t t = a.lose ? total : begin; t < total; t += stride) {
+            const uint32_t load_to = a.lose ? k0 : k1;
+            for (int32_t t = begin; t < total; t += stride) {
                 const Tile o = tile_at(a, s, t, &group, features);
                 /* rows of x for this CTA: of a pair, each holds half of the columns in use */
                 uint32_t half = 0;
@@ -1062,7 +1064,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     launch_wait(a);
                     asm volatile("fence.proxy.async.global;" ::: "memory");
                 }
-                for (uint32_t k = k0; k < k1; k += deep) {
+                for (uint32_t k = k0; k < load_to; k += deep) {
                     const uint32_t blocks = min(deep, k1 - k);
                     const uint32_t dst = ring + at * stage;
                     /* all blocks of the stage at once, unless the one that lacks columns is among
@@ -1676,14 +1678,18 @@ cudaError_t cfa_matmul_status(int *word)
     return e;
 }
 
-/* A product of one token whose loader asks for nothing, on the default stream: its waits run out after
- * 4096 polls each.  *word receives what this has been counted as, in counts of its own. */
+/* Products of 8 tokens whose loaders ask for nothing, on the default stream, by single CTAs, by clusters
+ * of two and four and by pairs: their waits run out after 4096 polls each.  *word receives what this has
+ * been counted as, in counts of its own: 1, or the first that was counted as something else. */
 cudaError_t cfa_matmul_selftest(int *word)
 {
+    const Cut cuts[] = {{false, 16, 128, 0}, {false, 16, 128, 1}, {false, 16, 128, 2}, {true, 96, 128, 0}};
+    const size_t w_bytes = 256 * 1024 * 2, x_bytes = 8 * 1024 * 2, y_bytes = 8 * 256 * 2;
     uint8_t *buf = nullptr;
-    const size_t w_bytes = 128 * 64 * 2, x_bytes = 64 * 2, y_bytes = 128 * 2;
-    cfa_op_counts before, after;
-    cudaError_t e = cudaMemcpyFromSymbol(&before, g_counts, sizeof before, sizeof before);
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (!e && (dev < 0 || dev >= kMaxDevices)) e = cudaErrorInvalidDevice;
+    if (!e) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (!e) e = cudaMalloc(reinterpret_cast<void **>(&buf), w_bytes + x_bytes + y_bytes);
     if (e) return e;
     e = cudaMemset(buf, 0, w_bytes + x_bytes + y_bytes);
@@ -1691,13 +1697,21 @@ cudaError_t cfa_matmul_selftest(int *word)
     m.w = buf;
     m.x = buf + w_bytes;
     m.y = buf + w_bytes + x_bytes;
-    m.tokens = m.likely = m.n_groups = m.busy = m.lose = 1;
-    m.w_rows = m.y_stride = 128;
-    m.cols = m.x_stride = m.w_stride = 64;
-    if (!e) e = cfa_launch_matmul(&m, 0, 0, nullptr);
-    if (!e) e = cudaDeviceSynchronize();
-    if (!e) e = cudaMemcpyFromSymbol(&after, g_counts, sizeof after, sizeof after);
-    if (!e) *word = cfa_op_news(&before, after);
+    m.tokens = m.likely = 8;
+    m.n_groups = m.busy = m.lose = 1;
+    m.w_rows = m.y_stride = 256;
+    m.cols = m.x_stride = m.w_stride = 1024;
+    *word = 1;
+    for (const Cut &cut : cuts) {
+        cfa_op_counts before, after;
+        if (!e) e = cudaMemcpyFromSymbol(&before, g_counts, sizeof before, sizeof before);
+        if (!e) e = launch(&m, g_device[dev], sms, cut, 0, 0, nullptr);
+        if (!e) e = cudaDeviceSynchronize();
+        if (!e) e = cudaMemcpyFromSymbol(&after, g_counts, sizeof after, sizeof after);
+        if (e) break;
+        const int news = cfa_op_news(&before, after);
+        if (*word == 1) *word = news;
+    }
     const cudaError_t freed = cudaFree(buf);
     return e ? e : freed;
 }

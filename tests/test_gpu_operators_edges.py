@@ -226,3 +226,17 @@ def test_a_thread_that_asks_takes_nothing_from_another():
         other.join()
     assert words == [1] * 40
     assert told and set(told) == {0}
+
+
+def test_products_run_on_after_the_waits_of_clusters_and_pairs_ran_out():
+    """The self-test goes through single CTAs, clusters and pairs, none of which hangs or leaves anything
+    behind for the products of each kind that follow."""
+    from paper_2607_18957_gb300 import _lib
+    word = ctypes.c_int(-1)
+    assert _lib.load().cfa_selftest_op_timeout(0, ctypes.byref(word)) == 0 and word.value == 1
+    for t, n, k in ((1, 128, 4096), (16, 256, 8192), (1024, 4096, 512)):
+        x, w = normal(t, (t, k), BF16), normal(n, (n, k), BF16, k ** -0.5)
+        ref = x.double() @ w.double().t()
+        bound = (x.double().abs() @ w.double().abs().t()) * ((k + 8) * 2.0 ** -23)
+        bound = bound + 2.0 ** -8 * (ref.abs() + bound)
+        assert bool(((cfa.linear(x, w).double() - ref).abs() <= bound).all())
