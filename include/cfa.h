@@ -745,8 +745,8 @@ cfa_status cfa_op_status(void);
 
 /*
  * Self-test of those waits, like cfa_selftest_wait_timeout: on `device` (-1 = current) products are
- * launched whose loaders ask for nothing, so that their other waits run out: by single CTAs, by clusters
- * and by pairs.  *status_word receives 1 when every wait ended, every kernel returned and each was counted;
+ * launched whose loaders ask for nothing, so that their other waits run out, and products that give up
+ * with their loads in flight: by single CTAs, by clusters and by pairs.  *status_word receives 1 when every wait ended, every kernel returned and each was counted;
  * cfa_op_status is told nothing of them.  The CUDA context stays usable.  Allocates and frees 532 KiB of
  * device memory; synchronizes the device.
  * Errors: CFA_ERR_INVAL (status_word NULL), CFA_ERR_CUDA.

@@ -48,8 +48,8 @@
  * that, are summed in one go.
  *
  * Every wait on an mbarrier has a limit.  One that runs out is counted in what cfa_op_status reads; its
- * CTA then issues nothing more, lets its loads in flight end (again with a limit) and frees its tensor
- * memory.  The barriers of a cluster have none: they end because every thread goes through all of its
+ * CTA then issues nothing more, lets its loads and products in flight end (again with a limit) and frees
+ * its tensor memory.  The barriers of a cluster have none: they end because every thread goes through all of its
  * CTA's tiles and arrives at each one's barriers, whether or not a wait of its has run out.
  */
 #include <cuda.h>
@@ -112,7 +112,8 @@ struct Args {
     uint32_t tmem_cols;
     uint32_t release;
     uint32_t polls;      /* of a wait, before it gives up */
-    uint32_t lose;       /* self-test: the loader asks for nothing, but goes through its tiles */
+    uint32_t lose;       /* self-test, 1: the loader asks for nothing, but goes through its tiles; 2: all
+                            others give up at once, with its loads in flight */
     uint32_t early_w;    /* w, and what tells the groups' rows, is there before the launch's wait */
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
@@ -123,8 +124,10 @@ __device__ cfa_op_counts g_counts[2]; /* of waits that ran out; [1]: the self-te
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t acc_full[2], acc_empty[2];
+    uint64_t idle;   /* after a wait that ran out: the products are done */
     uint32_t tmem;
     uint32_t polls;
+    uint32_t issued; /* stages that the loader has asked for */
     int dead;
     int32_t total;   /* output tiles */
     int32_t group[]; /* output tiles before each group's, and rows of x before each group's, in turn */
@@ -853,19 +856,29 @@ __device__ __forceinline__ void finish_narrow(const Args &a, const float *stage,
     }
 }
 
-/* After a wait that ran out: lets the loads in flight end, as far as a limit allows.  Of a pair, the
- * first CTA's barriers count the loads of both; the second only gives its own the same time. */
-__device__ void drain(const Args &a, Shared *s, uint32_t issued, bool second)
+/* After a wait that ran out and with all warps out of their tiles, whichever of them gave up: lets the
+ * loads and the products in flight end, as far as a limit allows.  One lane of the issuer's warp, the one
+ * that has issued the products.  Of a pair, the first CTA's barriers count the loads of both and it
+ * issues the products; the second only gives its own loads the time of one such wait. */
+template <bool PAIR> __device__ void drain(const Args &a, Shared *s, bool second)
 {
     bool ended = true;
-    const uint32_t most = issued < a.stages ? issued : a.stages;
+    const uint32_t issued = s->issued;
+    uint32_t most = issued < a.stages ? issued : a.stages;
+    if (second && most > 1) most = 1;
     for (uint32_t l = issued - most; l < issued; ++l) {
         bool done = false;
         for (uint32_t k = 0; !done && k < kDrainLimit; ++k)
             done = mbar_try_wait(smem_addr(s->full + l % a.stages), (l / a.stages) & 1u);
         if (!done && !second) ended = false;
     }
-    if (!ended) atomicAdd(&g_counts[a.lose].in_flight, 1u);
+    if (!second) {
+        bool done = false;
+        commit<PAIR>(smem_addr(&s->idle));
+        for (uint32_t k = 0; !done && k < kDrainLimit; ++k) done = mbar_try_wait(smem_addr(&s->idle), 0);
+        if (!done) ended = false;
+    }
+    if (!ended) atomicAdd(&g_counts[a.lose != 0].in_flight, 1u);
 }
 
 /* A stage's blocks of w, from block k on. */
@@ -927,7 +940,9 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             mbar_init(acc_empty + 8 * lane, PAIR ? 16 : 8);
         }
         if (lane == 0) {
+            mbar_init(smem_addr(&s->idle), 1);
             s->dead = 0;
+            s->issued = 0;
             s->polls = a.polls;
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap[0]) : "memory");
@@ -1019,7 +1034,8 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps >> share;
     const bool sync_tiles = !PAIR && share > 0;
     const uint32_t deep = a.deep, stages = a.stages, part = EXACT ? kPart : a.steps;
-    bool ok = true;
+    bool ok = a.lose != 2 || warp == kLoader;
+    if (!ok && threadIdx.x == 0) *(volatile int *)&s->dead = 1;
     if (a.early_w && warp != kLoader) launch_wait(a);
 
     if (warp == kLoader) {
@@ -1029,7 +1045,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             int32_t group = 0;
             asm volatile("fence.proxy.async.global;" ::: "memory");
             bool waited = !a.early_w;
-            const uint32_t load_to = a.lose ? k0 : k1;
+            const uint32_t load_to = a.lose == 1 ? k0 : k1;
             for (int32_t t = begin; t < total; t += stride) {
                 const Tile o = tile_at(a, s, t, &group, features);
                 /* rows of x for this CTA: of a pair, each holds half of the columns in use */
@@ -1101,7 +1117,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 }
             }
             if (!waited) launch_wait(a);
-            if (*(volatile int *)&s->dead) drain(a, s, issued, PAIR && rank);
+            s->issued = issued;
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
@@ -1349,7 +1365,16 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
 
     fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *(volatile int *)&s->dead) atomicAdd(&g_counts[a.lose].ran_out, 1u);
+    if (*(volatile int *)&s->dead) {
+        if (warp == kIssuer) {
+            if (elect_one()) {
+                drain<PAIR>(a, s, PAIR && rank);
+                atomicAdd(&g_counts[a.lose != 0].ran_out, 1u);
+            }
+            __syncwarp();
+        }
+        __syncthreads();
+    }
     if constexpr (PAIR) cluster_sync();
     if (warp == kIssuer) {
         const uint32_t tmem = s->tmem;
@@ -1678,9 +1703,11 @@ cudaError_t cfa_matmul_status(int *word)
     return e;
 }
 
-/* Products of 8 tokens whose loaders ask for nothing, on the default stream, by single CTAs, by clusters
- * of two and four and by pairs: their waits run out after 4096 polls each.  *word receives what this has
- * been counted as, in counts of its own: 1, or the first that was counted as something else. */
+/* Products of 8 tokens on the default stream, by single CTAs, by clusters of two and four and by pairs:
+ * first with loaders that ask for nothing, so that waits run out after 4096 polls each, then with warps
+ * that give up while all loads of their tile (four blocks, which the ring holds) are in flight.  *word
+ * receives what this has been counted as, in counts of its own: 1, or the first that was counted as
+ * something else. */
 cudaError_t cfa_matmul_selftest(int *word)
 {
     const Cut cuts[] = {{false, 16, 128, 0}, {false, 16, 128, 1}, {false, 16, 128, 2}, {true, 96, 128, 0}};
@@ -1698,12 +1725,14 @@ cudaError_t cfa_matmul_selftest(int *word)
     m.x = buf + w_bytes;
     m.y = buf + w_bytes + x_bytes;
     m.tokens = m.likely = 8;
-    m.n_groups = m.busy = m.lose = 1;
+    m.n_groups = m.busy = 1;
     m.w_rows = m.y_stride = 256;
-    m.cols = m.x_stride = m.w_stride = 1024;
     *word = 1;
-    for (const Cut &cut : cuts) {
+    for (int i = 0; i < 8; ++i) {
+        const Cut &cut = cuts[i / 2];
         cfa_op_counts before, after;
+        m.lose = 1 + i % 2;
+        m.cols = m.x_stride = m.w_stride = m.lose == 1 ? 1024 : (int64_t)256 << cut.split;
         if (!e) e = cudaMemcpyFromSymbol(&before, g_counts, sizeof before, sizeof before);
         if (!e) e = launch(&m, g_device[dev], sms, cut, 0, 0, nullptr);
         if (!e) e = cudaDeviceSynchronize();

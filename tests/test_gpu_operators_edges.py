@@ -229,8 +229,9 @@ def test_a_thread_that_asks_takes_nothing_from_another():
 
 
 def test_products_run_on_after_the_waits_of_clusters_and_pairs_ran_out():
-    """The self-test goes through single CTAs, clusters and pairs, none of which hangs or leaves anything
-    behind for the products of each kind that follow."""
+    """The self-test goes through single CTAs, clusters and pairs, without loads and with loads that are in
+    flight when the others give up; none hangs or leaves anything behind for the products of each kind
+    that follow."""
     from paper_2607_18957_gb300 import _lib
     word = ctypes.c_int(-1)
     assert _lib.load().cfa_selftest_op_timeout(0, ctypes.byref(word)) == 0 and word.value == 1
