@@ -2,7 +2,8 @@
 the matrix product with a weight in its fused layout, the choice of experts, and the products with
 stacked experts.  Forward passes for serving; argument marshalling only.
 
-Every call enqueues on `stream` (default: torch's current stream) and returns at once.  Outputs and
+Every call enqueues on `stream` (a torch stream of the operands' device or a stream's handle; default:
+torch's current stream there) and returns at once.  Outputs and
 workspaces that a call makes come from torch's allocator, on that stream.  Operands are CUDA tensors
 of one device whose last dimension is contiguous; rows may lie any distance apart.
 """
@@ -108,6 +109,8 @@ class _On:
 
 def _elsewhere(stream, device):
     """The guard of a call that is not for the current device's current stream."""
+    if stream is not None and not isinstance(stream, int) and stream.device.index != device:
+        raise ValueError(f"the stream is on {stream.device}, the operands on cuda:{device}")
     return torch.cuda.device(device) if stream is None else _On(stream, device)
 
 
