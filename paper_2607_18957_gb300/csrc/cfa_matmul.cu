@@ -112,8 +112,8 @@ struct Args {
     uint32_t tmem_cols;
     uint32_t release;
     uint32_t polls;      /* of a wait, before it gives up */
-    uint32_t lose;       /* self-test, 1: the loader asks for nothing, but goes through its tiles; 2: all
-                            others give up at once, with its loads in flight */
+    uint32_t lose;       /* self-test, 1: the loader asks for nothing, but goes through its tiles; 2: an
+                            accumulator is full only after one more arrival than the products' */
     uint32_t early_w;    /* w, and what tells the groups' rows, is there before the launch's wait */
     uint32_t pairs;      /* y and the residual can be read and written two columns at a time */
 };
@@ -124,10 +124,10 @@ __device__ cfa_op_counts g_counts[2]; /* of waits that ran out; [1]: the self-te
 struct Shared {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t acc_full[2], acc_empty[2];
-    uint64_t idle;   /* after a wait that ran out: the products are done */
     uint32_t tmem;
     uint32_t polls;
-    uint32_t issued; /* stages that the loader has asked for */
+    uint32_t loads;  /* stages that the loader has asked for */
+    uint32_t sums;   /* accumulators that the issuer has committed */
     int dead;
     int32_t total;   /* output tiles */
     int32_t group[]; /* output tiles before each group's, and rows of x before each group's, in turn */
@@ -856,29 +856,38 @@ __device__ __forceinline__ void finish_narrow(const Args &a, const float *stage,
     }
 }
 
+/* Waits, with a limit, until use `n` of a ring's barriers is over. */
+__device__ __forceinline__ bool drained(const uint64_t *bars, uint32_t n, uint32_t ring)
+{
+    for (uint32_t k = 0; k < kDrainLimit; ++k)
+        if (mbar_try_wait(smem_addr(bars + n % ring), (n / ring) & 1u)) return true;
+    return false;
+}
+
 /* After a wait that ran out and with all warps out of their tiles, whichever of them gave up: lets the
- * loads and the products in flight end, as far as a limit allows.  One lane of the issuer's warp, the one
- * that has issued the products.  Of a pair, the first CTA's barriers count the loads of both and it
- * issues the products; the second only gives its own loads the time of one such wait. */
-template <bool PAIR> __device__ void drain(const Args &a, Shared *s, bool second)
+ * loads and the products in flight end, as far as a limit allows.  One thread.  Of a pair, the first
+ * CTA's barriers count the loads of both and it issues the products; the second only gives what it has
+ * asked for some time. */
+__device__ __noinline__ void drain(const Args &a, Shared *s, bool second)
 {
     bool ended = true;
-    const uint32_t issued = s->issued;
-    uint32_t most = issued < a.stages ? issued : a.stages;
-    if (second && most > 1) most = 1;
-    for (uint32_t l = issued - most; l < issued; ++l) {
-        bool done = false;
-        for (uint32_t k = 0; !done && k < kDrainLimit; ++k)
-            done = mbar_try_wait(smem_addr(s->full + l % a.stages), (l / a.stages) & 1u);
-        if (!done && !second) ended = false;
+    if (second) {
+        for (int k = 0; k < 100; ++k) __nanosleep(10000);
+    } else {
+        const uint32_t loads = s->loads, sums = s->sums;
+        for (uint32_t n = loads < a.stages ? 0 : loads - a.stages; n < loads; ++n)
+            ended = drained(s->full, n, a.stages) && ended;
+        for (uint32_t n = sums < 2 ? 0 : sums - 2; n < sums; ++n) {
+            if (a.lose == 2) /* the arrival that the epilogue was left waiting for */
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(
+                                 smem_addr(s->acc_full + n % 2))
+                             : "memory");
+            ended = drained(s->acc_full, n, 2) && ended;
+        }
     }
-    if (!second) {
-        bool done = false;
-        commit<PAIR>(smem_addr(&s->idle));
-        for (uint32_t k = 0; !done && k < kDrainLimit; ++k) done = mbar_try_wait(smem_addr(&s->idle), 0);
-        if (!done) ended = false;
-    }
-    if (!ended) atomicAdd(&g_counts[a.lose != 0].in_flight, 1u);
+    cfa_op_counts &counts = g_counts[a.lose != 0];
+    if (!ended) atomicAdd(&counts.in_flight, 1u);
+    atomicAdd(&counts.ran_out, 1u);
 }
 
 /* A stage's blocks of w, from block k on. */
@@ -936,13 +945,12 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
             mbar_init(empty + 8 * lane, 1);
         }
         if (lane < 2) {
-            mbar_init(acc_full + 8 * lane, 1);
+            mbar_init(acc_full + 8 * lane, a.lose == 2 ? 2 : 1);
             mbar_init(acc_empty + 8 * lane, PAIR ? 16 : 8);
         }
         if (lane == 0) {
-            mbar_init(smem_addr(&s->idle), 1);
             s->dead = 0;
-            s->issued = 0;
+            s->loads = s->sums = 0;
             s->polls = a.polls;
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.wmap) : "memory");
             asm volatile("prefetch.tensormap [%0];" ::"l"(&a.xmap[0]) : "memory");
@@ -1034,8 +1042,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     const uint32_t k1 = PAIR ? a.steps : (rank + 1) * a.steps >> share;
     const bool sync_tiles = !PAIR && share > 0;
     const uint32_t deep = a.deep, stages = a.stages, part = EXACT ? kPart : a.steps;
-    bool ok = a.lose != 2 || warp == kLoader;
-    if (!ok && threadIdx.x == 0) *(volatile int *)&s->dead = 1;
+    bool ok = true;
     if (a.early_w && warp != kLoader) launch_wait(a);
 
     if (warp == kLoader) {
@@ -1117,7 +1124,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                 }
             }
             if (!waited) launch_wait(a);
-            s->issued = issued;
+            s->loads = issued;
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
@@ -1128,6 +1135,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     } else if (warp == kIssuer) {
         if (elect_one()) {
             uint32_t at = 0, phase = 0, buf = 0, buf_phase = 1;
+            uint32_t sums = 0;
             int32_t group = 0;
             const uint32_t tmem = s->tmem;
             /* descriptors count in 16 bytes */
@@ -1177,6 +1185,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                         }
                         if (!ok) break;
                         commit<PAIR>(acc_full + 8 * buf);
+                        ++sums;
                         if (buf) buf_phase ^= 1;
                         buf ^= 1;
                     }
@@ -1186,6 +1195,11 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                     cluster_done();
                 }
             }
+            if (!ok) { /* of a sum that was given up: its products count as one */
+                commit<PAIR>(acc_full + 8 * buf);
+                ++sums;
+            }
+            s->sums = sums;
         } else if (sync_tiles) {
             for (int32_t t = begin; t < total; t += stride) {
                 cluster_sync();
@@ -1366,13 +1380,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
     fence_before();
     __syncthreads();
     if (*(volatile int *)&s->dead) {
-        if (warp == kIssuer) {
-            if (elect_one()) {
-                drain<PAIR>(a, s, PAIR && rank);
-                atomicAdd(&g_counts[a.lose != 0].ran_out, 1u);
-            }
-            __syncwarp();
-        }
+        if (threadIdx.x == 0) drain(a, s, PAIR && rank);
         __syncthreads();
     }
     if constexpr (PAIR) cluster_sync();
@@ -1549,7 +1557,7 @@ cudaError_t launch(const cfa_matmul *m, Device &d, int sms, const Cut &cut, int 
     a.outs = gated ? m->w_rows / 2 : m->w_rows;
     a.steps = (uint32_t)((m->cols + kDepth - 1) / kDepth);
     a.release = (uint32_t)release;
-    a.polls = m->lose ? 4096 : kSpinLimit;
+    a.polls = m->lose == 0 ? kSpinLimit : m->lose == 1 ? 4096 : 0;
     a.lose = m->lose;
     a.early_w = m->w_ready && !pair;
     a.bn = cut.bn;
@@ -1704,9 +1712,9 @@ cudaError_t cfa_matmul_status(int *word)
 }
 
 /* Products of 8 tokens on the default stream, by single CTAs, by clusters of two and four and by pairs:
- * first with loaders that ask for nothing, so that waits run out after 4096 polls each, then with warps
- * that give up while all loads of their tile (four blocks, which the ring holds) are in flight.  *word
- * receives what this has been counted as, in counts of its own: 1, or the first that was counted as
+ * first with loaders that ask for nothing, so that waits run out after 4096 polls each, then with
+ * epilogues that give up at once, while all loads of the tile (four blocks, which the ring holds) are on
+ * their way.  *word receives what this has been counted as, in counts of its own: 1, or the first that was counted as
  * something else. */
 cudaError_t cfa_matmul_selftest(int *word)
 {

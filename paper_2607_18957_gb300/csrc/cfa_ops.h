@@ -37,7 +37,7 @@ typedef struct cfa_matmul {
     int64_t bias_up;  /* gated: where the up rows' bias starts, in elements */
     int32_t act, gated;
     int32_t exact;    /* 1: the sums are rounded as fp32 results are to be */
-    int32_t lose;     /* self-test, 1: the kernel's loads are not issued, 2: its other warps give up */
+    int32_t lose;     /* self-test, 1: the loads are not issued, 2: the epilogue gives up */
     int32_t busy;     /* groups that can hold rows at all (host's bound) */
     int64_t likely;   /* rows to expect in all groups, at most `tokens` */
 } cfa_matmul;
