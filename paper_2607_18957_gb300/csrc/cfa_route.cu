@@ -248,15 +248,19 @@ __global__ void __launch_bounds__(kWarps * 32) cfa_route_kernel(const cfa_route_
 #pragma unroll
         for (int r = 0; r < R; ++r) key[r] = v[r];
     }
+    /* What cannot be chosen, NaN among it, is -inf from here on: fminf and fmaxf give the other one of
+     * a NaN and a number, and a NaN key would count its group's best key twice.  (Without a bias a key
+     * is NaN only where its logit is.) */
     if (a.bias) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) key[r] += b[r];
+        for (int r = 0; r < R; ++r) {
+            key[r] += b[r];
+            if (!(key[r] > -INFINITY)) key[r] = -INFINITY;
+        }
     }
-    /* what cannot be chosen, NaN among it, is -inf from here on: fminf and fmaxf give the other one of
-     * a NaN and a number, and a NaN key would count its group's best key twice */
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        if (!(v[r] > -INFINITY && key[r] > -INFINITY)) key[r] = -INFINITY;
+        if (!(v[r] > -INFINITY)) key[r] = -INFINITY;
     if (a.groups > 1) keep_groups<R>(a, key, reinterpret_cast<float *>(s_key), lane, !softmax);
 
     uint32_t k[R], best = 0; /* the lane's best key, its place and its logit */
