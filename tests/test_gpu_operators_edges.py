@@ -113,8 +113,8 @@ def route_row(row, bias, top_k, scoring, groups, top_groups):
 
 
 def check_groups(z, top_k, scoring, bias, groups, top_groups):
-    """Keys without a bias are fp32 values below 1, at most three units of 2^-24 off, their sums seven: choices
-    that are 2^-20 apart have to be the definition's, and with a bias (below 4) those 2^-18 apart."""
+    """Keys without a bias are fp32 values below 1, at most three units of 2^-24 off, their sums seven:
+    choices that are 2^-20 apart have to be the definition's, and with a bias (below 4) those 2^-18 apart."""
     near = 2.0 ** -20 if bias is None else 2.0 ** -18
     w, i = cfa.route(z, top_k, scoring=scoring, bias=bias, groups=groups, top_groups=top_groups)
     b = None if bias is None else bias.double().cpu().tolist()
@@ -241,3 +241,38 @@ def test_products_run_on_after_the_waits_of_clusters_and_pairs_ran_out():
         bound = (x.double().abs() @ w.double().abs().t()) * ((k + 8) * 2.0 ** -23)
         bound = bound + 2.0 ** -8 * (ref.abs() + bound)
         assert bool(((cfa.linear(x, w).double() - ref).abs() <= bound).all())
+
+
+# ---- uneven experts -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("t,e,top_k,first,held", [(512, 16, 4, 0, 16), (300, 32, 6, 8, 8),
+                                                  (1100, 8, 2, 0, 8)])
+def test_experts_of_which_one_has_many_times_its_share(t, e, top_k, first, held):
+    """Most tokens name the first expert that is held, the rest is spread: its rows go through several
+    tiles that were cut for the average.  A product's sum is off by at most (K + 8) 2^-23 of its terms'
+    magnitudes, SiLU by 2^-16 of its argument and 1.2 times the argument's error, the activated values
+    and the result by half a unit in the last place (2^-8)."""
+    h, i = 136, 72
+    g = torch.Generator(device="cuda").manual_seed(t)
+    ids = torch.rand(t, e, generator=g, device="cuda").topk(top_k, dim=1).indices
+    hot = (torch.rand(t, generator=g, device="cuda") < 0.9) & ~(ids == first).any(dim=1)
+    ids[:, 0] = torch.where(hot, first, ids[:, 0])
+    weights = torch.rand(t, top_k, generator=g, device="cuda")
+    x = normal(t + 1, (t, h), BF16)
+    w13, w2 = normal(2, (held, 2 * i, h), BF16, h ** -0.5), normal(3, (held, h, i), BF16, i ** -0.5)
+    y = cfa.experts(x, ids.int(), weights, w13, w2, first_expert=first).double()
+    ref, bound = torch.zeros_like(y), torch.zeros_like(y)
+    u = 2.0 ** -23
+    for k in range(held):
+        tok, j = torch.where(ids == first + k)
+        xk, w, d = x[tok].double(), w13[k].double(), w2[k].double()
+        v, ev = xk @ w.t(), (xk.abs() @ w.abs().t()) * ((h + 8) * u)
+        a, ea = v[:, :i] / (1 + torch.exp(-v[:, :i])), 1.2 * ev[:, :i] + 2.0 ** -16 * v[:, :i].abs()
+        m, em = a * v[:, i:], ea * v[:, i:].abs() + (a.abs() + ea) * ev[:, i:]
+        em = em + (2.0 ** -8 + u) * (m.abs() + em)
+        o, eo = m @ d.t(), em @ d.abs().t() + ((m.abs() + em) @ d.abs().t()) * ((i + 8) * u)
+        s = weights[tok, j].double()[:, None]
+        ref.index_add_(0, tok, o * s)
+        bound.index_add_(0, tok, (eo + (top_k + 2) * u * o.abs()) * s)
+    bound = bound + 2.0 ** -8 * (ref.abs() + bound)
+    assert bool(((y - ref).abs() <= bound).all())
