@@ -599,14 +599,17 @@ cfa_status cfa_segment_range(uint64_t blob_bytes, uint64_t chunk_bytes, int32_t 
  *     and the operators on that stream see its parameters;
  *   - matrices are row-major with a row stride in elements (>= the row's length where there is more
  *     than one row); dtype is BF16 or F16 where not said otherwise, the same for x and the weights;
- *   - products and sums are held in fp32; results are rounded to nearest even, once, to y's dtype;
+ *   - products and sums are held in fp32 (the tensor cores cut each sum's last bits off: fp32 results
+ *     are off by 2.3e-7 at 4096 columns, a product in plain fp32 by 1.9e-7); results are rounded to
+ *     nearest even, once, to y's dtype;
  *   - zero tokens are valid and write nothing;
  *   - infinities and NaN go through the formulas; nothing reads outside the matrices, whatever the
  *     values (of ids too);
  *   - cfa_last_error(NULL) on the calling thread gives the detail of a refusal.
  * Errors of all three: CFA_ERR_INVAL (NULL pointer, size or stride out of range, unknown constant,
  * workspace too small), CFA_ERR_DTYPE (dtype not supported there), CFA_ERR_ALIGN, CFA_ERR_OVERLAP
- * (y overlaps an input; y may be the residual itself, same address and stride), CFA_ERR_CUDA.
+ * (y overlaps an input; y may be the residual itself, same address and stride; a matrix counts from its
+ * first element to its last, so that columns of one larger matrix overlap), CFA_ERR_CUDA.
  */
 #define CFA_ACT_NONE      0
 #define CFA_ACT_RELU      1
@@ -709,7 +712,8 @@ cfa_status cfa_route_async(const cfa_route_args *args, cfa_stream stream);
  *   workspace device memory of cfa_experts_workspace() bytes, 256-byte aligned; calls that may
  *             overlap need their own
  * hidden and inter are multiples of 8 and w13 and w2 of 16 bytes (CFA_ERR_ALIGN).  The activated
- * values are rounded once to dtype between the two products; experts are summed in fp32.
+ * values are rounded once to dtype between the two products, as the tensor cores take them: in F16 a
+ * value above 65,504 becomes infinite there.  Experts are summed in fp32.
  */
 typedef struct cfa_experts_args {
     const void *x, *w13, *w2, *residual;

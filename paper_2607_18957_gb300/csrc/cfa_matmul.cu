@@ -22,35 +22,39 @@
  *
  * What bounds it, and what it takes on one GB300 (bf16, weights from memory, not from L2):
  *   many tokens: the tensor cores.  2048 tokens, gated 28,672 x 4096: the tensor pipe is active in 95 %
- *     of the cycles, 4096 tokens take 480 us (2.0 PFLOP/s) in a burst and 550 (1.75) under the power
+ *     of the cycles, 4096 tokens take 475 us (2.0 PFLOP/s) in a burst and 550 (1.75) under the power
  *     limit, as cuBLAS does.
  *   few tokens: memory, 128 weight rows a stage and 150 to 200 KiB a CTA on their way.  One token,
- *     gated 28,672 x 4096 (235 MB): 37.5 us (6.3 TB/s); 57,344 x 4096: 70 us (6.7 TB/s).
- *   few tokens and a small weight: start and end.  A launch of one block takes 3.0 us, 50 MB
- *     12.4 us (7.4 at the rate of memory), 117 MB 22 us (17).
- * What made the difference, in the order it was found: stores of pairs of columns without a branch
- * between them (1078 -> 562 us on 4096 x 28,672 x 4096); one elected lane for loads and for products,
- * which lets the compiler keep their operands in uniform registers (0.31 -> 0.18 us a block), and a
- * look at the next stage's barrier before the products of this one (0.25 -> 0.21); one load for all
- * blocks of a stage instead of one or, gated, four per block (627 -> 447 us on the gate/up product);
- * loads before the tensor memory is there and the epilogue's code warmed up under them (4.0 -> 3.0 us
- * for one block); eight epilogue warps instead of four (88 -> 65 us on 2247 tokens, gated 16,384 x
- * 1280 with SiLU); tiles turned round in shared memory and stored 16 bytes at a time, or 4 where rows
- * lie off that grid, by kernels that hold no other way to store (62 -> 56 there; 2206 tokens x 6359 x
- * 392 with a residual 81 -> 37, x 6360 42 -> 27); rings of three stages or more beside a cluster's sums
- * (256 tokens x 4096 x 14,336 47 -> 37).
+ *     gated 28,672 x 4096 (235 MB): 38.8 us (6.1 TB/s); 57,344 x 4096: 72 us (6.5 TB/s); 128,256 x 4096
+ *     (1.05 GB): 152 us (6.9 TB/s).
+ *   few tokens and a small weight: start and end.  A launch of one block takes 3.1 us, 50 MB
+ *     12.9 us (7.4 at the rate of memory), 117 MB 22.5 us (17).
+ *   short rows: the epilogue.  2048 x 6400 x 64 takes 14.6 us, 2206 x 6360 x 392 with a residual 32, x
+ *     6359 46 (results and residuals from memory).
+ * What made the difference, in the order it was found, with the times of then: stores of pairs of
+ * columns without a branch between them (1078 -> 562 us on 4096 x 28,672 x 4096); one elected lane for
+ * loads and for products, which lets the compiler keep their operands in uniform registers (0.31 ->
+ * 0.18 us a block), and a look at the next stage's barrier before the products of this one (0.25 ->
+ * 0.21); one load for all blocks of a stage instead of one or, gated, four per block (627 -> 447 us on
+ * the gate/up product); loads before the tensor memory is there and the epilogue's code warmed up under
+ * them (4.0 -> 3.0 us for one block); eight epilogue warps instead of four (88 -> 65 us on 2247 tokens,
+ * gated 16,384 x 1280 with SiLU); tiles turned round in shared memory and stored 16 bytes at a time, or
+ * 4 where rows lie off that grid, by kernels that hold no other way to store (62 -> 56 there; 2206
+ * tokens x 6359 x 392 with a residual 81 -> 37, x 6360 42 -> 27); rings of three stages or more beside
+ * a cluster's sums (256 tokens x 4096 x 14,336 47 -> 37).
  *
  * exact: the tensor cores add in fp32, but cut each sum's last bits off where IEEE addition rounds, so
- * that an fp32 result is off by half a unit in the last place per addition in the same direction
- * (1e-6 after 64 of them: 1024 columns).  For fp32 results the accumulator therefore takes parts of
- * 256 columns, which the epilogue adds with rounding in a third place of tensor memory (2.3e-7 at 4096
- * columns, as a product in plain fp32 has).  Results of 16 bits, whose own rounding is a thousand times
- * that, are summed in one go.
+ * that an fp32 result is off by half a unit in the last place per addition in the same direction (1e-6
+ * after 64 of them: 1024 columns).  For fp32 results the accumulator therefore takes parts of 256
+ * columns, which the epilogue adds with rounding in a third place of tensor memory (2.3e-7 at 4096
+ * columns, where a product in plain fp32 has 1.9e-7).  Results of 16 bits, whose own rounding is a
+ * thousand times that, are summed in one go.
  *
  * Every wait on an mbarrier has a limit.  One that runs out is counted in what cfa_op_status reads; its
  * CTA then issues nothing more, lets its loads and products in flight end (again with a limit) and frees
- * its tensor memory.  The barriers of a cluster have none: they end because every thread goes through all of its
- * CTA's tiles and arrives at each one's barriers, whether or not a wait of its has run out.
+ * its tensor memory.  (The longest sum that a call can ask for, 2^31 columns, takes 0.94 s and stays
+ * inside the limit.)  The barriers of a cluster have none: they end because every thread goes through all
+ * of its CTA's tiles and arrives at each one's barriers, whether or not a wait of its has run out.
  */
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -623,9 +627,9 @@ __device__ __forceinline__ void finish(const Args &a, float (&all)[16], const Pl
 /* A batch of 16 tokens by way of shared memory, in which token j's sums of the warp's 32 weight rows lie
  * side by side from word j * kStageRow on (four words more than they are, so that 16-byte reads of
  * neighbouring tokens meet different banks).  The registers hold 16 tokens of one column: stored from
- * there, each store writes 64 bytes of two tokens at most, after an exchange with the next lane.  A lane takes 16 bytes of y at a time: 8 columns of 2 bytes
- * or 4 of 4, of the tokens lane / CHUNKS + i * STEP. */
-
+ * there, each store writes 64 bytes of two tokens at most, after an exchange with the next lane.  Here a
+ * lane takes 16 bytes of y at a time: 8 columns of 2 bytes or 4 of 4, of the tokens lane / CHUNKS + i *
+ * STEP. */
 template <bool GATED, bool F32> struct Wide {
     static constexpr int COLS = F32 ? 4 : 8, CHUNKS = (GATED ? 16 : 32) / COLS;
     static constexpr int ITEMS = kBatch * CHUNKS / 32, STEP = 32 / CHUNKS;
@@ -1341,11 +1345,11 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                         sum_load(src + c, sum + c, EXACT && more, v);
                     } else {
                         float p[4][16]; /* all on their way before the first is added */
-    #pragma unroll
+#pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const uint32_t from = map_to(base, dry ? rank : (uint32_t)r % sharers) +
                                                   (uint32_t)c * (kRows * 4u);
-    #pragma unroll
+#pragma unroll
                             for (int j = 0; j < 16; ++j) {
                                 p[r][j] = 0.0f;
                                 if (r < sharers && j < c1 - c)
@@ -1354,7 +1358,7 @@ __global__ void __launch_bounds__(kThreads, 1) cfa_matmul_kernel(const __grid_co
                                                  : "r"(from + (uint32_t)j * (kRows * 4u)));
                             }
                         }
-    #pragma unroll
+#pragma unroll
                         for (int j = 0; j < 16; ++j)
                             v[j] = ((p[0][j] + p[1][j]) + p[2][j]) + p[3][j];
                     }
@@ -1714,8 +1718,8 @@ cudaError_t cfa_matmul_status(int *word)
 /* Products of 8 tokens on the default stream, by single CTAs, by clusters of two and four and by pairs:
  * first with loaders that ask for nothing, so that waits run out after 4096 polls each, then with
  * epilogues that give up at once, while all loads of the tile (four blocks, which the ring holds) are on
- * their way.  *word receives what this has been counted as, in counts of its own: 1, or the first that was counted as
- * something else. */
+ * their way.  *word receives what this has been counted as, in counts of its own: 1, or the first that
+ * was counted as something else. */
 cudaError_t cfa_matmul_selftest(int *word)
 {
     const Cut cuts[] = {{false, 16, 128, 0}, {false, 16, 128, 1}, {false, 16, 128, 2}, {true, 96, 128, 0}};

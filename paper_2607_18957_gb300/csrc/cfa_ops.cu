@@ -386,7 +386,9 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     m.tokens = p.pairs;
     m.n_groups = a->experts;
     m.busy = (int32_t)(p.pairs < a->experts ? p.pairs : a->experts);
-    /* experts before the first are other ranks': their share of the pairs is not here */
+    /* Experts before the first are other ranks': their share of the pairs is not here.  How many come
+     * behind the last is not known, so that lower ranks are cut for more rows than come (32 of 128
+     * experts, 512 tokens: 70.5, 68.7, 66.6 and 68.0 us on ranks 0 to 3).  A guess for the cut alone. */
     m.likely = p.pairs * a->experts / ((int64_t)a->first_expert + a->experts);
     if (m.likely < m.busy) m.likely = m.busy;
     m.f16 = a->dtype == CFA_DTYPE_F16;
@@ -395,6 +397,10 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     m.w = a->w13;
     m.w_rows = rows13;
     m.cols = m.w_stride = a->hidden;
+    /* The activated values are rounded to x's type: the tensor cores take the second product's operands
+     * in 16 bits, and in 32 they would be split in two and multiplied twice.  Against 64 bits the result
+     * is off by 1.4 times what its own rounding makes (bf16 0.0024 instead of 0.0017); in f16 values
+     * above 65,504 become infinite. */
     m.y = ws + p.mid;
     m.y_stride = a->inter;
     m.act = a->activation;
@@ -417,6 +423,8 @@ extern "C" cfa_status cfa_experts_async(const cfa_experts_args *a, cfa_stream st
     m.w = a->w2;
     m.w_rows = a->hidden;
     m.cols = m.w_stride = a->inter;
+    /* The products of each choice stay in fp32 until they are summed; not `exact`, since the sum is
+     * rounded to 16 bits, a thousand times what the accumulator's truncation costs. */
     m.y = ws + p.part;
     m.y_stride = a->hidden;
     m.y_f32 = 1;

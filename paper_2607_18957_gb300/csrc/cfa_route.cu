@@ -7,12 +7,12 @@
  * The lane that has just given its best needs the next one.  With few logits per lane it goes through
  * them alone; from kShared on its keys, which lie in shared memory, go one to a lane and the warp takes
  * their largest: the others would wait for that lane's loop anyway (4096 tokens over 128 experts, eight
- * choices: 4.9 -> 4.2 us; 256 experts 7.3 -> 5.3).
+ * choices: 4.9 -> 4.2 us when it was built, 3.5 now; 256 experts 7.3 -> 5.3, 4.0 now).
  *
  * Bound by the launch and by the chain of loads, exponentials and top_k warp reductions of one token,
  * and beyond some thousand tokens by the instructions of that chain; the bytes would take a tenth.
- * One token over 8 experts 1.5 us beside the launch, 4099 tokens over 256 experts in 8 groups with a
- * bias 6.7 us, 16,384 tokens over 128 experts 10.0 us.  What made the difference there: neighbouring
+ * One token over 8 experts 1.5 us in a row of launches, 4099 tokens over 256 experts in 8 groups with a
+ * bias 6.3 us, 16,384 tokens over 128 experts 9.7 us.  What made the difference there: neighbouring
  * logits in a lane instead of every 32nd (13.8 -> 8.1 us without a bias), the bias through L1 (3.2 us
  * less), and a warp brought together again before its shuffles (1.1 us less: lanes that a branch has
  * parted trade values one by one).

@@ -297,6 +297,8 @@ def experts(x, ids, weights, w13, w2, *, activation="silu", first_expert=0, resi
               experts first_expert .. first_expert + E - 1, as loaded.  Other ids add nothing
     residual  [..., H] of x's dtype; `out` may be the same tensor
     workspace  uint8 tensor (default: allocated; its size is cfa_experts_workspace of cfa.h)
+    The values act(gate_e x) * (up_e x) are rounded to x's dtype between the two products (fp16: above
+    65,504 they become infinite).
     """
     if torch is None:
         _start()
