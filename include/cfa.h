@@ -80,6 +80,7 @@ typedef int cfa_status;
 #define CFA_DTYPE_I64   6
 #define CFA_DTYPE_F64   7
 #define CFA_DTYPE_I16   8
+#define CFA_DTYPE_F8_E4M3 9 /* in caches of the operators alone: loads move such tensors as U8 */
 
 #define CFA_MAX_DIMS    8
 #define CFA_MAX_LAYERS  65536
@@ -736,6 +737,111 @@ typedef struct cfa_experts_args {
 cfa_status cfa_experts_workspace(const cfa_experts_args *args, uint64_t *bytes);
 cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
 
+/* ---- operators of a decoding step around the products ------------------------------------- */
+
+/*
+ * Norms between blocks, on rows of cols values:
+ *   a = x, or with a post_weight (a norm behind the block) N(x) * (offset + post_weight)
+ *   a = a * act(gate)                    where there is a gate
+ *   h = residual + scale * a             (without a residual: scale * a)
+ *   y = N(h) * (offset + weight),        N(v) = v / sqrt(mean(v^2) + eps)
+ *
+ *   x, residual, gate, y, h   [tokens, cols] of dtype (BF16, F16 or F32).  residual, gate, post_weight
+ *             and h may be NULL.  A gate_stride of 0 gives every token the same gate
+ *   weight, post_weight   [cols] of weight_dtype (dtype or F32)
+ * Everything is held in fp32 (a square above 3.4e38 is infinite there, and y then 0); y is computed from
+ * h before h is rounded.  y and h may each be x, residual or gate, same address and stride (a gate only
+ * with a stride of its own); they do not overlap each other or any other operand.  At most
+ * CFA_NORM_MAX_COLS columns (CFA_ERR_INVAL).
+ */
+#define CFA_NORM_MAX_COLS 16384
+typedef struct cfa_norm_args {
+    const void *x, *residual, *gate, *weight, *post_weight;
+    void *y, *h;
+    int64_t tokens, cols;
+    int64_t x_stride, residual_stride, gate_stride, y_stride, h_stride;
+    int32_t dtype, weight_dtype;
+    int32_t activation; /* CFA_ACT_*, of the gate */
+    uint32_t flags;     /* 0 */
+    float scale, eps, offset;
+    int32_t reserved;   /* 0 */
+} cfa_norm_args;
+cfa_status cfa_norm_async(const cfa_norm_args *args, cfa_stream stream);
+
+/*
+ * A cache of keys or values in pages, for cfa_append and cfa_attend: the value d of head h of the token
+ * at place i of page p lies at element p * page_stride + i * token_stride + h * head_stride + d.  Whatever
+ * the order of the dimensions, strides are positive, no two values share an element, and keys and
+ * values share none.  A token's slot is p * page_size + i.
+ */
+
+#define CFA_APPEND_INTERLEAVED 0x1u
+#define CFA_HEAD_DIM_MAX 512
+
+/*
+ * Turns the queries and keys of new tokens by their positions and appends keys and values to the cache.
+ *
+ *   qkv       [tokens, (heads + 2 kv_heads) * head_dim] of dtype (BF16 or F16): a token's query heads,
+ *             key heads, value heads, as the product with a fused q/k/v weight gives them
+ *   positions [tokens], frequencies [rotary_dim / 2] in radians per position, in 64 bits; both NULL (and
+ *             rotary_dim 0): nothing turns.  The pair i of the first rotary_dim values of a head, (i, i +
+ *             rotary_dim / 2) or with CFA_APPEND_INTERLEAVED (2 i, 2 i + 1), turns by position *
+ *             frequencies[i]: (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  The angle is exact to
+ *             2^-53 of the frequency times the position, sine and cosine are in fp32
+ *   slots     [tokens]: where a token's keys and values go.  One below 0 or behind the last page: they go
+ *             nowhere.  Two tokens with the same slot leave values of either
+ *   q         [tokens, heads * head_dim] of dtype, the turned queries; may be qkv, same address and
+ *             stride.  NULL: not wanted
+ *   k_cache, v_cache   of cache_dtype: dtype, or F8_E4M3, which holds values divided by k_scale or
+ *             v_scale (> 0), beyond +-448 as +-448.  With dtype the scales are 1
+ * head_dim is a multiple of 8 up to CFA_HEAD_DIM_MAX, rotary_dim even and at most head_dim.  Everything is
+ * held in fp32 and rounded once.
+ */
+typedef struct cfa_append_args {
+    const void *qkv;
+    const int32_t *positions, *slots;
+    const double *frequencies;
+    void *q, *k_cache, *v_cache;
+    int64_t tokens, qkv_stride, q_stride;
+    int64_t k_page_stride, k_token_stride, k_head_stride;
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+    int32_t pages, page_size;
+    int32_t heads, kv_heads, head_dim, rotary_dim;
+    int32_t dtype, cache_dtype;
+    uint32_t flags; /* CFA_APPEND_* */
+    float magnitude, k_scale, v_scale;
+} cfa_append_args;
+cfa_status cfa_append_async(const cfa_append_args *args, cfa_stream stream);
+
+#define CFA_LOGPROBS_MAX_TOP 32
+
+/*
+ * Log probabilities: with z = scale * logits and p = softmax(z) of each row of cols values
+ *   logprobs[r]  = log p at tokens[r];  0 for a token below 0 (a padded row), NaN for one >= cols
+ *   entropy[r]   = -sum p log p
+ *   top_ids, top_logprobs [rows, top]   the top largest logits in descending order, of equal ones the
+ *                  lowest index first, and their log probabilities
+ * A logit of -inf has the probability 0.  In a row of -inf alone the log probabilities are -inf and the
+ * entropy is 0.  NaN or +inf makes a row's numbers NaN; among the ids a NaN ranks as -inf.
+ *
+ *   logits    [rows, cols] of dtype (BF16, F16 or F32);  tokens [rows]
+ *   logprobs, entropy [rows], top_logprobs and top_ids [rows, top], contiguous; the last two NULL with
+ *             top 0
+ * scale > 0 is the inverse temperature.  Sums are held in fp32.
+ */
+typedef struct cfa_logprobs_args {
+    const void *logits;
+    const int32_t *tokens;
+    float *logprobs, *entropy, *top_logprobs;
+    int32_t *top_ids;
+    int64_t rows, cols, stride;
+    int32_t dtype;
+    int32_t top; /* 0 .. min(cols, CFA_LOGPROBS_MAX_TOP) */
+    float scale;
+    uint32_t flags; /* 0 */
+} cfa_logprobs_args;
+cfa_status cfa_logprobs_async(const cfa_logprobs_args *args, cfa_stream stream);
+
 /*
  * The products wait for their own loads and for one another inside a kernel, each time with a limit.
  * Returns CFA_OK if no wait has run out on the current device since the calling thread's last call
@@ -786,7 +892,8 @@ const char *cfa_status_name(cfa_status st);
 
 /* sizeof of the ABI struct with this name ("cfa_tensor_entry", "cfa_dst", "cfa_plan_opts",
  * "cfa_source", "cfa_stats", "cfa_piece", "cfa_st_tensor", "cfa_chunk_times", "cfa_linear_args",
- * "cfa_route_args", "cfa_experts_args"), or 0 for an unknown name; lets a binding check its
+ * "cfa_route_args", "cfa_experts_args", "cfa_norm_args",
+ * "cfa_append_args", "cfa_logprobs_args"), or 0 for an unknown name; lets a binding check its
  * own copies of the layouts.  Host-only. */
 size_t cfa_abi_sizeof(const char *type_name);
 

@@ -121,12 +121,15 @@ SIGNATURES = {
     "cfa_file_source_close": (ctypes.c_int, [_P]),
     "cfa_selftest_wait_timeout": (ctypes.c_int, [ctypes.c_int, _P]),
     "cfa_get_timeline": (ctypes.c_int, [_P, _P, _SZ]),
-    # the operators' structs are packed by ops.py and passed as bytes
+    # the operators' structs are packed by ops.py and step.py and passed as bytes
     "cfa_linear_workspace": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_linear_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_route_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_experts_workspace": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_experts_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_norm_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_append_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_logprobs_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_op_status": (ctypes.c_int, []),
     "cfa_selftest_op_timeout": (ctypes.c_int, [ctypes.c_int, _P]),
 }
@@ -160,8 +163,9 @@ def _check_layouts(lib):
             "cfa_stats": ctypes.sizeof(Stats), "cfa_piece": ctypes.sizeof(Piece),
             "cfa_st_tensor": ST_TENSOR_DTYPE.itemsize,
             "cfa_chunk_times": 16}
-    from . import ops
+    from . import ops, step
     want.update(ops.SIZES)
+    want.update(step.SIZES)
     for name, size in want.items():
         got = lib.cfa_abi_sizeof(name.encode())
         if got != size:

@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libcfa.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CU_SOURCES = ["cfa_unpack.cu", "cfa_bulk.cu", "cfa_runtime.cu", "cfa_noalloc.cu", "cfa_ops.cu",
-              "cfa_route.cu", "cfa_sort.cu", "cfa_matmul.cu"]
+              "cfa_route.cu", "cfa_sort.cu", "cfa_matmul.cu", "cfa_step.cu", "cfa_norm.cu",
+              "cfa_append.cu", "cfa_logprobs.cu"]
 C_SOURCES = ["cfa_plan.c", "cfa_files.c"]
 
 
@@ -30,7 +31,8 @@ def _nvcc():
 
 def _sources():
     return [os.path.join(CSRC, f) for f in CU_SOURCES + C_SOURCES +
-            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h", "cfa_tiles.h"]] + \
+            ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h", "cfa_tiles.h",
+             "cfa_checks.h", "cfa_values.cuh"]] + \
         [os.path.join(INCLUDE, "cfa.h")]
 
 

@@ -99,4 +99,8 @@ typedef struct cfa_rows {
 } cfa_rows;
 cudaError_t cfa_launch_realign(const cfa_rows *m, int n, cudaStream_t stream);
 
+cudaError_t cfa_launch_norm(const cfa_norm_args *a, cudaStream_t stream);
+cudaError_t cfa_launch_append(const cfa_append_args *a, cudaStream_t stream);
+cudaError_t cfa_launch_logprobs(const cfa_logprobs_args *a, cudaStream_t stream);
+
 #endif /* CFA_OPS_H */

@@ -1,0 +1,296 @@
+"""Operators of a decoding step around the products (cfa_norm_async, cfa_append_async and
+cfa_logprobs_async of cfa.h): the norms between blocks, the rotation of queries and keys with the way of
+keys and values into a paged cache, and the log probabilities of tokens.  Forward passes for serving;
+argument marshalling only.
+
+As the operators of ops.py, the calls enqueue on `stream` (a torch stream of the operands' device or a
+stream's handle; default: torch's current stream there) and return at once; outputs and workspaces that
+a call makes come from torch's allocator, on that stream.
+"""
+import math
+import struct
+
+from . import _lib, ops
+from .ops import ACTIVATION, _check, _code, _elsewhere, _on, _one_of, _rows
+
+__all__ = ["norm", "append", "logprobs", "rotary_frequencies"]
+
+F8_E4M3 = 9  # CFA_DTYPE_F8_E4M3
+INTERLEAVED = 0x1
+
+_NORM = struct.Struct("<7Q7q3iI3fi")
+_APPEND = struct.Struct("<7Q9q8iI3f")
+_LOGPROBS = struct.Struct("<6Q3q2ifI")
+SIZES = {"cfa_norm_args": _NORM.size, "cfa_append_args": _APPEND.size,
+         "cfa_logprobs_args": _LOGPROBS.size}
+
+
+def _like(t, name, device, shape, dtype, cols):
+    """(address, row stride) of an operand that is shaped and typed like another."""
+    _on(t, name, device)
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
+    return t.data_ptr(), _rows(t, name, cols)[1]
+
+
+def norm(x, weight, *, residual=None, gate=None, activation="silu", post_weight=None, scale=1.0,
+         eps=1e-6, offset=0.0, out=None, stream=None):
+    """N(h) * (offset + weight) of h = residual + scale * act(gate) * a, N(v) = v / sqrt(mean(v^2) + eps):
+    y, or with a residual (y, h).
+
+    x         [..., C] bf16, fp16 or fp32: what the block gave
+    a         x, or with a post_weight (a norm behind the block) N(x) * (offset + post_weight)
+    gate      like x, or [C]: multiplies a by activation(gate) ("none", "relu", "gelu", "gelu_tanh",
+              "silu")
+    residual  like x: the stream that the block adds to
+    weight, post_weight  [C], both of x's dtype or both fp32
+    out       y, or with a residual (y, h), to write into: each may be x, the residual or a gate like x
+    """
+    if ops.torch is None:
+        ops._start()
+    torch = ops.torch
+    device = x.get_device()
+    _on(x, "x", device)
+    if stream is not None or device != ops._device():
+        with _elsewhere(stream, device):
+            return norm(x, weight, residual=residual, gate=gate, activation=activation,
+                        post_weight=post_weight, scale=scale, eps=eps, offset=offset, out=out)
+    shape, dtype = x.shape, x.dtype
+    cols = shape[-1] if shape else 0
+    if len(shape) == 2 and cols:
+        t, xs = shape[0], x.stride(0)
+    else:
+        t, xs = _rows(x, "x", cols)
+    code = _code(x, "x")
+    _on(weight, "weight", device)
+    if weight.shape != (cols,):
+        raise ValueError(f"weight: shape {tuple(weight.shape)}, not ({cols},)")
+    wcode = _code(weight, "weight")
+    pp = rp = rs = gp = gs = hp = hs = act = 0
+    if post_weight is not None:
+        _on(post_weight, "post_weight", device)
+        if post_weight.shape != (cols,) or post_weight.dtype is not weight.dtype:
+            raise ValueError(f"post_weight: {post_weight.dtype} {tuple(post_weight.shape)}, not "
+                             f"{weight.dtype} ({cols},)")
+        pp = post_weight.data_ptr()
+    if gate is not None:
+        act = _one_of(ACTIVATION, activation, "activation")
+        if gate.shape == (cols,) and len(shape) > 1:
+            _on(gate, "gate", device)
+            if gate.dtype is not dtype:
+                raise ValueError(f"gate: {gate.dtype}, not {dtype}")
+            gp = gate.data_ptr()
+        else:
+            gp, gs = _like(gate, "gate", device, shape, dtype, cols)
+    if residual is not None:
+        rp, rs = _like(residual, "residual", device, shape, dtype, cols)
+    y = h = None
+    if out is None:
+        y = torch.empty(shape, dtype=dtype, device=x.device)
+        ys = cols
+        if residual is not None:
+            h = torch.empty(shape, dtype=dtype, device=x.device)
+            hp, hs = h.data_ptr(), cols
+        yp = y.data_ptr()
+    else:
+        if residual is not None:
+            y, h = out
+            hp, hs = _like(h, "h", device, shape, dtype, cols)
+        else:
+            y = out
+        yp, ys = _like(y, "y", device, shape, dtype, cols)
+    st = ops._lib_c.cfa_norm_async(
+        _NORM.pack(x.data_ptr(), rp, gp, weight.data_ptr(), pp, yp, hp, t, cols, xs, rs, gs, ys, hs,
+                   code, wcode, act, 0, scale, eps, offset, 0), ops._raw_stream(device))
+    if st:
+        _check(st)
+    return y if residual is None else (y, h)
+
+
+def rotary_frequencies(dim, base=10000.0, *, scaling=None, factor=1.0, length=None, low=1.0, high=4.0,
+                       fast=32.0, slow=1.0, magnitude=None):
+    """Frequencies of append() for `dim` rotated values of a head: (a list of dim / 2 radians per
+    position, magnitude).  base ** (-2 i / dim), and for contexts `factor` times longer
+
+    scaling   None; "linear": every frequency divided by factor; "base": a larger base, so that the last
+              frequency is divided by factor and the first by one; "bands": with t the turns that a
+              pair makes within `length` positions, pairs of t >= high keep their frequency, those of
+              t <= low have it divided, between them smoothly; "ramp": the same, linear in the pair's
+              index between those that turn `fast` and `slow` times, and queries and keys grow by
+              `magnitude` (default 0.1 ln factor + 1)
+    """
+    if dim < 2 or dim % 2:
+        raise ValueError(f"{dim} values do not make pairs")
+    if not (base > 1.0 and factor >= 1.0):
+        raise ValueError(f"base {base}, factor {factor}")
+    half = dim // 2
+    if scaling == "base" and dim > 2:
+        base = base * factor ** (dim / (dim - 2))
+    f = [base ** (-i / half) for i in range(half)]
+    grow = 1.0
+    if scaling == "linear":
+        f = [v / factor for v in f]
+    elif scaling in ("bands", "ramp"):
+        if not length:
+            raise ValueError(f"scaling {scaling!r} goes by the length of the original contexts")
+        if scaling == "bands":
+            kept = [(length * v / (2 * math.pi) - low) / (high - low) for v in f]
+        else:
+            def index(turns):
+                return half * math.log(length / (turns * 2 * math.pi)) / math.log(base)
+            first, last = max(math.floor(index(fast)), 0), min(math.ceil(index(slow)), half - 1)
+            kept = [1.0 - (i - first) / max(last - first, 1e-3) for i in range(half)]
+            grow = 0.1 * math.log(factor) + 1.0
+        kept = [min(max(k, 0.0), 1.0) for k in kept]
+        f = [v * (k + (1.0 - k) / factor) for v, k in zip(f, kept)]
+    elif scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}: one of linear, base, bands, ramp")
+    return f, grow if magnitude is None else magnitude
+
+
+def _ints(t, name, device, shape):
+    """The address of an int32 operand."""
+    torch = ops.torch
+    _on(t, name, device)
+    if t.shape != shape or t.dtype is not torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, not a contiguous torch.int32 "
+                         f"{tuple(shape)}")
+    return t.data_ptr()
+
+
+def _cache(k, v, dtype, code, device):
+    """Checks a paged cache: (its dtype's code, the strides of k and of v)."""
+    torch = ops.torch
+    _on(k, "k_cache", device)
+    _on(v, "v_cache", device)
+    if len(k.shape) != 4 or v.shape != k.shape or v.dtype is not k.dtype:
+        raise ValueError(f"k_cache {k.dtype} {tuple(k.shape)} and v_cache {v.dtype} {tuple(v.shape)} "
+                         "are both [pages, page_size, kv_heads, head_dim]")
+    if k.dtype is not dtype:
+        if k.dtype is not torch.float8_e4m3fn:
+            raise ValueError(f"the cache is {k.dtype}, not {dtype} or torch.float8_e4m3fn")
+        code = F8_E4M3
+    return code, k.stride()[:3], v.stride()[:3]
+
+
+def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=None,
+           interleaved=False, magnitude=1.0, k_scale=1.0, v_scale=1.0, out=None, stream=None):
+    """Turns queries and keys by their positions and appends keys and values to a paged cache: the
+    turned queries [T, heads, D].
+
+    qkv       [T, (heads + 2 KV) D] bf16 or fp16, as linear() gives it with a fused q/k/v weight
+    k_cache, v_cache  [pages, page_size, KV, D] of any strides with D contiguous, of qkv's dtype or
+              torch.float8_e4m3fn, which holds values divided by k_scale or v_scale
+    slots     [T] int32, page * page_size + place; a token whose slot is negative or behind the last page
+              is not appended
+    positions [T] int32;  frequencies [R / 2] fp64, radians per position (rotary_frequencies()): the first
+              R <= D values of a head turn, in pairs (i, i + R / 2) or, interleaved, (2 i, 2 i + 1),
+              and grow by `magnitude`.  Without them nothing turns, and the result is qkv's own part
+    out       [T, heads, D] to write the queries into; may be qkv's own part
+    """
+    if ops.torch is None:
+        ops._start()
+    torch = ops.torch
+    device = qkv.get_device()
+    _on(qkv, "qkv", device)
+    if stream is not None or device != ops._device():
+        with _elsewhere(stream, device):
+            return append(qkv, k_cache, v_cache, slots, heads=heads, positions=positions,
+                          frequencies=frequencies, interleaved=interleaved, magnitude=magnitude,
+                          k_scale=k_scale, v_scale=v_scale, out=out)
+    dtype = qkv.dtype
+    code = _code(qkv, "qkv")
+    ccode, ks, vs = _cache(k_cache, v_cache, dtype, code, device)
+    pages, page_size, kv, dim = k_cache.shape
+    if heads < 1 or len(qkv.shape) != 2 or qkv.shape[1] != (heads + 2 * kv) * dim:
+        raise ValueError(f"qkv: {tuple(qkv.shape)}, not rows of ({heads} + 2 * {kv}) * {dim}")
+    t, xs = qkv.shape[0], qkv.stride(0)
+    sp = _ints(slots, "slots", device, (t,))
+    if (positions is None) != (frequencies is None):
+        raise ValueError("positions and frequencies belong together")
+    pp = fp = qp = qs = rot = 0
+    if positions is not None:
+        pp = _ints(positions, "positions", device, (t,))
+        _on(frequencies, "frequencies", device)
+        if frequencies.dtype is not torch.float64 or len(frequencies.shape) != 1:
+            raise ValueError(f"frequencies: {frequencies.dtype} {tuple(frequencies.shape)}, not "
+                             "torch.float64 (R / 2,)")
+        rot = 2 * frequencies.shape[0]
+        fp = frequencies.data_ptr()
+    shape = (t, heads, dim)
+    if out is not None:
+        _on(out, "out", device)
+        if out.shape != shape or out.dtype is not dtype or (heads > 1 and out.stride(1) != dim):
+            raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, not {dtype} {shape} with rows of "
+                             f"{heads * dim}")
+        q, qp, qs = out, out.data_ptr(), out.stride(0)
+    elif rot:
+        q = torch.empty(shape, dtype=dtype, device=qkv.device)
+        qp, qs = q.data_ptr(), heads * dim
+    else:
+        q = qkv[:, :heads * dim].unflatten(1, (heads, dim))
+    st = ops._lib_c.cfa_append_async(
+        _APPEND.pack(qkv.data_ptr(), pp, sp, fp, qp, k_cache.data_ptr(), v_cache.data_ptr(), t, xs, qs,
+                     *ks, *vs, pages, page_size, heads, kv, dim, rot, code, ccode,
+                     INTERLEAVED if interleaved else 0, magnitude, k_scale, v_scale),
+        ops._raw_stream(device))
+    if st:
+        _check(st)
+    return q
+
+
+def logprobs(logits, tokens, *, top=0, scale=1.0, out=None, stream=None):
+    """Log probabilities of a token per row under softmax(scale * logits): (logprobs, entropy), fp32
+    [...]; with top > 0 also (.., top_logprobs fp32 [..., top], top_ids int32 [..., top]), the largest
+    logits in descending order, equal ones by their index.
+
+    logits    [..., V] bf16, fp16 or fp32;  tokens [...] int32: below 0 gives 0 (a padded row)
+    top       0 to 32;  scale  the inverse temperature
+    out       the same tuple to write into
+    """
+    if ops.torch is None:
+        ops._start()
+    torch = ops.torch
+    device = logits.get_device()
+    _on(logits, "logits", device)
+    if stream is not None or device != ops._device():
+        with _elsewhere(stream, device):
+            return logprobs(logits, tokens, top=top, scale=scale, out=out)
+    shape = logits.shape
+    if len(shape) == 2 and shape[1]:
+        rows, cols = shape
+        xs = logits.stride(0)
+    else:
+        cols = shape[-1] if shape else 0
+        rows, xs = _rows(logits, "logits", cols)
+    code = _code(logits, "logits")
+    lead = shape[:-1]
+    tp = _ints(tokens, "tokens", device, lead)
+    top = int(top)
+    if out is None:
+        on = logits.device
+        out = (torch.empty(lead, dtype=torch.float32, device=on),
+               torch.empty(lead, dtype=torch.float32, device=on))
+        if top:
+            if top < 0:
+                raise ValueError(f"top is {top}")
+            out += (torch.empty(lead + (top,), dtype=torch.float32, device=on),
+                    torch.empty(lead + (top,), dtype=torch.int32, device=on))
+    else:
+        out = tuple(out)
+        want = [(lead, torch.float32), (lead, torch.float32)]
+        if top:
+            want += [(lead + (top,), torch.float32), (lead + (top,), torch.int32)]
+        if len(out) != len(want):
+            raise ValueError(f"out: {len(out)} tensors, not {len(want)}")
+        for o, (sh, dt) in zip(out, want):
+            _on(o, "out", device)
+            if o.shape != sh or o.dtype is not dt or not o.is_contiguous():
+                raise ValueError(f"out: {o.dtype} {tuple(o.shape)}, not a contiguous {dt} {tuple(sh)}")
+    st = ops._lib_c.cfa_logprobs_async(
+        _LOGPROBS.pack(logits.data_ptr(), tp, out[0].data_ptr(), out[1].data_ptr(),
+                       out[2].data_ptr() if top else 0, out[3].data_ptr() if top else 0, rows, cols, xs,
+                       code, top, scale, 0), ops._raw_stream(device))
+    if st:
+        _check(st)
+    return out
