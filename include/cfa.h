@@ -813,6 +813,52 @@ typedef struct cfa_append_args {
 } cfa_append_args;
 cfa_status cfa_append_async(const cfa_append_args *args, cfa_stream stream);
 
+/*
+ * Attention of new tokens over the cache: new_tokens (1 for a decoding step, a few for drafted tokens) of
+ * each sequence, whose keys and values are in the cache already.  Token i of sequence s sees the keys j
+ * with j <= lengths[s] - new_tokens + i, with window > 0 only the last `window` of them:
+ *   out = sum_j p_j v_j,  p = softmax(scale * q . k_j) over the keys that it sees
+ *   lse = log sum_j exp(scale * q . k_j)
+ * Query heads h * heads / kv_heads .. share the key head h.
+ *
+ *   q, out    [sequences * new_tokens, heads * head_dim] of dtype (BF16 or F16); lse [sequences *
+ *             new_tokens, heads] contiguous, or NULL
+ *   k_cache, v_cache   of cache_dtype: dtype, or F8_E4M3, whose values count k_scale and v_scale times
+ *   pages     [sequences, max_pages]: key j of sequence s is in page pages[s, j / page_size] at place j %
+ *             page_size.  The keys of a page whose number is not in [0, cache_pages) are not there
+ *             (pages that a window has left behind, for instance)
+ *   lengths   [sequences]: keys of each, the new tokens' among them; below 0 counts as 0, above max_pages *
+ *             page_size as that
+ *   workspace device memory of cfa_attend_workspace() bytes, 256-byte aligned; calls that may overlap
+ *             need their own.  Its size goes by the head_dim and the heads alone
+ * A row that sees no key gets 0 and -inf; so does one whose scores all are -inf.  Whatever lies in
+ * keys and values that a row does not see, NaN included, does not come into it.  Scores, maxima, sums and
+ * out are held in fp32; probabilities enter the second product as sums of two 16-bit values (in F16, or with
+ * an 8-bit cache, those below 2^-28 of a row's largest count as 0).
+ * head_dim is 64, 96, 128 or 256; q, out and the caches lie on the 16-byte grid with all their strides
+ * (CFA_ERR_ALIGN).  max_pages * page_size is at most 2^30.
+ */
+typedef struct cfa_attend_args {
+    const void *q, *k_cache, *v_cache;
+    const int32_t *pages, *lengths;
+    void *out;
+    float *lse;
+    void *workspace;
+    uint64_t workspace_bytes;
+    int64_t sequences, q_stride, out_stride, pages_stride;
+    int64_t k_page_stride, k_token_stride, k_head_stride;
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+    int32_t new_tokens, max_pages, cache_pages, page_size;
+    int32_t heads, kv_heads, head_dim, window;
+    int32_t dtype, cache_dtype;
+    uint32_t flags; /* 0 */
+    float scale, k_scale, v_scale;
+} cfa_attend_args;
+
+/* Workspace bytes that cfa_attend_async needs for these sizes (host-only). */
+cfa_status cfa_attend_workspace(const cfa_attend_args *args, uint64_t *bytes);
+cfa_status cfa_attend_async(const cfa_attend_args *args, cfa_stream stream);
+
 #define CFA_LOGPROBS_MAX_TOP 32
 
 /*
@@ -893,7 +939,7 @@ const char *cfa_status_name(cfa_status st);
 /* sizeof of the ABI struct with this name ("cfa_tensor_entry", "cfa_dst", "cfa_plan_opts",
  * "cfa_source", "cfa_stats", "cfa_piece", "cfa_st_tensor", "cfa_chunk_times", "cfa_linear_args",
  * "cfa_route_args", "cfa_experts_args", "cfa_norm_args",
- * "cfa_append_args", "cfa_logprobs_args"), or 0 for an unknown name; lets a binding check its
+ * "cfa_append_args", "cfa_attend_args", "cfa_logprobs_args"), or 0 for an unknown name; lets a binding check its
  * own copies of the layouts.  Host-only. */
 size_t cfa_abi_sizeof(const char *type_name);
 

@@ -14,9 +14,9 @@ memory and streams only, and is imported lazily.
     ck = plan.checksums()
 
 linear, route and experts compute with what a load has written (ops.py): the product with a fused
-weight, the choice of experts, the products with stacked experts.  norm, append and logprobs are what a
-decoding step runs around the products (step.py): the norms between blocks, the rotation of queries and
-keys and the way into a paged cache, the log probabilities of tokens.
+weight, the choice of experts, the products with stacked experts.  norm, append, attend and logprobs are
+what a decoding step runs around the products (step.py): the norms between blocks, the rotation of queries
+and keys and the way into a paged cache, the attention over it, the log probabilities of tokens.
 """
 import contextlib
 import ctypes
@@ -28,11 +28,12 @@ import numpy as np
 from . import _lib
 from ._lib import ALL, DTYPE, ENTRY_DTYPE, DST_DTYPE, PIECE_DTYPE  # noqa: F401
 from .ops import experts, linear, op_status, route
-from .step import append, logprobs, norm, rotary_frequencies
+from .step import append, attend, logprobs, norm, rotary_frequencies
 
 __all__ = ["Plan", "Source", "FileSource", "Safetensors", "StTensor", "CfaError", "make_entries",
            "make_dsts", "ALL", "library_path", "segment_range", "AllGather", "linear", "route",
-           "experts", "op_status", "norm", "append", "logprobs", "rotary_frequencies"]
+           "experts", "op_status", "norm", "append", "attend", "logprobs",
+           "rotary_frequencies"]
 
 
 class CfaError(RuntimeError):

@@ -129,6 +129,8 @@ SIGNATURES = {
     "cfa_experts_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_norm_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_append_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_attend_workspace": (ctypes.c_int, [ctypes.c_char_p, _P]),
+    "cfa_attend_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_logprobs_async": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "cfa_op_status": (ctypes.c_int, []),
     "cfa_selftest_op_timeout": (ctypes.c_int, [ctypes.c_int, _P]),

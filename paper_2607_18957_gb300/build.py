@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libcfa.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CU_SOURCES = ["cfa_unpack.cu", "cfa_bulk.cu", "cfa_runtime.cu", "cfa_noalloc.cu", "cfa_ops.cu",
               "cfa_route.cu", "cfa_sort.cu", "cfa_matmul.cu", "cfa_step.cu", "cfa_norm.cu",
-              "cfa_append.cu", "cfa_logprobs.cu"]
+              "cfa_append.cu", "cfa_logprobs.cu", "cfa_attend_bf16.cu", "cfa_attend_f16.cu",
+              "cfa_attend_bf16_f8.cu", "cfa_attend_f16_f8.cu"]
 C_SOURCES = ["cfa_plan.c", "cfa_files.c"]
 
 
@@ -32,7 +33,7 @@ def _nvcc():
 def _sources():
     return [os.path.join(CSRC, f) for f in CU_SOURCES + C_SOURCES +
             ["cfa_internal.h", "cfa_pool.h", "cfa_device.cuh", "cfa_ops.h", "cfa_tiles.h",
-             "cfa_checks.h", "cfa_values.cuh"]] + \
+             "cfa_checks.h", "cfa_values.cuh", "cfa_attend.cuh"]] + \
         [os.path.join(INCLUDE, "cfa.h")]
 
 

@@ -1,0 +1,7 @@
+/* The attention's kernels for bf16 queries over a cache of the same type (cfa_attend.cuh). */
+#include "cfa_attend.cuh"
+
+cudaError_t cfa_launch_attend_bf16(const cfa_attend_work *w, cudaStream_t stream)
+{
+    return cfa_attend_dev::launch_any<__nv_bfloat16, false>(*w, stream);
+}

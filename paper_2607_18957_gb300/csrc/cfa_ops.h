@@ -103,4 +103,18 @@ cudaError_t cfa_launch_norm(const cfa_norm_args *a, cudaStream_t stream);
 cudaError_t cfa_launch_append(const cfa_append_args *a, cudaStream_t stream);
 cudaError_t cfa_launch_logprobs(const cfa_logprobs_args *a, cudaStream_t stream);
 
+#define CFA_ATTEND_BLOCKS 152 /* of a launch, one to an SM */
+typedef struct cfa_attend_work {
+    cfa_attend_args a;
+    int32_t group, row_tiles; /* query heads of a key head; tiles of a sequence and key head */
+    int32_t nt, pad;          /* a tile has 8 nt rows */
+    float *parts;             /* [CFA_ATTEND_BLOCKS][2] partials */
+    int64_t *ends;            /* [CFA_ATTEND_BLOCKS][2]: the tile inside which a block's share begins and
+                               * the one inside which it ends, -1 for none */
+} cfa_attend_work;
+cudaError_t cfa_launch_attend_bf16(const cfa_attend_work *w, cudaStream_t stream);
+cudaError_t cfa_launch_attend_f16(const cfa_attend_work *w, cudaStream_t stream);
+cudaError_t cfa_launch_attend_bf16_f8(const cfa_attend_work *w, cudaStream_t stream);
+cudaError_t cfa_launch_attend_f16_f8(const cfa_attend_work *w, cudaStream_t stream);
+
 #endif /* CFA_OPS_H */

@@ -1485,6 +1485,7 @@ size_t cfa_abi_sizeof(const char *type_name)
     if (!std::strcmp(type_name, "cfa_route_args")) return sizeof(cfa_route_args);
     if (!std::strcmp(type_name, "cfa_experts_args")) return sizeof(cfa_experts_args);
     if (!std::strcmp(type_name, "cfa_norm_args")) return sizeof(cfa_norm_args);
+    if (!std::strcmp(type_name, "cfa_attend_args")) return sizeof(cfa_attend_args);
     if (!std::strcmp(type_name, "cfa_append_args")) return sizeof(cfa_append_args);
     if (!std::strcmp(type_name, "cfa_logprobs_args")) return sizeof(cfa_logprobs_args);
     return 0;

@@ -183,6 +183,133 @@ extern "C" cfa_status cfa_append_async(const cfa_append_args *a, cfa_stream stre
     return cuda_result("cfa_append", cfa_launch_append(a, reinterpret_cast<cudaStream_t>(stream)));
 }
 
+/* ---- attend ---- */
+
+namespace {
+
+constexpr int64_t kMostKeys = 1ll << 30; /* of a sequence */
+
+struct AttendPlan {
+    cfa_attend_work w;
+    uint64_t ends, total; /* bytes */
+};
+
+cfa_status attend_plan(const cfa_attend_args *a, AttendPlan *p)
+{
+    if (!a) return refuse(CFA_ERR_INVAL, "cfa_attend: NULL arguments");
+    if (!is_half(a->dtype)) return refuse(CFA_ERR_DTYPE, "cfa_attend: q is bf16 or f16");
+    if (a->head_dim != 64 && a->head_dim != 96 && a->head_dim != 128 && a->head_dim != 256)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: heads of %d: 64, 96, 128 or 256", a->head_dim);
+    if (a->heads < 1 || a->heads > 8192 || a->kv_heads < 1 || a->heads % a->kv_heads ||
+        a->new_tokens < 1 || a->new_tokens > 1 << 20)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: %d heads over %d, %d new tokens", a->heads,
+                      a->kv_heads, a->new_tokens);
+    p->w = {};
+    p->w.a = *a;
+    p->w.group = a->heads / a->kv_heads;
+    const int64_t rows = (int64_t)p->w.group * a->new_tokens;
+    p->w.nt = rows <= 8 ? 1 : 2;
+    const int64_t row_tiles = (rows + 8 * p->w.nt - 1) / (8 * p->w.nt);
+    if (row_tiles * a->kv_heads >= kMost) return refuse(CFA_ERR_INVAL, "cfa_attend: too many rows");
+    p->w.row_tiles = (int32_t)row_tiles;
+    /* a partial: O of 8 nt rows, their maxima and sums */
+    const uint64_t part = 4ull * (8 * p->w.nt) * (a->head_dim + 2);
+    p->ends = aligned(sizeof(int64_t) * 2 * CFA_ATTEND_BLOCKS);
+    p->total = p->ends + aligned(part * 2 * CFA_ATTEND_BLOCKS);
+    return CFA_OK;
+}
+
+} // namespace
+
+extern "C" cfa_status cfa_attend_workspace(const cfa_attend_args *a, uint64_t *bytes)
+{
+    if (!bytes) return refuse(CFA_ERR_INVAL, "cfa_attend_workspace: NULL output");
+    AttendPlan p;
+    const cfa_status st = attend_plan(a, &p);
+    *bytes = st ? 0 : p.total;
+    return st;
+}
+
+extern "C" cfa_status cfa_attend_async(const cfa_attend_args *a, cfa_stream stream_)
+{
+    AttendPlan p;
+    cfa_status st = attend_plan(a, &p);
+    if (st) return st;
+    st = scales_ok("cfa_attend", a->dtype, a->cache_dtype, a->k_scale, a->v_scale);
+    if (st) return st;
+    if (!size_ok(a->sequences, 0) || a->max_pages < 0 || a->cache_pages < 1 || a->page_size < 1 ||
+        (int64_t)a->max_pages * a->page_size > kMostKeys)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: %lld sequences of %d pages of %d, %d in the cache",
+                      (long long)a->sequences, a->max_pages, a->page_size, a->cache_pages);
+    if (a->window < 0 || a->window > kMostKeys || a->flags || !std::isfinite(a->scale))
+        return refuse(CFA_ERR_INVAL, "cfa_attend: window %d, scale %g, flags %u", a->window, a->scale,
+                      a->flags);
+    const int64_t slots = (int64_t)a->max_pages * a->page_size / 16 + 1;
+    const int64_t tiles = (int64_t)p.w.row_tiles * a->kv_heads;
+    if ((unsigned __int128)slots * (uint64_t)tiles * (uint64_t)a->sequences >> 40)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: %lld sequences are too many", (long long)a->sequences);
+    const int64_t cols = (int64_t)a->heads * a->head_dim, rows = a->sequences * a->new_tokens;
+    if (rows > 1 && (a->q_stride < cols || a->q_stride >= kMost || a->out_stride < cols ||
+                     a->out_stride >= kMost))
+        return refuse(CFA_ERR_INVAL, "cfa_attend: row strides %lld, %lld of rows of %lld",
+                      (long long)a->q_stride, (long long)a->out_stride, (long long)cols);
+    if (a->sequences > 1 && (a->pages_stride < a->max_pages || a->pages_stride >= kMost))
+        return refuse(CFA_ERR_INVAL, "cfa_attend: row stride %lld of %d pages",
+                      (long long)a->pages_stride, a->max_pages);
+    const uint64_t cs = a->cache_dtype == CFA_DTYPE_F8_E4M3 ? 1 : 2;
+    Cache k = {a->k_cache, a->k_page_stride, a->k_token_stride, a->k_head_stride, 0};
+    Cache v = {a->v_cache, a->v_page_stride, a->v_token_stride, a->v_head_stride, 0};
+    if ((st = cache_ok("cfa_attend", &k, a->cache_pages, a->page_size, a->kv_heads, a->head_dim, cs)) ||
+        (st = cache_ok("cfa_attend", &v, a->cache_pages, a->page_size, a->kv_heads, a->head_dim, cs)))
+        return st;
+    if (a->sequences == 0) return CFA_OK;
+    if (!a->q || !a->k_cache || !a->v_cache || !a->lengths || (!a->pages && a->max_pages) || !a->out ||
+        !a->workspace)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: NULL pointer");
+    uint64_t grid = 0;
+    for (const Cache *c : {&k, &v}) {
+        grid |= (uint64_t)(uintptr_t)c->p;
+        if (a->cache_pages > 1) grid |= (uint64_t)c->page * cs;
+        if (a->page_size > 1) grid |= (uint64_t)c->token * cs;
+        if (a->kv_heads > 1) grid |= (uint64_t)c->head * cs;
+    }
+    grid |= (uint64_t)(uintptr_t)a->q | (uint64_t)(uintptr_t)a->out;
+    if (rows > 1) grid |= (uint64_t)(a->q_stride | a->out_stride) * 2;
+    if (grid & 15)
+        return refuse(CFA_ERR_ALIGN, "cfa_attend: q, out or a cache is off the 16-byte grid");
+    if (off_grid(a->pages, 4) || off_grid(a->lengths, 4) || off_grid(a->lse, 4))
+        return refuse(CFA_ERR_ALIGN, "cfa_attend: a pointer is off its element grid");
+    if (off_grid(a->workspace, kAlign))
+        return refuse(CFA_ERR_ALIGN, "cfa_attend: the workspace must be 256-byte aligned");
+    if (a->workspace_bytes < p.total)
+        return refuse(CFA_ERR_INVAL, "cfa_attend: the workspace must hold %llu bytes",
+                      (unsigned long long)p.total);
+    uint64_t nq, no, np;
+    if (!extent(rows, cols, a->q_stride, 2, &nq) || !extent(rows, cols, a->out_stride, 2, &no) ||
+        !extent(a->sequences, a->max_pages, a->pages_stride, 4, &np))
+        return refuse(CFA_ERR_INVAL, "cfa_attend: a matrix is too large");
+    const uint64_t nl = a->lse ? (uint64_t)rows * a->heads * 4 : 0, n4 = (uint64_t)a->sequences * 4;
+    const struct {
+        const void *p;
+        uint64_t n;
+    } m[] = {{a->out, no},        {a->lse, nl},   {a->workspace, p.total}, {a->q, nq}, {k.p, k.bytes},
+             {v.p, v.bytes}, {a->pages, np}, {a->lengths, n4}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (overlap(m[i].p, m[i].n, m[j].p, m[j].n))
+                return refuse(CFA_ERR_OVERLAP,
+                              "cfa_attend: an output or the workspace overlaps another operand");
+    p.w.ends = reinterpret_cast<int64_t *>(a->workspace);
+    p.w.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a->workspace) + p.ends);
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+    const bool f16 = a->dtype == CFA_DTYPE_F16;
+    const cudaError_t e = cs == 1 ? (f16 ? cfa_launch_attend_f16_f8(&p.w, stream)
+                                         : cfa_launch_attend_bf16_f8(&p.w, stream))
+                                  : (f16 ? cfa_launch_attend_f16(&p.w, stream)
+                                         : cfa_launch_attend_bf16(&p.w, stream));
+    return cuda_result("cfa_attend", e);
+}
+
 /* ---- logprobs ---- */
 
 extern "C" cfa_status cfa_logprobs_async(const cfa_logprobs_args *a, cfa_stream stream)

@@ -1,7 +1,7 @@
-"""Operators of a decoding step around the products (cfa_norm_async, cfa_append_async and
-cfa_logprobs_async of cfa.h): the norms between blocks, the rotation of queries and keys with the way of
-keys and values into a paged cache, and the log probabilities of tokens.  Forward passes for serving;
-argument marshalling only.
+"""Operators of a decoding step around the products (cfa_norm_async, cfa_append_async, cfa_attend_async
+and cfa_logprobs_async of cfa.h): the norms between blocks, the rotation of queries and keys with the way
+of keys and values into a paged cache, the attention over that cache, and the log probabilities of
+tokens.  Forward passes for serving; argument marshalling only.
 
 As the operators of ops.py, the calls enqueue on `stream` (a torch stream of the operands' device or a
 stream's handle; default: torch's current stream there) and return at once; outputs and workspaces that
@@ -13,16 +13,19 @@ import struct
 from . import _lib, ops
 from .ops import ACTIVATION, _check, _code, _elsewhere, _on, _one_of, _rows
 
-__all__ = ["norm", "append", "logprobs", "rotary_frequencies"]
+__all__ = ["norm", "append", "attend", "logprobs", "rotary_frequencies"]
 
 F8_E4M3 = 9  # CFA_DTYPE_F8_E4M3
 INTERLEAVED = 0x1
 
 _NORM = struct.Struct("<7Q7q3iI3fi")
 _APPEND = struct.Struct("<7Q9q8iI3f")
+_ATTEND = struct.Struct("<9Q10q10iI3f")
 _LOGPROBS = struct.Struct("<6Q3q2ifI")
 SIZES = {"cfa_norm_args": _NORM.size, "cfa_append_args": _APPEND.size,
+         "cfa_attend_args": _ATTEND.size,
          "cfa_logprobs_args": _LOGPROBS.size}
+_ATTEND_BYTES = {}  # workspace bytes by a call's sizes
 
 
 def _like(t, name, device, shape, dtype, cols):
@@ -237,6 +240,101 @@ def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=N
     if st:
         _check(st)
     return q
+
+
+def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale=1.0, v_scale=1.0,
+           lse=False, out=None, workspace=None, stream=None):
+    """Attention of new tokens over a paged cache that holds their keys and values already: like q, or
+    with lse=True (that, log of the sum of the exponentials fp32 [B, (N,) heads]).
+
+    q         [B, heads, D], one new token of each of B sequences, or [B, N, heads, D], a few; bf16 or
+              fp16, D 64, 96, 128 or 256
+    k_cache, v_cache  as append() fills them; 8-bit values count k_scale and v_scale times
+    pages     [B, P] int32: key j of a sequence is in page pages[b, j // page_size] at place j % page_size.
+              The keys of a page whose number is not in the cache are not there
+    lengths   [B] int32: keys of each sequence, the new tokens' among them.  Token i of N sees those up to
+              lengths - N + i, with a window only the last `window` of them; one that sees none gets 0
+              and -inf
+    scale     of the scores (default: D ** -0.5)
+    out       like q; with lse=True (out, lse)
+    workspace  uint8 tensor (default: allocated; its size is cfa_attend_workspace of cfa.h)
+    """
+    if ops.torch is None:
+        ops._start()
+    torch = ops.torch
+    device = q.get_device()
+    _on(q, "q", device)
+    if stream is not None or device != ops._device():
+        with _elsewhere(stream, device):
+            return attend(q, k_cache, v_cache, pages, lengths, scale=scale, window=window,
+                          k_scale=k_scale, v_scale=v_scale, lse=lse, out=out, workspace=workspace)
+    shape, dtype = q.shape, q.dtype
+    code = _code(q, "q")
+    ccode, ks, vs = _cache(k_cache, v_cache, dtype, code, device)
+    cache_pages, page_size, kv, dim = k_cache.shape
+    if len(shape) == 3:
+        (b, heads, d), new = shape, 1
+        rows = q
+    elif len(shape) == 4:
+        b, new, heads, d = shape
+        rows = q.flatten(0, 1) if q.is_contiguous() else q.view(b * new, heads, d)
+    else:
+        raise ValueError(f"q: shape {tuple(shape)}")
+    if d != dim:
+        raise ValueError(f"q has heads of {d}, the cache of {dim}")
+    if heads > 1 and q.stride(-2) != dim:
+        raise ValueError("q: the heads of a token must lie side by side")
+    qs = rows.stride(0)
+    _on(pages, "pages", device)
+    if len(pages.shape) != 2 or pages.shape[0] != b or pages.dtype is not torch.int32:
+        raise ValueError(f"pages: {pages.dtype} {tuple(pages.shape)}, not torch.int32 ({b}, P)")
+    np_ = _ints(lengths, "lengths", device, (b,))
+    lp, sums = 0, None
+    if out is None:
+        o = torch.empty(shape, dtype=dtype, device=q.device)
+        os_ = heads * dim
+        if lse:
+            sums = torch.empty(shape[:-1], dtype=torch.float32, device=q.device)
+    else:
+        if lse:
+            o, sums = out
+            _on(sums, "lse", device)
+            if (sums.shape != shape[:-1] or sums.dtype is not torch.float32 or
+                    not sums.is_contiguous()):
+                raise ValueError(f"lse: {sums.dtype} {tuple(sums.shape)}, not a contiguous "
+                                 f"torch.float32 {tuple(shape[:-1])}")
+        else:
+            o = out
+        _on(o, "out", device)
+        if o.shape != shape or o.dtype is not dtype or (heads > 1 and o.stride(-2) != dim):
+            raise ValueError(f"out: {o.dtype} {tuple(o.shape)}, not {dtype} {tuple(shape)} with the heads "
+                             "of a token side by side")
+        os_ = (o if len(shape) == 3 else o.view(b * new, heads, dim)).stride(0)
+    if lse:
+        lp = sums.data_ptr()
+    if scale is None:
+        scale = dim ** -0.5
+
+    def packed(ws, size):
+        return _ATTEND.pack(
+            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), np_, o.data_ptr(),
+            lp, ws, size, b, qs, os_, pages.stride(0), *ks, *vs, new, pages.shape[1], cache_pages,
+            page_size, heads, kv, dim, window, code, ccode, 0, scale, k_scale, v_scale)
+    sizes = (new, heads, kv, dim)
+    need = _ATTEND_BYTES.get(sizes)
+    if need is None:
+        size = _lib.ctypes.c_uint64()
+        _check(ops._lib_c.cfa_attend_workspace(packed(0, 0), _lib.ctypes.byref(size)))
+        if len(_ATTEND_BYTES) >= 1024:
+            _ATTEND_BYTES.clear()
+        need = _ATTEND_BYTES[sizes] = size.value
+    workspace = ops._workspace(workspace, need, q.device)
+    st = ops._lib_c.cfa_attend_async(
+        packed(workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+        ops._raw_stream(device))
+    if st:
+        _check(st)
+    return (o, sums) if lse else o
 
 
 def logprobs(logits, tokens, *, top=0, scale=1.0, out=None, stream=None):
