@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kThreads) cfa_append_kernel(const cfa_append_a
     const int head0 = blockIdx.y * s.heads, all = a.heads + 2 * a.kv_heads;
     const int heads = min(s.heads, all - head0);
     const int half = a.rotary_dim / 2;
-    wait_for_earlier();
+    launch_in_turn();
 
     for (int i = threadIdx.x; i < n * half; i += kThreads) {
         const int t = i / half;

@@ -2,16 +2,17 @@
  * Attention of new tokens over a paged cache: o = softmax(scale q K^T) V, each row over the keys that it
  * sees.
  *
- * The keys of a sequence are cut into slots of 16.  A tile is up to 8 NT rows (new tokens times the query
+ * The keys of a sequence are cut into slots of 32.  A tile is up to 8 NT rows (new tokens times the query
  * heads that share a key head) of one sequence and key head; the slots of all tiles in a row, sequence by
  * sequence, are split evenly over the warps of all blocks, whatever the sequences' lengths, so that the
  * work is even without the host knowing a length.  Where a warp's share begins or ends inside a tile its
- * sums are joined with its neighbours': in shared memory within a block, through the workspace and by a
- * second launch between blocks.  All joins go in a fixed order.
+ * sums are joined with its neighbours': in shared memory within a block, through the workspace between
+ * blocks, by whichever of a tile's blocks comes last (none waits for another).  All joins go in a fixed
+ * order.
  *
  * A warp brings its slots into its own ring in shared memory (cp.async; rows that are not there are filled
  * with zeros and nothing is read for them) and needs no barrier with other warps.  Per slot it computes
- * S^T = K Q^T (16 keys by 8 NT rows), follows the rows' running maximum m and sum l, and adds V^T P^T to
+ * S^T = K Q^T (32 keys by 8 NT rows), follows the rows' running maximum m and sum l, and adds V^T P^T to
  * O^T (dim by 8 NT rows): with the keys along the 16 of the matrix instruction and the rows along its 8, one
  * token of a group of 8 heads fills it.
  */
@@ -27,23 +28,25 @@ namespace cfa_attend_dev {
 using namespace cfa_dev;
 
 constexpr int kBlocks = CFA_ATTEND_BLOCKS;
-constexpr int kKeys = 16; /* of a slot */
+constexpr int kLeast = 4; /* slots of a block, where there are few */
+constexpr int kKeys = 32; /* of a slot, one to a lane when they are looked up */
+constexpr int kHalves = kKeys / 16; /* of 16 keys, as the matrix instruction takes them */
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 template <int D, int NT, bool F8> struct Shape {
-    static constexpr int kWarps = D > 128 ? 4 : 8;
+    static constexpr int kWarps = D > 128 && !F8 ? 4 : 8;
     static constexpr int kTiles = D / 16;                     /* of 16 dims */
     static constexpr int kRows = 8 * NT;
     static constexpr int kRowBytes = D * (F8 ? 1 : 2);
     static constexpr int kPitch = kRowBytes + 16;             /* an odd number of 16 bytes: no conflicts */
     static constexpr int kStage = 2 * kKeys * kPitch;         /* keys, then values */
     static constexpr int kFloats = kTiles * NT * 4 * 32 + 2 * kRows; /* of a partial: O, m, l */
-    static constexpr int kRoom = (232448 - 2048) / kWarps - kFloats * 4;
+    static constexpr int kRoom = (232448 - 7168) / kWarps - kFloats * 4;
     static constexpr int kFit = kRoom / kStage;
-    static constexpr int kStages = kFit > 6 ? 6 : kFit;
+    static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kWarpBytes = kStages * kStage + kFloats * 4;
     static constexpr int kSmem = kWarps * kWarpBytes;
-    static_assert(kStages >= 2 && kStages * kStage >= kFloats * 4 && kStage % 16 == 0 &&
+    static_assert(kStages >= 1 && kStages * kStage >= kFloats * 4 && kStage % 16 == 0 &&
                   kWarpBytes % 16 == 0 && D % 32 == 0, "");
 };
 
@@ -51,7 +54,8 @@ using Work = cfa_attend_work;
 
 /* A place in the row of slots. */
 struct Place {
-    int32_t b, tile, slot; /* sequence, tile of it, slot of the tile */
+    int32_t b, kv, part;   /* sequence, key head and which of its tiles of rows */
+    int32_t slot;          /* of the tile */
     int32_t slots, first;  /* of a tile; the first slot that any row sees */
     int32_t len, low;      /* keys of the sequence; the first one that any row sees */
 };
@@ -77,9 +81,24 @@ __device__ __forceinline__ int length_of(const Work &w, int b)
     return b < w.a.sequences ? __ldcg(w.a.lengths + b) : 0;
 }
 
-__device__ __forceinline__ void cp_async(uint32_t to, const void *from, int bytes)
+/* Keys and values pass through L2 as the first to go: what the kernel comes back to (its code, the page
+ * table, partials) stays there. */
+__device__ __forceinline__ uint64_t passing()
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes)
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void cp_async(uint32_t to, const void *from, int bytes, uint64_t policy)
+{
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(to), "l"(from),
+                 "r"(bytes), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async(uint32_t to, const void *from, uint64_t policy)
+{
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to), "l"(from),
+                 "l"(policy)
                  : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -195,6 +214,27 @@ __device__ __forceinline__ float exp2_fast(float v) /* off by 2^-22; below 2^-12
     return r;
 }
 
+/* Whether an infinity or NaN is among kKeys rows of `pieces` 16 bytes in shared memory, a row to a lane. */
+template <typename T, bool F8>
+__device__ __forceinline__ bool any_special(uint32_t at, int lane, int pieces, int pitch)
+{
+    static_assert(kKeys == 32, "");
+    /* adding the second to the exponent's bits (an 8-bit value: to all but the sign's) overflows */
+    constexpr uint32_t BITS = F8 ? 0x7F7F7F7Fu : std::is_same<T, __half>::value ? 0x7C007C00u : 0x7F807F80u;
+    constexpr uint32_t ONE = F8 ? 0x01010101u : std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+    uint32_t over = 0;
+    for (int c = 0; c < pieces; ++c) {
+        uint32_t q[4];
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
+                     : "r"(at + lane * pitch + c * 16)
+                     : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) over |= (q[i] & BITS) + ONE;
+    }
+    return __any_sync(kAllLanes, (over & (F8 ? 0x80808080u : 0x80008000u)) != 0);
+}
+
 /* exp2 of the difference of two maxima, the second the larger: 0 where the first is of no key at all */
 __device__ __forceinline__ float shrink(float m, float top)
 {
@@ -203,61 +243,125 @@ __device__ __forceinline__ float shrink(float m, float top)
 
 /* Where a row's results go: rows of a tile are the new tokens' heads of one key head. */
 struct Row {
-    int64_t token; /* of all sequences' new tokens */
-    int32_t head;
+    int32_t token, head; /* of the sequence's new tokens, of all heads */
     bool here;
 };
-__device__ __forceinline__ Row row_of(const Work &w, int b, int tile, int n, int rows)
+__device__ __forceinline__ Row row_of(const Work &w, int kv, int part, int n, int rows)
 {
-    const int kv = tile / w.row_tiles, r = (tile - kv * w.row_tiles) * rows + n;
-    const int i = r / w.group;
+    const uint32_t r = part * rows + n; /* below 2^19 */
+    const uint32_t i = w.group == 1 ? r : __umulhi(r, w.group_inverse);
     Row x;
-    x.here = i < w.a.new_tokens;
-    x.token = (int64_t)b * w.a.new_tokens + i;
-    x.head = kv * w.group + r - i * w.group;
+    x.here = (int)i < w.a.new_tokens;
+    x.token = i;
+    x.head = kv * w.group + (int)r - (int)i * w.group;
     return x;
 }
 
-/* Writes 16 dims of a tile's rows: c is O^T as the matrix instruction leaves it, l its sums, m the
- * maxima in powers of two.  With an 8-bit cache the dims of a lane are 2 g and 2 g + 1 instead of g and g +
- * 8 (see below). */
-template <typename T, int NT, bool F8>
-__device__ __forceinline__ void finish(const Work &w, int b, int tile, int dims, int lane,
-                                       const float (*c)[4], const float (*m)[2], const float (*l)[2],
-                                       bool sums)
-{
-    using P = typename std::conditional<F8, __half, T>::type;
-    const int g = lane >> 2, t = lane & 3;
+/* Where a tile's results go, and its log sums, which it writes at once: m are the rows' maxima in powers
+ * of two, l their sums. */
+template <typename T, int NT, bool F8> struct Finish {
+    T *o[NT];          /* the lane's row, NULL for none */
+    float u[NT][2];    /* what its columns of O^T are multiplied by */
+
+    __device__ __forceinline__ Finish(const Work &w, int b, int kv, int part, int lane, bool sums,
+                                      const float (&m)[NT][2], const float (&l)[NT][2])
+    {
+        using P = typename std::conditional<F8, __half, T>::type;
+        const int g = lane >> 2, t = lane & 3;
+        const int64_t first = (int64_t)b * w.a.new_tokens;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const float u0 = l[nt][0] == 0.0f ? 0.0f : w.a.v_scale / l[nt][0];
-        const float u1 = l[nt][1] == 0.0f ? 0.0f : w.a.v_scale / l[nt][1];
-        float v[4] = {c[nt][0] * u0, c[nt][1] * u1, c[nt][2] * u0, c[nt][3] * u1};
-        /* rows along the lanes: two dims side by side (F8: the pairs are of every second dim) */
-        const uint32_t a0 = transposed(pack2(T(), v[0], v[1])), a1 = transposed(pack2(T(), v[2], v[3]));
-        const Row r = row_of(w, b, tile, nt * 8 + g, 8 * NT);
-        if (r.here) {
-            T *o = static_cast<T *>(w.a.out) + r.token * w.a.out_stride +
-                   (int64_t)r.head * w.a.head_dim + dims;
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) u[nt][j] = l[nt][j] == 0.0f ? 0.0f : w.a.v_scale / l[nt][j];
+            const Row r = row_of(w, kv, part, nt * 8 + g, 8 * NT);
+            o[nt] = r.here ? static_cast<T *>(w.a.out) + (first + r.token) * w.a.out_stride +
+                                 (int64_t)r.head * w.a.head_dim
+                           : nullptr;
+            if (sums && w.a.lse && g < 2) {
+                const Row s = row_of(w, kv, part, nt * 8 + 2 * t + g, 8 * NT);
+                const float top = g ? m[nt][1] : m[nt][0], sum = g ? l[nt][1] : l[nt][0];
+                if (s.here)
+                    w.a.lse[(first + s.token) * w.a.heads + s.head] =
+                        sum == 0.0f ? -INFINITY : (top + (log2f(sum) - kUp<P>)) * kLn2;
+            }
+        }
+    }
+
+    /* Writes 16 dims: c is O^T as the matrix instruction leaves it.  With an 8-bit cache the dims of a lane
+     * are 2 g and 2 g + 1 instead of g and g + 8 (see below). */
+    __device__ __forceinline__ void write(int dims, int lane, const float (*c)[4]) const
+    {
+        const int t = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            /* rows along the lanes: two dims side by side (F8: the pairs are of every second dim) */
+            const uint32_t a0 = transposed(pack2(T(), c[nt][0] * u[nt][0], c[nt][1] * u[nt][1]));
+            const uint32_t a1 = transposed(pack2(T(), c[nt][2] * u[nt][0], c[nt][3] * u[nt][1]));
+            T *const to = o[nt];
+            if (!to) continue;
             if constexpr (F8) { /* a0: dims 4 t, 4 t + 2; a1: 4 t + 1, 4 t + 3 */
                 uint2 q;
                 q.x = __byte_perm(a0, a1, 0x5410);
                 q.y = __byte_perm(a0, a1, 0x7632);
-                *reinterpret_cast<uint2 *>(o + 4 * t) = q;
+                *reinterpret_cast<uint2 *>(to + dims + 4 * t) = q;
             } else {
-                *reinterpret_cast<uint32_t *>(o + 2 * t) = a0;
-                *reinterpret_cast<uint32_t *>(o + 8 + 2 * t) = a1;
+                *reinterpret_cast<uint32_t *>(to + dims + 2 * t) = a0;
+                *reinterpret_cast<uint32_t *>(to + dims + 8 + 2 * t) = a1;
             }
         }
-        if (sums && w.a.lse && g < 2) {
-            const Row s = row_of(w, b, tile, nt * 8 + 2 * t + g, 8 * NT);
-            const float top = g ? m[nt][1] : m[nt][0], sum = g ? l[nt][1] : l[nt][0];
-            if (s.here)
-                w.a.lse[s.token * w.a.heads + s.head] =
-                    sum == 0.0f ? -INFINITY : (top + (log2f(sum) - kUp<P>)) * kLn2;
-        }
     }
-}
+};
+
+/* Sums of some of a tile's keys, to which others' are added. */
+template <int MT, int NT> struct Joined {
+    float c[MT][NT][4], top[NT][2], sum[NT][2];
+
+    __device__ __forceinline__ Joined()
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                top[nt][j] = -INFINITY;
+                sum[nt][j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) c[i][nt][j] = c[i][nt][j + 2] = 0.0f;
+            }
+    }
+
+    /* Adds a partial: of its dims those 16 of which (i & mask) == sub. */
+    __device__ __forceinline__ void add(const float *part, int sub, int mask, int lane)
+    {
+        const int t = lane & 3;
+        const float *ml = part + MT * NT * 128;
+        float f0[NT][2], f1[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float2 m1 = *reinterpret_cast<const float2 *>(ml + nt * 8 + 2 * t);
+            const float2 l1 = *reinterpret_cast<const float2 *>(ml + 8 * NT + nt * 8 + 2 * t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float mj = j ? m1.y : m1.x, both = fmaxf(top[nt][j], mj);
+                f0[nt][j] = shrink(top[nt][j], both);
+                f1[nt][j] = shrink(mj, both);
+                top[nt][j] = both;
+                sum[nt][j] = sum[nt][j] * f0[nt][j] + (j ? l1.y : l1.x) * f1[nt][j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            if ((i & mask) == sub) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float4 q = reinterpret_cast<const float4 *>(part)[(i * NT + nt) * 32 + lane];
+                    const float v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        c[i][nt][j] = c[i][nt][j] * f0[nt][j & 1] + v[j] * f1[nt][j & 1];
+                }
+            }
+    }
+};
 
 template <typename T, int D, int NT, bool F8>
 __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_kernel(const Work w)
@@ -266,145 +370,211 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
     using P = typename std::conditional<F8, __half, T>::type; /* of the probabilities and values */
     constexpr int W = S::kWarps, MT = S::kTiles, ROWS = S::kRows, STAGES = S::kStages;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t s_sum[W];
+    __shared__ uint32_t s_sum[W], s_before[W * 32];
+    __shared__ int32_t s_len[W * 32];
     __shared__ Place s_at[W + 1];     /* the borders of the warps' shares */
+    __shared__ int64_t s_id[W + 1];   /* the tile that a border lies inside, or -1 */
     __shared__ uint8_t s_part[W][2];  /* which partials there are */
-    __shared__ uint32_t s_ok[W][STAGES];
+    __shared__ int s_join[2][3];      /* whether to join a tile's parts, its first block, how many */
+    __shared__ uint32_t s_ok[W][STAGES];              /* which keys of a slot are there */
+    __shared__ const uint8_t *s_from[W][2][kKeys];    /* where they are, and their values; or NULL */
     const cfa_attend_args &a = w.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int64_t tiles = (int64_t)a.kv_heads * w.row_tiles; /* of a sequence */
-    wait_for_earlier();
+    launch_in_turn();
 
     /* ---- the block's and the warps' shares ---- */
-    const int64_t per = (a.sequences + W * 32 - 1) / (W * 32);
-    const int b0 = (int)min(tid * per, a.sequences), b1 = (int)min(b0 + per, a.sequences);
-    int64_t mine = 0;
+    const int per = (int)((a.sequences + W * 32 - 1) / (W * 32)); /* sequences of a thread */
+    const int b0 = (int)min((int64_t)tid * per, a.sequences), b1 = (int)min((int64_t)b0 + per, a.sequences);
+    uint32_t mine = 0; /* slots of a tile, summed over the sequences: below 2^31 */
+    int len = 0;
     for (int b = b0; b < b1; ++b) {
         Place p;
-        enter(w, p, length_of(w, b));
+        len = length_of(w, b);
+        enter(w, p, len);
         mine += p.slots;
     }
-    int64_t before = mine;
+    uint32_t before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(kAllLanes, before, o);
+        const uint32_t v = __shfl_up_sync(kAllLanes, before, o);
         if (lane >= o) before += v;
     }
     if (lane == 31) s_sum[warp] = before;
     if (tid < W * 2) s_part[tid >> 1][tid & 1] = 0;
     __syncthreads();
-    int64_t total = 0;
+    uint32_t sum = 0;
     before -= mine;
+#pragma unroll
     for (int i = 0; i < W; ++i) {
         if (i < warp) before += s_sum[i];
-        total += s_sum[i];
+        sum += s_sum[i];
     }
-    total *= tiles;
-    const int64_t full = (total + W - 1) / W;
-    const int blocks = full < kBlocks ? (int)full : kBlocks; /* that get any */
-    if ((int)blockIdx.x >= blocks) {
-        if (tid < 2) w.ends[blockIdx.x * 2 + tid] = -1;
-        return;
+    s_before[tid] = before;
+    s_len[tid] = len;
+    __syncthreads();
+    /* Blocks have equal shares but for one slot, and so have a block's warps; few slots go to as many
+     * blocks as have kLeast of them. */
+    const int64_t total = sum * tiles;
+    const int blocks = total < kBlocks * kLeast ? (int)(total + kLeast - 1) / kLeast : kBlocks;
+    if ((int)blockIdx.x >= blocks) return;
+    int64_t each, rest; /* slots of a block, blocks with one more */
+    if (total >> 32) {
+        each = total / blocks;
+        rest = total - each * blocks;
+    } else {
+        each = (uint32_t)total / (uint32_t)blocks;
+        rest = (uint32_t)total - (uint32_t)each * (uint32_t)blocks;
     }
-    const int64_t shares = (int64_t)blocks * W;
-    const int64_t lo = before * tiles, hi = (before + mine) * tiles;
-    for (int i = 0; i <= W; ++i) {
-        /* total * share fits: total < 2^48 */
-        const int64_t at = total * ((int64_t)blockIdx.x * W + i) / shares;
-        const bool end = at == total;
-        if (end ? tid == 0 : lo <= at && at < hi) {
-            Place p;
-            p.b = (int)a.sequences;
-            p.tile = p.slot = p.slots = p.first = p.len = p.low = 0;
-            if (!end) {
-                int64_t from = lo;
-                int b = b0;
-                for (;; ++b) {
-                    enter(w, p, length_of(w, b));
-                    if (at < from + p.slots * tiles) break;
-                    from += p.slots * tiles;
-                }
-                p.b = b;
-                p.tile = (int)((at - from) / p.slots);
-                p.slot = (int)((at - from) % p.slots);
+    const int64_t from = blockIdx.x * each + min((int64_t)blockIdx.x, rest);
+    const int64_t size = each + (blockIdx.x < rest);
+    /* Lane i, in every warp: the border between warps i - 1 and i. */
+    Place in;
+    {
+        const int64_t at = from + (size * min(lane, W)) / W;
+        in.b = (int)a.sequences;
+        in.kv = in.part = in.slot = in.slots = in.first = in.len = in.low = 0;
+        if (at < total) {
+            /* the thread whose sequences it lies in: the last one with before * tiles <= at */
+            const uint32_t q = at >> 32 ? (uint32_t)(at / tiles) : (uint32_t)at / (uint32_t)tiles;
+            int k = 0;
+#pragma unroll
+            for (int o = W * 16; o; o >>= 1)
+                if (s_before[k + o] <= q) k += o;
+            int b = k * per;
+            int64_t x = at - s_before[k] * tiles;
+            for (enter(w, in, per == 1 ? s_len[k] : length_of(w, b)); x >= in.slots * tiles;
+                 enter(w, in, length_of(w, b))) {
+                x -= in.slots * tiles;
+                ++b;
             }
-            s_at[i] = p;
+            in.b = b;
+            const int tile = (int)(x >> 32 ? x / in.slots : (uint32_t)x / (uint32_t)in.slots);
+            in.slot = (int)(x - (int64_t)tile * in.slots);
+            in.kv = tile;
+            if (w.row_tiles > 1) {
+                in.kv = tile / w.row_tiles;
+                in.part = tile - in.kv * w.row_tiles;
+            }
+        }
+        if (warp == 0 && lane <= W) {
+            s_at[lane] = in;
+            s_id[lane] = in.slot ? ((int64_t)in.b * a.kv_heads + in.kv) * w.row_tiles + in.part : -1;
         }
     }
-    __syncthreads();
-    const int64_t share = (int64_t)blockIdx.x * W + warp;
-    int count = (int)(total * (share + 1) / shares - total * share / shares);
+    int *const place_words = reinterpret_cast<int *>(&in); /* the warp's own */
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Place) / 4); ++i)
+        place_words[i] = __shfl_sync(kAllLanes, place_words[i], warp);
+    int count = (int)((size * (warp + 1)) / W - (size * warp) / W);
 
     /* ---- the warp's slots ---- */
     uint8_t *const ring = smem + warp * S::kWarpBytes;
     float *const held = reinterpret_cast<float *>(ring + STAGES * S::kStage); /* the first partial */
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-    Place in = s_at[warp], out = in; /* of the loads, of the products */
+    Place out = in; /* `in` is where the loads are, `out` where the products are */
     const uint8_t *const kc = static_cast<const uint8_t *>(a.k_cache);
     const uint8_t *const vc = static_cast<const uint8_t *>(a.v_cache);
     constexpr int ES = F8 ? 1 : 2;
 
-    /* Each lane looks one key up, one slot ahead of the loads: its page's number, -1 if it is not there. */
-    auto page_at = [&](const Place &p, int left) {
-        const int key = (p.first + p.slot) * kKeys + (lane & 15);
-        if (left <= 0 || key >= p.len || key < p.low) return -1;
-        return __ldcg(a.pages + (int64_t)p.b * a.pages_stride + key / a.page_size);
+    /* Each lane looks one key up, one slot ahead of the loads: its page's number, -1 if it is not there,
+     * and its place in the page. */
+    int to_load = count, page, place = 0;
+    auto look_up = [&] {
+        const int key = (in.first + in.slot) * kKeys + lane;
+        page = -1;
+        if (to_load > 0 && key < in.len && key >= in.low) {
+            const int n = key / a.page_size;
+            place = key - n * a.page_size;
+            page = __ldcg(a.pages + (int64_t)in.b * a.pages_stride + n);
+        }
     };
     auto advance = [&](Place &p) {
         if (++p.slot < p.slots) return;
         p.slot = 0;
-        if (++p.tile < tiles) return;
-        p.tile = 0;
+        if (++p.part < w.row_tiles) return;
+        p.part = 0;
+        if (++p.kv < a.kv_heads) return;
+        p.kv = 0;
         ++p.b;
         enter(w, p, length_of(w, p.b));
     };
-    int to_load = count, page = page_at(in, to_load);
-    auto load = [&](int stage) {
-        if (to_load > 0) {
-            const int key = (in.first + in.slot) * kKeys + (lane & 15), place = key % a.page_size;
-            const int kv = in.tile / w.row_tiles;
+    /* A slot's keys or values, 16 bytes a lane: neighbouring lanes take a row's pieces. */
+    const uint64_t policy = passing();
+    auto bring = [&](uint32_t to, const uint8_t *const *from, bool all, const uint8_t *any) {
+        constexpr int CH = S::kRowBytes / 16;
+        constexpr int SIDE = CH % 8 == 0 ? 8 : CH % 4 == 0 ? 4 : 2, ROWS = 32 / SIDE;
+        static_assert(CH % SIDE == 0, "");
+        const int c0 = lane % SIDE, r0 = lane / SIDE;
+        to += r0 * S::kPitch + c0 * 16;
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < kKeys / ROWS; ++i) {
+                const uint8_t *at = from[i * ROWS + r0] + c0 * 16;
+#pragma unroll
+                for (int c = 0; c < CH; c += SIDE)
+                    cp_async(to + i * ROWS * S::kPitch + c * 16, at + c * 16, policy);
+            }
+        } else {
+#pragma unroll 2
+            for (int i = 0; i < kKeys / ROWS; ++i) {
+                const uint8_t *at = from[i * ROWS + r0];
+                const int bytes = at ? 16 : 0;
+                at = (at ? at : any) + c0 * 16;
+#pragma unroll
+                for (int c = 0; c < CH; c += SIDE)
+                    cp_async(to + i * ROWS * S::kPitch + c * 16, at + c * 16, bytes, policy);
+            }
+        }
+    };
+    bool due = false, whole = false; /* values are to be asked for; all of them are there */
+    look_up();
+    auto load_keys = [&](int stage) {
+        due = to_load > 0;
+        if (due) {
             const bool ok = page >= 0 && page < a.cache_pages;
-            const uint32_t all = __ballot_sync(kAllLanes, ok) & 0xFFFFu;
-            const int64_t ko = ok ? (page * a.k_page_stride + place * a.k_token_stride +
-                                     kv * a.k_head_stride) * ES : 0;
-            const int64_t vo = ok ? (page * a.v_page_stride + place * a.v_token_stride +
-                                     kv * a.v_head_stride) * ES : 0;
-            constexpr int CH = S::kRowBytes / 16;
-            const uint32_t to = ring_at + stage * S::kStage;
-#pragma unroll
-            for (int i = 0; i < kKeys * CH / 32; ++i) {
-                const int n = i * 32 + lane, r = n / CH, c = n - r * CH;
-                const int64_t at = __shfl_sync(kAllLanes, ko, r);
-                cp_async(to + r * S::kPitch + c * 16, kc + at + c * 16, all >> r & 1u ? 16 : 0);
-            }
-#pragma unroll
-            for (int i = 0; i < kKeys * CH / 32; ++i) {
-                const int n = i * 32 + lane, r = n / CH, c = n - r * CH;
-                const int64_t at = __shfl_sync(kAllLanes, vo, r);
-                cp_async(to + (kKeys + r) * S::kPitch + c * 16, vc + at + c * 16,
-                         all >> r & 1u ? 16 : 0);
-            }
-            if (lane == 0) s_ok[warp][stage] = all;
+            const uint32_t there = __ballot_sync(kAllLanes, ok);
+            s_from[warp][0][lane] =
+                ok ? kc + (page * a.k_page_stride + place * a.k_token_stride + in.kv * a.k_head_stride) * ES
+                   : nullptr;
+            s_from[warp][1][lane] =
+                ok ? vc + (page * a.v_page_stride + place * a.v_token_stride + in.kv * a.v_head_stride) * ES
+                   : nullptr;
+            if (lane == 0) s_ok[warp][stage] = there;
+            __syncwarp();
+            whole = there == kAllLanes;
+            bring(ring_at + stage * S::kStage, s_from[warp][0], whole, kc);
             --to_load;
             advance(in);
-            page = page_at(in, to_load);
+            look_up();
         }
         cp_commit();
     };
+    auto load_values = [&](int stage) { /* of the slot whose keys have been asked for last */
+        if (due) bring(ring_at + stage * S::kStage + kKeys * S::kPitch, s_from[warp][1], whole, vc);
+        cp_commit();
+    };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) load(i);
+    for (int i = 0; i < STAGES; ++i) {
+        load_keys(i);
+        load_values(i);
+        __syncwarp();
+    }
 
     uint32_t qf[MT][NT][2];
     float o[MT][NT][4], m[NT][2], l[NT][2];
     int hi_n[NT][2], hi_least = 0, hi_most = 0; /* keys below these are seen */
-    const float unit = a.scale * kLog2e * a.k_scale;
+    /* Scores stay as the products leave them until they are exponents; a scale below 0 turns q round. */
+    const float unit = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e * a.k_scale;
+    const uint32_t q_and = a.scale == 0.0f ? 0u : 0xFFFFFFFFu, q_xor = a.scale < 0.0f ? 0x80008000u : 0u;
 
     auto start = [&] { /* a tile */
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const Row r = row_of(w, out.b, out.tile, nt * 8 + g, ROWS);
-            const T *q = static_cast<const T *>(a.q) + r.token * a.q_stride + (int64_t)r.head * D;
+            const Row r = row_of(w, out.kv, out.part, nt * 8 + g, ROWS);
+            const T *q = static_cast<const T *>(a.q) +
+                         ((int64_t)out.b * a.new_tokens + r.token) * a.q_stride + (int64_t)r.head * D;
 #pragma unroll
             for (int k = 0; k < MT; ++k) {
                 qf[k][nt][0] = qf[k][nt][1] = 0;
@@ -419,18 +589,23 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
                     }
                 }
             }
+            if (a.scale <= 0.0f) {
+#pragma unroll
+                for (int k = 0; k < MT; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) qf[k][nt][j] = (qf[k][nt][j] & q_and) ^ q_xor;
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 m[nt][j] = -INFINITY;
                 l[nt][j] = 0.0f;
-                const Row s = row_of(w, out.b, out.tile, nt * 8 + 2 * t + j, ROWS);
-                hi_n[nt][j] = out.len - a.new_tokens + 1 +
-                              min((int)(s.token - (int64_t)out.b * a.new_tokens), a.new_tokens - 1);
+                const Row s = row_of(w, out.kv, out.part, nt * 8 + 2 * t + j, ROWS);
+                hi_n[nt][j] = out.len - a.new_tokens + 1 + min(s.token, a.new_tokens - 1);
             }
         }
-        const int r0 = (out.tile % w.row_tiles) * ROWS;
-        hi_least = out.len - a.new_tokens + 1 + r0 / w.group;
-        hi_most = out.len - a.new_tokens + 1 + min((r0 + ROWS - 1) / w.group, a.new_tokens - 1);
+        hi_least = out.len - a.new_tokens + 1 + row_of(w, 0, out.part, 0, ROWS).token;
+        hi_most = out.len - a.new_tokens + 1 +
+                  min(row_of(w, 0, out.part, ROWS - 1, ROWS).token, a.new_tokens - 1);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -438,8 +613,12 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.0f;
     };
-    /* l over the lanes that hold one row's keys */
+    /* l over the lanes that hold one row's keys, m in powers of two */
     auto sum_up = [&] {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) m[nt][j] *= unit;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -473,75 +652,98 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
     const uint32_t v_row = F8 ? (kKeys + (lane & 15)) * S::kPitch + (lane >> 4) * 16
                               : (kKeys + (lane & 7) + (lane >> 4) * 8) * S::kPitch + (lane >> 3 & 1) * 16;
     for (; count > 0; --count) {
-        cp_wait<STAGES - 2>();
-        __syncwarp(); /* this stage is there for all lanes, and all have read the one before */
-        load((stage + STAGES - 1) % STAGES);
+        cp_wait<2 * STAGES - 1>();
+        __syncwarp(); /* the keys are there for all lanes */
         const uint32_t at = ring_at + stage * S::kStage, ok = s_ok[warp][stage];
-        float s[NT][4];
+        float s[kHalves][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[nt][j] = 0.0f;
-        if constexpr (F8) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < MT; k += 2) {
+                for (int j = 0; j < 4; ++j) s[h][nt][j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < MT; k += F8 ? 2 : 1) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
                 uint32_t r[4];
-                ldmatrix(r, at + k_row + k * 16);
-                const uint32_t f0[4] = {widen(T(), r[0]), widen(T(), r[1]), widen(T(), r[0] >> 16),
-                                        widen(T(), r[1] >> 16)};
-                const uint32_t f1[4] = {widen(T(), r[2]), widen(T(), r[3]), widen(T(), r[2] >> 16),
-                                        widen(T(), r[3] >> 16)};
+                ldmatrix(r, at + k_row + h * 16 * S::kPitch + k * (F8 ? 16 : 32));
+                if constexpr (F8) {
+                    const uint32_t f0[4] = {widen(T(), r[0]), widen(T(), r[1]), widen(T(), r[0] >> 16),
+                                            widen(T(), r[1] >> 16)};
+                    const uint32_t f1[4] = {widen(T(), r[2]), widen(T(), r[3]), widen(T(), r[2] >> 16),
+                                            widen(T(), r[3] >> 16)};
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<T>(s[nt], f0, qf[k][nt][0], qf[k][nt][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma<T>(s[h][nt], f0, qf[k][nt][0], qf[k][nt][1]);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<T>(s[nt], f1, qf[k + 1][nt][0], qf[k + 1][nt][1]);
-            }
-        } else {
+                    for (int nt = 0; nt < NT; ++nt)
+                        mma<T>(s[h][nt], f1, qf[k + 1][nt][0], qf[k + 1][nt][1]);
+                } else {
 #pragma unroll
-            for (int k = 0; k < MT; ++k) {
-                uint32_t f[4];
-                ldmatrix(f, at + k_row + k * 32);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<T>(s[nt], f, qf[k][nt][0], qf[k][nt][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma<T>(s[h][nt], r, qf[k][nt][0], qf[k][nt][1]);
+                }
             }
         }
+        __syncwarp(); /* all lanes have read them */
+        load_keys(stage);
 
-        /* scores in powers of two, -inf for keys that a row does not see */
+        /* -inf for keys that a row does not see */
         const int base = (out.first + out.slot) * kKeys;
         /* keys that are there, but not for every row of the tile (one token's rows all see the same) */
         const bool mixed = a.new_tokens > 1 && ((base + kKeys > hi_least && base < out.len) ||
                                                 (a.window > 0 && base < hi_most - a.window));
-        const bool some = ok != 0xFFFFu || base + kKeys > hi_least ||
+        const bool some = ok != 0xFFFFFFFFu || base + kKeys > hi_least ||
                           (a.window > 0 && base < hi_most - a.window);
+        if (some) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int i = h * 16 + g + (j >> 1) * 8, key = base + i, top = hi_n[nt][j & 1];
+                        const bool seen = (ok >> i & 1u) && key < top &&
+                                          (a.window <= 0 || key >= top - a.window);
+                        if (!seen) s[h][nt][j] = -INFINITY;
+                    }
+        }
         bool rise = false;
         float f[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[nt][j] *= unit;
-                if (some) {
-                    const int i = g + (j >> 1) * 8, key = base + i, top = hi_n[nt][j & 1];
-                    const bool seen = (ok >> i & 1u) && key < top &&
-                                      (a.window <= 0 || key >= top - a.window);
-                    if (!seen) s[nt][j] = -INFINITY;
-                }
-            }
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float top = fmaxf(s[nt][j], s[nt][j + 2]);
+                float top = fmaxf(s[0][nt][j], s[0][nt][j + 2]);
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, x));
-                top = fmaxf(top, m[nt][j]);
-                f[nt][j] = shrink(m[nt][j], top);
+                for (int h = 1; h < kHalves; ++h)
+                    top = fmaxf(top, fmaxf(s[h][nt][j], s[h][nt][j + 2]));
+                f[nt][j] = top;
+            }
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    f[nt][j] = fmaxf(f[nt][j], __shfl_xor_sync(kAllLanes, f[nt][j], x));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float top = fmaxf(f[nt][j], m[nt][j]);
+                const float ref = top == -INFINITY ? 0.0f : top * unit;
+                f[nt][j] = exp2_fast(m[nt][j] * unit - ref);
                 rise |= top > m[nt][j];
                 m[nt][j] = top;
-                const float ref = (top == -INFINITY ? 0.0f : top) - kUp<P>;
-                s[nt][j] = exp2_fast(s[nt][j] - ref);
-                s[nt][j + 2] = exp2_fast(s[nt][j + 2] - ref);
-                l[nt][j] = l[nt][j] * f[nt][j] + (s[nt][j] + s[nt][j + 2]);
+                float sum = 0.0f;
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    s[h][nt][j] = exp2_fast(fmaf(s[h][nt][j], unit, kUp<P> - ref));
+                    s[h][nt][j + 2] = exp2_fast(fmaf(s[h][nt][j + 2], unit, kUp<P> - ref));
+                    sum += s[h][nt][j] + s[h][nt][j + 2];
+                }
+                l[nt][j] = l[nt][j] * f[nt][j] + sum;
             }
-        }
         if (__any_sync(kAllLanes, rise)) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -550,19 +752,25 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[i][nt][j] *= f[nt][j & 1];
         }
-        uint32_t p[NT][2][2];
+        /* Values of 8 bits for a result in bf16: fp16's 11 bits of a probability do. */
+        constexpr bool TWO = !F8 || std::is_same<T, __half>::value;
+        uint32_t p[kHalves][NT][2][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t low;
-                const uint32_t high = split(P(), s[nt][2 * j], s[nt][2 * j + 1], low);
-                p[nt][j][0] = transposed(high);
-                p[nt][j][1] = transposed(low);
-            }
-        auto values = [&](int i, uint32_t (&v)[4], uint32_t (&r)[4]) { /* V^T of 16 dims */
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float x = s[h][nt][2 * j], y = s[h][nt][2 * j + 1];
+                    uint32_t low;
+                    const uint32_t high = TWO ? split(P(), x, y, low) : pack2(P(), x, y);
+                    p[h][nt][j][0] = transposed(high);
+                    p[h][nt][j][1] = TWO ? transposed(low) : 0;
+                }
+        auto values = [&](int i, int h, uint32_t (&v)[4], uint32_t (&r)[4]) { /* V^T of 16 dims */
+            const uint32_t from = at + v_row + h * 16 * S::kPitch;
             if constexpr (F8) {
-                if (i % 2 == 0) ldmatrix_trans(r, at + v_row + i * 16);
+                if (i % 2 == 0) ldmatrix_trans(r, from + i * 16);
                 const uint32_t r0 = r[i % 2 * 2], r1 = r[i % 2 * 2 + 1];
                 const uint32_t x0 = widen(P(), r0), y0 = widen(P(), r0 >> 16);
                 const uint32_t x1 = widen(P(), r1), y1 = widen(P(), r1 >> 16);
@@ -571,53 +779,61 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
                 v[2] = __byte_perm(x1, y1, 0x5410);
                 v[3] = __byte_perm(x1, y1, 0x7632);
             } else {
-                ldmatrix_trans(v, at + v_row + i * 32);
+                ldmatrix_trans(v, from + i * 32);
             }
         };
-        uint32_t r[4] = {};
-        if (!mixed) {
+        cp_wait<2 * STAGES - 1>();
+        __syncwarp();
+        uint32_t r[kHalves][4] = {};
+        /* 0 times a value that a row does not see is 0, unless that is an infinity or NaN */
+        if (!mixed || !any_special<T, F8>(at + kKeys * S::kPitch, lane, S::kRowBytes / 16, S::kPitch)) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                uint32_t v[4];
-                values(i, v, r);
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma<P>(o[i][nt], v, p[nt][0][0], p[nt][1][0]);
-                    mma<P>(o[i][nt], v, p[nt][0][1], p[nt][1][1]);
-                }
-            }
-        } else {
-            /* Keys that some rows see and others do not: token by token, with the values that it does not
-             * see taken out, since 0 times an infinity or NaN would come through. */
-            for (int top = hi_least; top <= hi_most; ++top) {
-                uint32_t mask[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int key = base + j * 8 + 2 * t;
-                    const bool x = key < top && (a.window <= 0 || key >= top - a.window);
-                    const bool y = key + 1 < top && (a.window <= 0 || key + 1 >= top - a.window);
-                    mask[j] = (x ? 0x0000FFFFu : 0u) | (y ? 0xFFFF0000u : 0u);
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
+                for (int h = 0; h < kHalves; ++h) {
                     uint32_t v[4];
-                    values(i, v, r);
-                    v[0] &= mask[0];
-                    v[1] &= mask[0];
-                    v[2] &= mask[1];
-                    v[3] &= mask[1];
+                    values(i, h, v, r[h]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float c[4] = {};
-                        mma<P>(c, v, p[nt][0][0], p[nt][1][0]);
-                        mma<P>(c, v, p[nt][0][1], p[nt][1][1]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (hi_n[nt][j & 1] == top) o[i][nt][j] += c[j];
+                        mma<P>(o[i][nt], v, p[h][nt][0][0], p[h][nt][1][0]);
+                        if (TWO) mma<P>(o[i][nt], v, p[h][nt][0][1], p[h][nt][1][1]);
                     }
                 }
-            }
+        } else {
+            /* token by token, with the values that it does not see taken out */
+            for (int top = hi_least; top <= hi_most; ++top)
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    uint32_t mask[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int key = base + h * 16 + j * 8 + 2 * t;
+                        const bool x = key < top && (a.window <= 0 || key >= top - a.window);
+                        const bool y = key + 1 < top && (a.window <= 0 || key + 1 >= top - a.window);
+                        mask[j] = (x ? 0x0000FFFFu : 0u) | (y ? 0xFFFF0000u : 0u);
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        uint32_t v[4];
+                        values(i, h, v, r[h]);
+                        v[0] &= mask[0];
+                        v[1] &= mask[0];
+                        v[2] &= mask[1];
+                        v[3] &= mask[1];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float c[4] = {};
+                            mma<P>(c, v, p[h][nt][0][0], p[h][nt][1][0]);
+                            if (TWO) mma<P>(c, v, p[h][nt][0][1], p[h][nt][1][1]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (hi_n[nt][j & 1] == top) o[i][nt][j] += c[j];
+                        }
+                    }
+                }
         }
+        __syncwarp();
+        load_values(stage);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
 
         const bool ends = out.slot + 1 == out.slots;
@@ -632,9 +848,9 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
                 keep(reinterpret_cast<float *>(ring));
                 if (lane == 0) s_part[warp][1] = 1;
             } else {
+                const Finish<T, NT, F8> to(w, out.b, out.kv, out.part, lane, true, m, l);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-                    finish<T, NT, F8>(w, out.b, out.tile, i * 16, lane, o[i], m, l, i == 0);
+                for (int i = 0; i < MT; ++i) to.write(i * 16, lane, o[i]);
             }
             if (count > 1) {
                 advance(out);
@@ -646,157 +862,170 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
         }
     }
     cp_wait<0>();
-    release_later();
     __syncthreads();
 
-    /* ---- tiles that several warps have worked on: 16 dims to a warp ---- */
-    const bool any0 = s_at[0].slot != 0, anyW = s_at[W].slot != 0;
-    auto id = [&](const Place &p) { return p.slot ? (int64_t)p.b * tiles + p.tile : (int64_t)-1; };
-    if (tid == 0) {
-        w.ends[blockIdx.x * 2] = any0 ? id(s_at[0]) : -1;
-        w.ends[blockIdx.x * 2 + 1] = anyW ? id(s_at[W]) : -1;
-    }
-    for (int e = 0; e <= W;) {
-        const int64_t tile = id(s_at[e]);
-        if (tile < 0) {
-            ++e;
-            continue;
-        }
-        int last = e; /* borders e .. last lie inside this tile */
-        while (last < W && id(s_at[last + 1]) == tile) ++last;
-        const bool outside = e == 0 || last == W;
-        const int pb = s_at[e].b, pt = s_at[e].tile;
-        for (int i = warp; i < MT; i += W) {
-            float c[NT][4], top[NT][2], sum[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c[nt][j] = 0.0f;
-                top[nt][0] = top[nt][1] = -INFINITY;
-                sum[nt][0] = sum[nt][1] = 0.0f;
-            }
+    /* ---- tiles that several warps have worked on ----
+     * Borders inside the same tile make a group; groups go to the warps, the dims of one to as many warps
+     * as there are for it. */
+    {
+        const int64_t id = lane <= W ? s_id[lane] : -1;
+        const uint32_t same = __match_any_sync(kAllLanes, id);
+        const uint32_t first_of = __ballot_sync(kAllLanes, id >= 0 && lane == __ffs(same) - 1);
+        const uint32_t held0 = __ballot_sync(kAllLanes, lane < W && s_part[lane & (W - 1)][0]);
+        const uint32_t held1 = __ballot_sync(kAllLanes, lane < W && s_part[lane & (W - 1)][1]);
+        const int groups = __popc(first_of);
+        int split = W; /* warps of a group, a power of two */
+        while (split > 1 && (split * groups > W || split > MT)) split >>= 1;
+        for (int n = warp / split; n < groups; n += W / split) {
+            const int e = __fns(first_of, 0, n + 1);
+            const int last = 31 - __clz(__shfl_sync(kAllLanes, same, e));
+            const bool outside = e == 0 || last == W;
+            Joined<MT, NT> all;
             for (int x = max(e - 1, 0); x <= min(last, W - 1); ++x) {
-                const int which = x < e ? 1 : 0; /* the warp in which it begins holds it as its last */
-                if (!s_part[x][which]) continue;
-                const uint8_t *from = smem + x * S::kWarpBytes + (which ? 0 : STAGES * S::kStage);
-                const float *part = reinterpret_cast<const float *>(from), *ml = part + MT * NT * 128;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float4 q =
-                        *reinterpret_cast<const float4 *>(part + ((i * NT + nt) * 32 + lane) * 4);
-                    const float v[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float m1 = ml[nt * 8 + 2 * t + j], l1 = ml[ROWS + nt * 8 + 2 * t + j];
-                        const float both = fmaxf(m1, top[nt][j]);
-                        const float f0 = shrink(top[nt][j], both), f1 = shrink(m1, both);
-                        top[nt][j] = both;
-                        sum[nt][j] = sum[nt][j] * f0 + l1 * f1;
-                        c[nt][j] = c[nt][j] * f0 + v[j] * f1;
-                        c[nt][j + 2] = c[nt][j + 2] * f0 + v[j + 2] * f1;
-                    }
-                }
+                /* the warp in which the tile begins holds it as its last */
+                const bool begins = x < e;
+                if (!((begins ? held1 : held0) >> x & 1u)) continue;
+                all.add(reinterpret_cast<const float *>(smem + x * S::kWarpBytes +
+                                                        (begins ? 0 : STAGES * S::kStage)),
+                        warp & (split - 1), split - 1, lane);
             }
             if (!outside) {
-                finish<T, NT, F8>(w, pb, pt, i * 16, lane, c, top, sum, i == 0);
+                const Place p = s_at[e];
+                const Finish<T, NT, F8> to(w, p.b, p.kv, p.part, lane, (warp & (split - 1)) == 0, all.top,
+                                           all.sum);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    if ((i & (split - 1)) == (warp & (split - 1))) to.write(i * 16, lane, all.c[i]);
                 continue;
             }
             float *to = w.parts + (int64_t)(blockIdx.x * 2 + (e == 0 ? 0 : 1)) * S::kFloats;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-                *reinterpret_cast<float4 *>(to + ((i * NT + nt) * 32 + lane) * 4) =
-                    make_float4(c[nt][0], c[nt][1], c[nt][2], c[nt][3]);
-            if (i == 0 && g == 0) {
+            for (int i = 0; i < MT; ++i)
+                if ((i & (split - 1)) == (warp & (split - 1))) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        reinterpret_cast<float4 *>(to)[(i * NT + nt) * 32 + lane] = make_float4(
+                            all.c[i][nt][0], all.c[i][nt][1], all.c[i][nt][2], all.c[i][nt][3]);
+                }
+            if ((warp & (split - 1)) == 0 && g == 0) {
                 float *ml = to + MT * NT * 128;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        ml[nt * 8 + 2 * t + j] = top[nt][j];
-                        ml[ROWS + nt * 8 + 2 * t + j] = sum[nt][j];
+                        ml[nt * 8 + 2 * t + j] = all.top[nt][j];
+                        ml[ROWS + nt * 8 + 2 * t + j] = all.sum[nt][j];
                     }
             }
         }
-        e = last + 1;
     }
-}
 
-constexpr int kJoinWarps = 8;
-
-/* Tiles that several blocks have worked on: block (c, i) joins 16 dims of the tile that begins in block c
- * of the launch before and ends in a later one. */
-template <typename T, int D, int NT, bool F8>
-__global__ void __launch_bounds__(kJoinWarps * 32) cfa_attend_join_kernel(const Work w)
-{
-    using S = Shape<D, NT, F8>;
-    __shared__ float4 s_c[kJoinWarps][NT][32];
-    __shared__ float s_m[kJoinWarps][8 * NT], s_l[kJoinWarps][8 * NT];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int first = blockIdx.x, i = blockIdx.y;
-    wait_for_earlier();
-    const int64_t tile = __ldcg(w.ends + first * 2 + 1);
-    if (tile < 0 || __ldcg(w.ends + first * 2) == tile) return;
-    float c[NT][4], top[NT][2], sum[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[nt][j] = 0.0f;
-        top[nt][0] = top[nt][1] = -INFINITY;
-        sum[nt][0] = sum[nt][1] = 0.0f;
-    }
-    auto join = [&](int nt, const float (&v)[4], const float (&m1)[2], const float (&l1)[2]) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float both = fmaxf(m1[j], top[nt][j]);
-            const float f0 = shrink(top[nt][j], both), f1 = shrink(m1[j], both);
-            top[nt][j] = both;
-            sum[nt][j] = sum[nt][j] * f0 + l1[j] * f1;
-            c[nt][j] = c[nt][j] * f0 + v[j] * f1;
-            c[nt][j + 2] = c[nt][j + 2] * f0 + v[j + 2] * f1;
+    /* ---- tiles that several blocks have worked on ----
+     * A block says that its part is there, and looks whether all others of the tile's are: the last one
+     * finds them, and joins.  Its mark is this call's own number, which nothing else in the workspace
+     * holds, and is taken back by whoever joins, so that the next call (or the next run of a captured
+     * one) finds none.  Two that find all of them at a time ask for the joining in turn; should both be
+     * given it, one after the other, they write the same. */
+    const bool outer[2] = {s_id[0] >= 0, s_id[W] >= 0 && s_id[W] != s_id[0]};
+    if (!outer[0] && !outer[1]) return;
+    __threadfence(); /* this thread's part of the partials is there for all before the mark */
+    __syncthreads();
+    if (warp < 2 && outer[warp]) {
+        /* the tile's slots are those from `begin` on; lane 0: its first block, lane 1: its last */
+        const Place &p = s_at[warp * W];
+        const int64_t begin = from + (warp ? size : 0) - p.slot;
+        const int64_t x = lane == 0 ? begin : begin + p.slots - 1, big = rest * (each + 1);
+        int block;
+        if (total >> 32)
+            block = (int)(x < big ? x / (each + 1) : rest + (x - big) / each);
+        else
+            block = x < big ? (uint32_t)x / (uint32_t)(each + 1)
+                            : (uint32_t)rest + (uint32_t)(x - big) / (uint32_t)each;
+        const int f = __shfl_sync(kAllLanes, block, 0), l = __shfl_sync(kAllLanes, block, 1);
+        if (lane == 0) atomicExch(w.marks + blockIdx.x * 2 + warp, w.number);
+        __threadfence();
+        __syncwarp();
+        bool all = true;
+        for (int y = f + lane; y <= l; y += 32)
+            all &= atomicAdd(w.marks + y * 2 + (y == f ? 1 : 0), 0ull) == w.number;
+        all = __all_sync(kAllLanes, all);
+        if (lane == 0) {
+            s_join[warp][0] = all && atomicExch(w.marks + (2 * kBlocks + f), w.number) != w.number;
+            s_join[warp][1] = f;
+            s_join[warp][2] = l - f + 1;
         }
-    };
-    int parts = 1;
-    for (int x0 = first + 1; x0 < kBlocks; x0 += 32) { /* blocks that lie inside it */
-        const int x = x0 + lane;
-        const bool in = x < kBlocks && __ldcg(w.ends + x * 2) == tile;
-        const uint32_t all = __ballot_sync(kAllLanes, in);
-        parts += __popc(all);
-        if (all != kAllLanes) break;
-    }
-    for (int x = warp; x < parts; x += kJoinWarps) {
-        const float *part = w.parts + (int64_t)((first + x) * 2 + (x == 0 ? 1 : 0)) * S::kFloats;
-        const float *ml = part + S::kTiles * NT * 128;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float4 q =
-                __ldcg(reinterpret_cast<const float4 *>(part + ((i * NT + nt) * 32 + lane) * 4));
-            const float2 m1 = __ldcg(reinterpret_cast<const float2 *>(ml + nt * 8 + 2 * t));
-            const float2 l1 = __ldcg(reinterpret_cast<const float2 *>(ml + 8 * NT + nt * 8 + 2 * t));
-            join(nt, {q.x, q.y, q.z, q.w}, {m1.x, m1.y}, {l1.x, l1.y});
-        }
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        s_c[warp][nt][lane] = make_float4(c[nt][0], c[nt][1], c[nt][2], c[nt][3]);
-        if (g == 0) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                s_m[warp][nt * 8 + 2 * t + j] = top[nt][j];
-                s_l[warp][nt * 8 + 2 * t + j] = sum[nt][j];
-            }
-        }
+        __threadfence();
     }
     __syncthreads();
-    if (warp) return;
-    for (int x = 1; x < kJoinWarps && x < parts; ++x)
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        if (!outer[which] || !s_join[which][0]) continue;
+        const int f = s_join[which][1], parts = s_join[which][2];
+        const Place p = s_at[which * W];
+        for (int i = warp; i < MT; i += W) {
+            constexpr int AHEAD = 8 / NT; /* parts that are asked for at a time */
+            float c[NT][4], top[NT][2], sum[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float4 q = s_c[x][nt][lane];
-            const int n = nt * 8 + 2 * t;
-            join(nt, {q.x, q.y, q.z, q.w}, {s_m[x][n], s_m[x][n + 1]}, {s_l[x][n], s_l[x][n + 1]});
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    top[nt][j] = -INFINITY;
+                    sum[nt][j] = c[nt][j] = c[nt][j + 2] = 0.0f;
+                }
+            for (int x0 = 0; x0 < parts; x0 += AHEAD) {
+                float4 q[AHEAD][NT];
+                float2 m1[AHEAD][NT], l1[AHEAD][NT];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int x = x0 + k;
+                    const float *part =
+                        w.parts + (int64_t)((f + x) * 2 + (x == 0 ? 1 : 0)) * S::kFloats;
+                    const float *ml = part + MT * NT * 128;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        q[k][nt] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        m1[k][nt] = make_float2(-INFINITY, -INFINITY);
+                        l1[k][nt] = make_float2(0.0f, 0.0f);
+                        if (x < parts) {
+                            q[k][nt] = __ldcg(reinterpret_cast<const float4 *>(part) +
+                                              (i * NT + nt) * 32 + lane);
+                            m1[k][nt] = __ldcg(reinterpret_cast<const float2 *>(ml + nt * 8 + 2 * t));
+                            l1[k][nt] =
+                                __ldcg(reinterpret_cast<const float2 *>(ml + ROWS + nt * 8 + 2 * t));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float both = top[nt][j];
+#pragma unroll
+                        for (int k = 0; k < AHEAD; ++k) both = fmaxf(both, j ? m1[k][nt].y : m1[k][nt].x);
+                        const float f0 = shrink(top[nt][j], both);
+                        top[nt][j] = both;
+                        sum[nt][j] *= f0;
+                        c[nt][j] *= f0;
+                        c[nt][j + 2] *= f0;
+#pragma unroll
+                        for (int k = 0; k < AHEAD; ++k) {
+                            const float f1 = shrink(j ? m1[k][nt].y : m1[k][nt].x, both);
+                            sum[nt][j] += (j ? l1[k][nt].y : l1[k][nt].x) * f1;
+                            c[nt][j] += (j ? q[k][nt].y : q[k][nt].x) * f1;
+                            c[nt][j + 2] += (j ? q[k][nt].w : q[k][nt].z) * f1;
+                        }
+                    }
+            }
+            const Finish<T, NT, F8> to(w, p.b, p.kv, p.part, lane, i == 0, top, sum);
+            to.write(i * 16, lane, c);
         }
-    const int64_t tiles = (int64_t)w.a.kv_heads * w.row_tiles;
-    finish<T, NT, F8>(w, (int)(tile / tiles), (int)(tile % tiles), i * 16, lane, c, top, sum, i == 0);
+        if (warp == 0)
+            for (int x = lane; x <= parts; x += 32) {
+                /* the marks, and the joining's */
+                const int at = x == parts ? 2 * kBlocks + f : (f + x) * 2 + (x == 0 ? 1 : 0);
+                __stcg(w.marks + at, 0ull);
+            }
+    }
 }
 
 template <typename T, int D, int NT, bool F8> cudaError_t launch(const Work &w, cudaStream_t stream)
@@ -816,13 +1045,7 @@ template <typename T, int D, int NT, bool F8> cudaError_t launch(const Work &w, 
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     void *p[] = {const_cast<Work *>(&w)};
-    e = cudaLaunchKernelExC(&cfg, fn, p);
-    if (e) return e;
-    cfg.gridDim = dim3(kBlocks, S::kTiles);
-    cfg.blockDim = dim3(kJoinWarps * 32);
-    cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelExC(
-        &cfg, reinterpret_cast<const void *>(&cfa_attend_join_kernel<T, D, NT, F8>), p);
+    return cudaLaunchKernelExC(&cfg, fn, p);
 }
 
 template <typename T, bool F8> cudaError_t launch_any(const Work &w, cudaStream_t stream)
@@ -832,7 +1055,7 @@ template <typename T, bool F8> cudaError_t launch_any(const Work &w, cudaStream_
     case 64: return nt == 1 ? launch<T, 64, 1, F8>(w, stream) : launch<T, 64, 2, F8>(w, stream);
     case 96: return nt == 1 ? launch<T, 96, 1, F8>(w, stream) : launch<T, 96, 2, F8>(w, stream);
     case 128: return nt == 1 ? launch<T, 128, 1, F8>(w, stream) : launch<T, 128, 2, F8>(w, stream);
-    case 256: return nt == 1 ? launch<T, 256, 1, F8>(w, stream) : launch<T, 256, 2, F8>(w, stream);
+    case 256: return launch<T, 256, 1, F8>(w, stream);
     default: return cudaErrorInvalidValue; /* refused before */
     }
 }

@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2)
     const float c = a.scale * 1.4426950408889634f;
     const T *x = static_cast<const T *>(a.logits) + row * a.stride;
     if (blocks > 1) cg::this_cluster().barrier_arrive(); /* its shared memory is there: waited for below */
-    wait_for_earlier();
+    launch_in_turn();
 
     /* the row: `head` single values up to the 16-byte grid, pieces of VEC, `tail` single values */
     const int cols = (int)a.cols;

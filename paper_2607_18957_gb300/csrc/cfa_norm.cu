@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(1024) cfa_norm_kernel(const cfa_norm_args a, i
     const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
     const T *g = static_cast<const T *>(a.gate) + row * a.gate_stride;
     constexpr bool early = NV * VEC <= kEarly;
-    wait_for_earlier();
+    launch_in_turn();
 
     Pack<T, VEC> px[NV], pr[NV], pg[NV];
 #pragma unroll

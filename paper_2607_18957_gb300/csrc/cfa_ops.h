@@ -107,10 +107,11 @@ cudaError_t cfa_launch_logprobs(const cfa_logprobs_args *a, cudaStream_t stream)
 typedef struct cfa_attend_work {
     cfa_attend_args a;
     int32_t group, row_tiles; /* query heads of a key head; tiles of a sequence and key head */
-    int32_t nt, pad;          /* a tile has 8 nt rows */
+    int32_t nt;               /* a tile has 8 nt rows */
+    uint32_t group_inverse;   /* 2^32 / group, rounded up */
     float *parts;             /* [CFA_ATTEND_BLOCKS][2] partials */
-    int64_t *ends;            /* [CFA_ATTEND_BLOCKS][2]: the tile inside which a block's share begins and
-                               * the one inside which it ends, -1 for none */
+    unsigned long long *marks; /* [CFA_ATTEND_BLOCKS][2] of the partials that are there, [..] of joins */
+    unsigned long long number; /* of the call, its mark; not 0 */
 } cfa_attend_work;
 cudaError_t cfa_launch_attend_bf16(const cfa_attend_work *w, cudaStream_t stream);
 cudaError_t cfa_launch_attend_f16(const cfa_attend_work *w, cudaStream_t stream);

@@ -2,6 +2,8 @@
  * Entry points of the operators of a decoding step around the products: they check every argument and
  * enqueue the kernels.  Nothing is allocated and nothing is read back.
  */
+#include <atomic>
+#include <chrono>
 #include <cmath>
 
 #include "cfa_checks.h"
@@ -188,11 +190,26 @@ extern "C" cfa_status cfa_append_async(const cfa_append_args *a, cfa_stream stre
 namespace {
 
 constexpr int64_t kMostKeys = 1ll << 30; /* of a sequence */
+constexpr int64_t kMostRows = 1 << 18;   /* new tokens times query heads of a key head */
 
 struct AttendPlan {
     cfa_attend_work w;
-    uint64_t ends, total; /* bytes */
+    uint64_t marks, total; /* bytes */
 };
+
+/* A number that no other call has and that memory does not hold by chance: a counter from a start that
+ * differs by process, mixed over 64 bits (one to one, so that no two counts give the same). */
+unsigned long long call_number()
+{
+    static std::atomic<unsigned long long> next{
+        (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() << 20 ^
+        (unsigned long long)(uintptr_t)&next};
+    unsigned long long x = next.fetch_add(1, std::memory_order_relaxed);
+    x = (x ^ x >> 30) * 0xBF58476D1CE4E5B9ull;
+    x = (x ^ x >> 27) * 0x94D049BB133111EBull;
+    x ^= x >> 31;
+    return x ? x : 1;
+}
 
 cfa_status attend_plan(const cfa_attend_args *a, AttendPlan *p)
 {
@@ -201,21 +218,21 @@ cfa_status attend_plan(const cfa_attend_args *a, AttendPlan *p)
     if (a->head_dim != 64 && a->head_dim != 96 && a->head_dim != 128 && a->head_dim != 256)
         return refuse(CFA_ERR_INVAL, "cfa_attend: heads of %d: 64, 96, 128 or 256", a->head_dim);
     if (a->heads < 1 || a->heads > 8192 || a->kv_heads < 1 || a->heads % a->kv_heads ||
-        a->new_tokens < 1 || a->new_tokens > 1 << 20)
+        a->new_tokens < 1 || (int64_t)a->new_tokens * (a->heads / a->kv_heads) > kMostRows)
         return refuse(CFA_ERR_INVAL, "cfa_attend: %d heads over %d, %d new tokens", a->heads,
                       a->kv_heads, a->new_tokens);
     p->w = {};
     p->w.a = *a;
     p->w.group = a->heads / a->kv_heads;
     const int64_t rows = (int64_t)p->w.group * a->new_tokens;
-    p->w.nt = rows <= 8 ? 1 : 2;
+    p->w.nt = rows <= 8 || a->head_dim > 128 ? 1 : 2; /* 16 rows of 256 dims do not fit the registers */
     const int64_t row_tiles = (rows + 8 * p->w.nt - 1) / (8 * p->w.nt);
-    if (row_tiles * a->kv_heads >= kMost) return refuse(CFA_ERR_INVAL, "cfa_attend: too many rows");
+    p->w.group_inverse = (uint32_t)(((1ull << 32) + p->w.group - 1) / p->w.group);
     p->w.row_tiles = (int32_t)row_tiles;
     /* a partial: O of 8 nt rows, their maxima and sums */
     const uint64_t part = 4ull * (8 * p->w.nt) * (a->head_dim + 2);
-    p->ends = aligned(sizeof(int64_t) * 2 * CFA_ATTEND_BLOCKS);
-    p->total = p->ends + aligned(part * 2 * CFA_ATTEND_BLOCKS);
+    p->marks = aligned(sizeof(unsigned long long) * 3 * CFA_ATTEND_BLOCKS);
+    p->total = p->marks + aligned(part * 2 * CFA_ATTEND_BLOCKS);
     return CFA_OK;
 }
 
@@ -244,9 +261,9 @@ extern "C" cfa_status cfa_attend_async(const cfa_attend_args *a, cfa_stream stre
     if (a->window < 0 || a->window > kMostKeys || a->flags || !std::isfinite(a->scale))
         return refuse(CFA_ERR_INVAL, "cfa_attend: window %d, scale %g, flags %u", a->window, a->scale,
                       a->flags);
-    const int64_t slots = (int64_t)a->max_pages * a->page_size / 16 + 1;
+    const int64_t slots = (int64_t)a->max_pages * a->page_size / 32 + 1;
     const int64_t tiles = (int64_t)p.w.row_tiles * a->kv_heads;
-    if ((unsigned __int128)slots * (uint64_t)tiles * (uint64_t)a->sequences >> 40)
+    if (slots * a->sequences >> 31 || (unsigned __int128)(slots * a->sequences) * (uint64_t)tiles >> 40)
         return refuse(CFA_ERR_INVAL, "cfa_attend: %lld sequences are too many", (long long)a->sequences);
     const int64_t cols = (int64_t)a->heads * a->head_dim, rows = a->sequences * a->new_tokens;
     if (rows > 1 && (a->q_stride < cols || a->q_stride >= kMost || a->out_stride < cols ||
@@ -299,8 +316,9 @@ extern "C" cfa_status cfa_attend_async(const cfa_attend_args *a, cfa_stream stre
             if (overlap(m[i].p, m[i].n, m[j].p, m[j].n))
                 return refuse(CFA_ERR_OVERLAP,
                               "cfa_attend: an output or the workspace overlaps another operand");
-    p.w.ends = reinterpret_cast<int64_t *>(a->workspace);
-    p.w.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a->workspace) + p.ends);
+    p.w.marks = static_cast<unsigned long long *>(a->workspace);
+    p.w.number = call_number();
+    p.w.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(a->workspace) + p.marks);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     const bool f16 = a->dtype == CFA_DTYPE_F16;
     const cudaError_t e = cs == 1 ? (f16 ? cfa_launch_attend_f16_f8(&p.w, stream)

@@ -16,11 +16,12 @@ namespace cfa_dev {
 
 constexpr uint32_t kAllLanes = 0xFFFFFFFFu;
 
-/* Nothing of an earlier kernel's is read or overwritten before this. */
-__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-/* The kernel behind this one may start (it waits by itself for this one's end). */
-__device__ __forceinline__ void release_later()
+/* Before anything that an earlier kernel has written is read, and anything at all written: the earlier
+ * kernels have ended.  From here on the next one may start (its own wait is for this kernel's end), not
+ * before, so that a kernel that reads ahead of its wait reads nothing that these still write. */
+__device__ __forceinline__ void launch_in_turn()
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 

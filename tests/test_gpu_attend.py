@@ -126,7 +126,7 @@ class Setup:
                 assert worst <= 0, f"lse of {b}, {i}: off by {worst:g} more than the bound"
 
 
-LENS = [[1], [2], [15], [16], [17], [33], [1000], [0, 1, 0, 16, 5], [100, 3, 257, 1, 64, 1023],
+LENS = [[1], [2], [15], [16], [17], [31], [32], [33], [64], [65], [1000], [0, 1, 0, 16, 5], [100, 3, 257, 1, 64, 1023],
         [4097, 1, 300], list(range(1, 70))]
 
 
