@@ -455,3 +455,46 @@ def test_logprobs_shapes():
     assert cfa.logprobs(logits[:0], tokens[:0])[0].shape == (0, 3)
     one = cfa.logprobs(logits[0, 0], tokens[0, 0])
     assert one[0].shape == () and one[0].item() == out[0][0, 0].item()
+
+
+# ---- norm of many rows ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("t,c", [(153, 1), (200, 7), (1000, 64), (1201, 130), (400, 1003), (333, 2307),
+                                 (305, 8192), (700, 5121), (160, 16384), (155, 16383)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_norm_of_many_rows(t, c, dtype):
+    g = gen(t + c)
+    x, w, r = normal(g, (t, c), dtype), normal(g, (c,), dtype), normal(g, (t, c), dtype, 3.0)
+    z, p = normal(g, (t, c), dtype), normal(g, (c,), F32)
+    y64, ey, _, _ = norm64(x, w)
+    close(cfa.norm(x, w), y64, ey)
+    y64, ey, h64, eh = norm64(x, w.float(), r, z, "silu", p, 0.37, 1e-5, 1.0)
+    y, h = cfa.norm(x, w.float(), residual=r, gate=z, post_weight=p, scale=0.37, offset=1.0, eps=1e-5)
+    close(y, y64, ey)
+    close(h, h64, eh)
+    # with the results in the operands' places
+    r2, z2 = r.clone(), z.clone()
+    y2, h2 = cfa.norm(x, w.float(), residual=r2, gate=z2, post_weight=p, scale=0.37, offset=1.0, eps=1e-5,
+                      out=(z2, r2))
+    assert torch.equal(y2, y) and torch.equal(h2, h)
+    # one gate for all
+    y64, ey, _, _ = norm64(x, w, None, z[0].expand(t, c), "relu")
+    close(cfa.norm(x, w, gate=z[0], activation="relu"), y64, ey)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("extras", [(0, 0, 0), (8, 8, 8), (3, 3, 3), (5, 13, 21), (1, 2, 3)])
+@pytest.mark.parametrize("lead", [0, 1])
+def test_norm_of_many_rows_apart(extras, lead, dtype):
+    g = gen(sum(extras))
+    t, c = 211, 517
+    x, r, w = normal(g, (t, c), dtype), normal(g, (t, c), dtype), normal(g, (c,), dtype)
+    (_, xv), (rb, rv), (yb, yv) = (inside(v, e, lead) for v, e in zip((x, r, torch.zeros_like(x)), extras))
+    y, h = cfa.norm(xv, w, residual=rv, out=(yv, rv))
+    y64, ey, h64, eh = norm64(x, w, r)
+    close(y, y64, ey)
+    close(h, h64, eh)
+    for buf, e in ((rb, extras[1]), (yb, extras[2])):
+        mask = torch.ones_like(buf, dtype=torch.bool)
+        mask[lead:].as_strided((t, c), (c + e, 1)).fill_(False)
+        assert bool((buf[mask] == 7.0).all())
