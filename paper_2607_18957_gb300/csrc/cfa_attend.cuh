@@ -922,13 +922,11 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
 
     /* ---- tiles that several blocks have worked on ----
      * A block says that its part is there, and looks whether all others of the tile's are: the last one
-     * finds them, and joins.  Its mark is this call's own number, which nothing else in the workspace
-     * holds, and is taken back by whoever joins, so that the next call (or the next run of a captured
-     * one) finds none.  Two that find all of them at a time ask for the joining in turn; should both be
-     * given it, one after the other, they write the same. */
+     * finds them, and joins (so may several that come at a time: they write the same).  Its mark is this
+     * call's own number, which nothing else in the workspace holds, and is taken back by whoever joins,
+     * when all have been set, so that the next call (or the next run of a captured one) finds none. */
     const bool outer[2] = {s_id[0] >= 0, s_id[W] >= 0 && s_id[W] != s_id[0]};
     if (!outer[0] && !outer[1]) return;
-    __threadfence(); /* this thread's part of the partials is there for all before the mark */
     __syncthreads();
     if (warp < 2 && outer[warp]) {
         /* the tile's slots are those from `begin` on; lane 0: its first block, lane 1: its last */
@@ -942,19 +940,27 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
             block = x < big ? (uint32_t)x / (uint32_t)(each + 1)
                             : (uint32_t)rest + (uint32_t)(x - big) / (uint32_t)each;
         const int f = __shfl_sync(kAllLanes, block, 0), l = __shfl_sync(kAllLanes, block, 1);
-        if (lane == 0) atomicExch(w.marks + blockIdx.x * 2 + warp, w.number);
-        __threadfence();
+        if (lane == 0) {
+            __threadfence(); /* the block's partials before its mark */
+            __stcg(w.marks + blockIdx.x * 2 + warp, w.number);
+            __threadfence(); /* its mark before the look at the others' */
+        }
         __syncwarp();
         bool all = true;
-        for (int y = f + lane; y <= l; y += 32)
-            all &= atomicAdd(w.marks + y * 2 + (y == f ? 1 : 0), 0ull) == w.number;
+        for (int y = f + lane; y <= l; y += 32) {
+            unsigned long long mark;
+            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];"
+                         : "=l"(mark)
+                         : "l"(w.marks + y * 2 + (y == f ? 1 : 0))
+                         : "memory");
+            all &= mark == w.number;
+        }
         all = __all_sync(kAllLanes, all);
         if (lane == 0) {
-            s_join[warp][0] = all && atomicExch(w.marks + (2 * kBlocks + f), w.number) != w.number;
+            s_join[warp][0] = all;
             s_join[warp][1] = f;
             s_join[warp][2] = l - f + 1;
         }
-        __threadfence();
     }
     __syncthreads();
 #pragma unroll 1
@@ -1020,11 +1026,8 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
             to.write(i * 16, lane, c);
         }
         if (warp == 0)
-            for (int x = lane; x <= parts; x += 32) {
-                /* the marks, and the joining's */
-                const int at = x == parts ? 2 * kBlocks + f : (f + x) * 2 + (x == 0 ? 1 : 0);
-                __stcg(w.marks + at, 0ull);
-            }
+            for (int x = lane; x < parts; x += 32)
+                __stcg(w.marks + (f + x) * 2 + (x == 0 ? 1 : 0), 0ull);
     }
 }
 

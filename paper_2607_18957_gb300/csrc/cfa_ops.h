@@ -110,7 +110,7 @@ typedef struct cfa_attend_work {
     int32_t nt;               /* a tile has 8 nt rows */
     uint32_t group_inverse;   /* 2^32 / group, rounded up */
     float *parts;             /* [CFA_ATTEND_BLOCKS][2] partials */
-    unsigned long long *marks; /* [CFA_ATTEND_BLOCKS][2] of the partials that are there, [..] of joins */
+    unsigned long long *marks; /* [CFA_ATTEND_BLOCKS][2]: the partials that are there */
     unsigned long long number; /* of the call, its mark; not 0 */
 } cfa_attend_work;
 cudaError_t cfa_launch_attend_bf16(const cfa_attend_work *w, cudaStream_t stream);

@@ -231,7 +231,7 @@ cfa_status attend_plan(const cfa_attend_args *a, AttendPlan *p)
     p->w.row_tiles = (int32_t)row_tiles;
     /* a partial: O of 8 nt rows, their maxima and sums */
     const uint64_t part = 4ull * (8 * p->w.nt) * (a->head_dim + 2);
-    p->marks = aligned(sizeof(unsigned long long) * 3 * CFA_ATTEND_BLOCKS);
+    p->marks = aligned(sizeof(unsigned long long) * 2 * CFA_ATTEND_BLOCKS);
     p->total = p->marks + aligned(part * 2 * CFA_ATTEND_BLOCKS);
     return CFA_OK;
 }
