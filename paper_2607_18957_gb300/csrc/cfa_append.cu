@@ -16,7 +16,7 @@ using namespace cfa_dev;
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kTokens = 8; /* of a block, at most */
 
 template <typename CT, int N>
@@ -40,7 +40,7 @@ struct Split {
 };
 
 template <typename T, typename CT, int VEC>
-__global__ void __launch_bounds__(kThreads) cfa_append_kernel(const cfa_append_args a, const Split s)
+__global__ void __launch_bounds__(kThreads, 12) cfa_append_kernel(const cfa_append_args a, const Split s)
 {
     extern __shared__ float2 turn[]; /* [tokens][rotary_dim / 2] cos, sin */
     __shared__ int64_t page_of[kTokens];

@@ -1035,7 +1035,8 @@ template <typename T, int D, int NT, bool F8> cudaError_t launch(const Work &w, 
 {
     using S = Shape<D, NT, F8>;
     const void *fn = reinterpret_cast<const void *>(&cfa_attend_kernel<T, D, NT, F8>);
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_shared(fn, S::kSmem, done);
     if (e) return e;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;

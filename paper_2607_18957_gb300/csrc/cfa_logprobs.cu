@@ -495,12 +495,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2)
 
 template <typename T> cudaError_t launch(const cfa_logprobs_args &a, cudaStream_t stream)
 {
-    /* Few rows: a cluster of blocks for each, as long as there are SMs for them and columns.  Many: small
-     * blocks with more loads each, whose ends meet others' streams (2048 rows of 128,256 bf16 logits: 128
-     * threads of 8 loads 101 us, of 4 106, 256 threads of 4 116). */
-    int blocks = kMaxCluster;
-    while (blocks > 1 && (a.rows * blocks > 4 * 152 || a.cols < 4096 * (blocks / 2))) blocks /= 2;
-    const int threads = blocks > 1 ? 512 : 128;
+    /* So many threads to a row that the rows fill the SMs, but that each has some loads; a cluster of blocks
+     * where one does not hold them.  Many rows get small blocks with more loads at a time, whose ends meet
+     * others' streams (2048 rows of 128,256 bf16 logits: 128 threads of 8 loads 101 us, of 4 106, 256 threads
+     * of 4 116; 116 rows of 18,319: one block of 512 to each 10.8 us, clusters of four 19.8). */
+    const int64_t loads = a.cols * (int64_t)sizeof(T) / 16;
+    int64_t threads_of_row = 152 * 1024 / a.rows;
+    if (threads_of_row > loads / 4) threads_of_row = loads / 4;
+    int blocks = 1, threads = 128;
+    while (threads < 512 && 2 * threads <= threads_of_row) threads *= 2;
+    while (blocks < kMaxCluster && 2 * blocks * threads <= threads_of_row) blocks *= 2;
     const void *fn = blocks > 1 ? reinterpret_cast<const void *>(&cfa_logprobs_kernel<T, 4>)
                                 : reinterpret_cast<const void *>(&cfa_logprobs_kernel<T, 8>);
     cudaLaunchConfig_t cfg = {};

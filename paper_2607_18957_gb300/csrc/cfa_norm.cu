@@ -448,7 +448,8 @@ cudaError_t launch_rows(const cfa_norm_args &a, cudaStream_t stream, bool *fits)
     if (!*fits) return cudaSuccess;
     const int64_t most = (a.tokens + side - 1) / side;
     const void *fn = reinterpret_cast<const void *>(&cfa_norm_rows_kernel<T, NV, SHIFT>);
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_shared(fn, kRoom, done);
     if (e) return e;
     cfa_launch_ctl ctl = {};
     ctl.flags = CFA_LAUNCH_EARLY;

@@ -7,12 +7,27 @@
 
 #include <math.h>
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "cfa_device.cuh"
 
 namespace cfa_dev {
+
+/* Lets kernel fn have so much shared memory, once per device (`done` has a bit for each that knows). */
+inline cudaError_t allow_shared(const void *fn, int bytes, std::atomic<uint64_t> &done)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (!e) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 constexpr uint32_t kAllLanes = 0xFFFFFFFFu;
 

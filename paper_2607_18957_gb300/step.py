@@ -30,9 +30,13 @@ _ATTEND_BYTES = {}  # workspace bytes by a call's sizes
 
 def _like(t, name, device, shape, dtype, cols):
     """(address, row stride) of an operand that is shaped and typed like another."""
-    _on(t, name, device)
+    if t.get_device() != device or t.requires_grad:
+        _on(t, name, device)
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    _on(t, name, device)
     return t.data_ptr(), _rows(t, name, cols)[1]
 
 
@@ -51,9 +55,11 @@ def norm(x, weight, *, residual=None, gate=None, activation="silu", post_weight=
     """
     if ops.torch is None:
         ops._start()
-    torch = ops.torch
     device = x.get_device()
-    _on(x, "x", device)
+    if device < 0 or weight.get_device() != device or (
+            ops._grad() and (x.requires_grad or weight.requires_grad)):
+        _on(x, "x", device)
+        _on(weight, "weight", device)
     if stream is not None or device != ops._device():
         with _elsewhere(stream, device):
             return norm(x, weight, residual=residual, gate=gate, activation=activation,
@@ -61,14 +67,19 @@ def norm(x, weight, *, residual=None, gate=None, activation="silu", post_weight=
     shape, dtype = x.shape, x.dtype
     cols = shape[-1] if shape else 0
     if len(shape) == 2 and cols:
-        t, xs = shape[0], x.stride(0)
+        t = shape[0]
+        xs, one = x.stride()
+        if one != 1 and cols > 1:
+            _on(x, "x", device)
     else:
+        _on(x, "x", device)
         t, xs = _rows(x, "x", cols)
-    code = _code(x, "x")
-    _on(weight, "weight", device)
+    code = ops._CODE.get(dtype) or _code(x, "x")
     if weight.shape != (cols,):
         raise ValueError(f"weight: shape {tuple(weight.shape)}, not ({cols},)")
-    wcode = _code(weight, "weight")
+    if not weight.is_contiguous():
+        _on(weight, "weight", device)
+    wcode = ops._CODE.get(weight.dtype) or _code(weight, "weight")
     pp = rp = rs = gp = gs = hp = hs = act = 0
     if post_weight is not None:
         _on(post_weight, "post_weight", device)
@@ -89,6 +100,7 @@ def norm(x, weight, *, residual=None, gate=None, activation="silu", post_weight=
         rp, rs = _like(residual, "residual", device, shape, dtype, cols)
     y = h = None
     if out is None:
+        torch = ops.torch
         y = torch.empty(shape, dtype=dtype, device=x.device)
         ys = cols
         if residual is not None:
@@ -153,9 +165,9 @@ def rotary_frequencies(dim, base=10000.0, *, scaling=None, factor=1.0, length=No
 
 def _ints(t, name, device, shape):
     """The address of an int32 operand."""
-    torch = ops.torch
-    _on(t, name, device)
-    if t.shape != shape or t.dtype is not torch.int32 or not t.is_contiguous():
+    if t.get_device() != device:
+        _on(t, name, device)
+    if t.shape != shape or t.dtype is not ops.torch.int32 or not t.is_contiguous():
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, not a contiguous torch.int32 "
                          f"{tuple(shape)}")
     return t.data_ptr()
@@ -163,17 +175,19 @@ def _ints(t, name, device, shape):
 
 def _cache(k, v, dtype, code, device):
     """Checks a paged cache: (its dtype's code, the strides of k and of v)."""
-    torch = ops.torch
-    _on(k, "k_cache", device)
-    _on(v, "v_cache", device)
-    if len(k.shape) != 4 or v.shape != k.shape or v.dtype is not k.dtype:
+    ks, vs = k.stride(), v.stride()
+    if (k.get_device() != device or v.get_device() != device or ks[-1] != 1 or vs[-1] != 1 or
+            k.requires_grad or v.requires_grad):
+        _on(k, "k_cache", device)
+        _on(v, "v_cache", device)
+    if len(ks) != 4 or v.shape != k.shape or v.dtype is not k.dtype:
         raise ValueError(f"k_cache {k.dtype} {tuple(k.shape)} and v_cache {v.dtype} {tuple(v.shape)} "
                          "are both [pages, page_size, kv_heads, head_dim]")
     if k.dtype is not dtype:
-        if k.dtype is not torch.float8_e4m3fn:
+        if k.dtype is not ops.torch.float8_e4m3fn:
             raise ValueError(f"the cache is {k.dtype}, not {dtype} or torch.float8_e4m3fn")
         code = F8_E4M3
-    return code, k.stride()[:3], v.stride()[:3]
+    return code, ks[:3], vs[:3]
 
 
 def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=None,
@@ -315,23 +329,25 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
     if scale is None:
         scale = dim ** -0.5
 
-    def packed(ws, size):
-        return _ATTEND.pack(
-            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), np_, o.data_ptr(),
-            lp, ws, size, b, qs, os_, pages.stride(0), *ks, *vs, new, pages.shape[1], cache_pages,
-            page_size, heads, kv, dim, window, code, ccode, 0, scale, k_scale, v_scale)
     sizes = (new, heads, kv, dim)
     need = _ATTEND_BYTES.get(sizes)
+    args = (b, qs, os_, pages.stride(0), *ks, *vs, new, pages.shape[1], cache_pages, page_size, heads, kv,
+            dim, window, code, ccode, 0, scale, k_scale, v_scale)
+    ptrs = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), np_, o.data_ptr(), lp)
     if need is None:
         size = _lib.ctypes.c_uint64()
-        _check(ops._lib_c.cfa_attend_workspace(packed(0, 0), _lib.ctypes.byref(size)))
+        _check(ops._lib_c.cfa_attend_workspace(_ATTEND.pack(*ptrs, 0, 0, *args),
+                                               _lib.ctypes.byref(size)))
         if len(_ATTEND_BYTES) >= 1024:
             _ATTEND_BYTES.clear()
         need = _ATTEND_BYTES[sizes] = size.value
-    workspace = ops._workspace(workspace, need, q.device)
-    st = ops._lib_c.cfa_attend_async(
-        packed(workspace.data_ptr(), workspace.numel() * workspace.element_size()),
-        ops._raw_stream(device))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    else:
+        ops._workspace(workspace, need, q.device)
+        need = workspace.numel() * workspace.element_size()
+    st = ops._lib_c.cfa_attend_async(_ATTEND.pack(*ptrs, workspace.data_ptr(), need, *args),
+                                     ops._raw_stream(device))
     if st:
         _check(st)
     return (o, sums) if lse else o
@@ -366,14 +382,14 @@ def logprobs(logits, tokens, *, top=0, scale=1.0, out=None, stream=None):
     tp = _ints(tokens, "tokens", device, lead)
     top = int(top)
     if out is None:
-        on = logits.device
-        out = (torch.empty(lead, dtype=torch.float32, device=on),
-               torch.empty(lead, dtype=torch.float32, device=on))
+        on, f32 = logits.device, torch.float32
+        out = (torch.empty(lead, dtype=f32, device=on), torch.empty(lead, dtype=f32, device=on))
         if top:
             if top < 0:
                 raise ValueError(f"top is {top}")
-            out += (torch.empty(lead + (top,), dtype=torch.float32, device=on),
-                    torch.empty(lead + (top,), dtype=torch.int32, device=on))
+            best = lead + (top,)
+            out += (torch.empty(best, dtype=f32, device=on),
+                    torch.empty(best, dtype=torch.int32, device=on))
     else:
         out = tuple(out)
         want = [(lead, torch.float32), (lead, torch.float32)]
