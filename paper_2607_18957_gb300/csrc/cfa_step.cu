@@ -139,9 +139,8 @@ extern "C" cfa_status cfa_append_async(const cfa_append_args *a, cfa_stream stre
     if (a->rotary_dim < 0 || a->rotary_dim > a->head_dim || a->rotary_dim % 2)
         return refuse(CFA_ERR_INVAL, "cfa_append: %d of %d values turn", a->rotary_dim, a->head_dim);
     if (a->flags & ~CFA_APPEND_INTERLEAVED) return refuse(CFA_ERR_INVAL, "cfa_append: unknown flags");
-    if (a->rotary_dim ? !a->positions || !a->frequencies || !std::isfinite(a->magnitude)
-                      : a->positions || a->frequencies)
-        return refuse(CFA_ERR_INVAL, "cfa_append: positions and frequencies belong to values that turn");
+    if (a->rotary_dim && !std::isfinite(a->magnitude))
+        return refuse(CFA_ERR_INVAL, "cfa_append: magnitude %g", a->magnitude);
     const int64_t q_cols = (int64_t)a->heads * a->head_dim;
     const int64_t cols = q_cols + 2 * (int64_t)a->kv_heads * a->head_dim;
     if (a->tokens > 1 && (a->qkv_stride < cols || a->qkv_stride >= kMost ||
@@ -158,6 +157,8 @@ extern "C" cfa_status cfa_append_async(const cfa_append_args *a, cfa_stream stre
     if (a->tokens == 0) return CFA_OK;
     if (!a->qkv || !a->slots || (a->pages && (!a->k_cache || !a->v_cache)))
         return refuse(CFA_ERR_INVAL, "cfa_append: NULL qkv, slots or cache");
+    if (a->rotary_dim ? !a->positions || !a->frequencies : a->positions || a->frequencies)
+        return refuse(CFA_ERR_INVAL, "cfa_append: positions and frequencies belong to values that turn");
     if (off_grid(a->qkv, 2) || off_grid(a->q, 2) || off_grid(a->k_cache, cs) ||
         off_grid(a->v_cache, cs) || off_grid(a->positions, 4) || off_grid(a->slots, 4) ||
         off_grid(a->frequencies, 8))
