@@ -327,6 +327,7 @@ __global__ void __launch_bounds__(1024) cfa_norm_rows_kernel(const cfa_norm_args
             if (c < cols) S::weight(a.weight, held, none, 0, f32, c, a.offset, w[i]);
         }
     }
+    const float per_col = 1.0f / (float)cols;
     int stage = 0, odd = 0;
     /* every thread of a block goes through as many rows: the sums want all of them */
     for (int64_t first = (int64_t)blockIdx.x * side; first < a.tokens; first += step, row += step) {
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(1024) cfa_norm_rows_kernel(const cfa_norm_args
             for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) sum += h[i][k] * h[i][k];
-            const float unit = 1.0f / sqrtf(block_sum(sum, lanes, part[odd][0]) / (float)cols + a.eps);
+            const float unit = rsqrtf(block_sum(sum, lanes, part[odd][0]) * per_col + a.eps);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (here && c[i] < cols) {
@@ -404,7 +405,7 @@ __global__ void __launch_bounds__(1024) cfa_norm_rows_kernel(const cfa_norm_args
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) sum += h[i][k] * h[i][k];
             }
-        const float unit = 1.0f / sqrtf(block_sum(sum, lanes, part[odd][1]) / (float)cols + a.eps);
+        const float unit = rsqrtf(block_sum(sum, lanes, part[odd][1]) * per_col + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (here && c[i] < cols) {
