@@ -740,6 +740,12 @@ cfa_status cfa_experts_async(const cfa_experts_args *args, cfa_stream stream);
 /* ---- operators of a decoding step around the products ------------------------------------- */
 
 /*
+ * What a decoding step runs beside the products: the norms between blocks, the way of keys and values into
+ * a paged cache, the attention over it, and the log probabilities of tokens.  Conventions and errors are
+ * those of the operators above.
+ */
+
+/*
  * Norms between blocks, on rows of cols values:
  *   a = x, or with a post_weight (a norm behind the block) N(x) * (offset + post_weight)
  *   a = a * act(gate)                    where there is a gate
@@ -836,7 +842,9 @@ cfa_status cfa_append_async(const cfa_append_args *args, cfa_stream stream);
  * out are held in fp32; probabilities enter the second product as sums of two 16-bit values (in F16, or with
  * an 8-bit cache, those below 2^-28 of a row's largest count as 0).
  * head_dim is 64, 96, 128 or 256; q, out and the caches lie on the 16-byte grid with all their strides
- * (CFA_ERR_ALIGN).  max_pages * page_size is at most 2^30.
+ * (CFA_ERR_ALIGN).  max_pages * page_size is at most 2^30, new_tokens * heads / kv_heads at most 2^18.  The
+ * keys are read once for every 16 rows of a key head (8 with a head_dim of 256), which suits few new tokens.
+ * The workspace's content need not be set up.
  */
 typedef struct cfa_attend_args {
     const void *q, *k_cache, *v_cache;

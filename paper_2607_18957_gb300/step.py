@@ -5,7 +5,8 @@ tokens.  Forward passes for serving; argument marshalling only.
 
 As the operators of ops.py, the calls enqueue on `stream` (a torch stream of the operands' device or a
 stream's handle; default: torch's current stream there) and return at once; outputs and workspaces that
-a call makes come from torch's allocator, on that stream.
+a call makes come from torch's allocator, on that stream.  attend keeps its workspace for the stream's next
+call (a captured call gets one of its own, which the graph keeps).
 """
 import math
 import struct
@@ -26,6 +27,7 @@ SIZES = {"cfa_norm_args": _NORM.size, "cfa_append_args": _APPEND.size,
          "cfa_attend_args": _ATTEND.size,
          "cfa_logprobs_args": _LOGPROBS.size}
 _ATTEND_BYTES = {}  # workspace bytes by a call's sizes
+_KEPT = {}          # attend's workspaces, by device and stream: its calls there follow one another
 
 
 def _like(t, name, device, shape, dtype, cols):
@@ -271,7 +273,7 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
               and -inf
     scale     of the scores (default: D ** -0.5)
     out       like q; with lse=True (out, lse)
-    workspace  uint8 tensor (default: allocated; its size is cfa_attend_workspace of cfa.h)
+    workspace  uint8 tensor (default: the stream's; its size is cfa_attend_workspace of cfa.h)
     """
     if ops.torch is None:
         ops._start()
@@ -341,13 +343,20 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
         if len(_ATTEND_BYTES) >= 1024:
             _ATTEND_BYTES.clear()
         need = _ATTEND_BYTES[sizes] = size.value
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    else:
+    on = ops._raw_stream(device)
+    if workspace is not None:
         ops._workspace(workspace, need, q.device)
         need = workspace.numel() * workspace.element_size()
-    st = ops._lib_c.cfa_attend_async(_ATTEND.pack(*ptrs, workspace.data_ptr(), need, *args),
-                                     ops._raw_stream(device))
+    elif torch.cuda.is_current_stream_capturing():
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    else:
+        workspace = _KEPT.get((device, on))
+        if workspace is None or workspace.numel() < need:
+            if len(_KEPT) >= 64:
+                _KEPT.clear()
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            _KEPT[device, on] = workspace
+    st = ops._lib_c.cfa_attend_async(_ATTEND.pack(*ptrs, workspace.data_ptr(), need, *args), on)
     if st:
         _check(st)
     return (o, sums) if lse else o

@@ -132,6 +132,39 @@ def test_a_graph_follows_lengths_and_shares_its_workspace():
             torch.cuda.synchronize()
 
 
+def test_workspaces_are_the_streams():
+    """Eager calls keep one per stream, grown where a call needs more; captured ones have their own."""
+    from paper_2607_18957_gb300 import step
+    small, large = operands(6, heads=2, kv=2, dim=64), operands(7, heads=32, kv=2, dim=128)
+    want = [cfa.attend(**o, lse=True) for o in (small, large)]
+    torch.cuda.synchronize()
+    step._KEPT.clear()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a = cfa.attend(**small, lse=True)
+        kept = step._KEPT[0, s.cuda_stream]
+        b = cfa.attend(**large, lse=True)
+        assert step._KEPT[0, s.cuda_stream].numel() > kept.numel() and len(step._KEPT) == 1
+        kept = step._KEPT[0, s.cuda_stream]
+        c = cfa.attend(**small, lse=True)
+        assert step._KEPT[0, s.cuda_stream] is kept
+    s.synchronize()
+    assert same(a, want[0]) and same(b, want[1]) and same(c, want[0])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        r = cfa.attend(**large, lse=True)
+    assert len(step._KEPT) == 1 and step._KEPT[0, s.cuda_stream] is kept
+    # replays on another stream beside eager calls on the stream of the capture
+    other = torch.cuda.Stream()
+    for _ in range(20):
+        with torch.cuda.stream(other):
+            g.replay()
+        with torch.cuda.stream(s):
+            b = cfa.attend(**large, lse=True)
+    torch.cuda.synchronize()
+    assert same(r, want[1]) and same(b, want[1])
+
+
 def test_two_streams_at_once():
     """Calls that overlap, each with a workspace of its own."""
     a = [operands(i, keys=20000) for i in range(2)]
