@@ -3,7 +3,8 @@
 Bounds, element by element, with u = 2^-24: a score of D products in fp32, truncated by the tensor cores,
 is off by (D + 8) 2 u of the sum of the products' magnitudes, and by 4 u of itself where it is scaled;
 an exponential by what its argument's error makes of it and 2^-21; a probability that enters the second
-product as two 16-bit values by 2^-17.  A warp adds the keys of its share one after another: shares are
+product as two 16-bit values by 2^-17, as one fp16 value (bf16 queries over 8-bit values) by half of fp16's
+step, 2^-11.  A warp adds the keys of its share one after another: shares are
 the slots of 16 keys of all rows' tiles over 152 blocks of at least four warps, each slot 32 truncated
 additions, and up to 160 joins follow.  The result is rounded once."""
 import math
@@ -114,7 +115,8 @@ class Setup:
                 p = torch.softmax(z, 2)
                 ref = torch.einsum("hgn,nhd->hgd", p, v[see])
                 mag = torch.einsum("hgn,nhd->hgd", p, v[see].abs())
-                rel = (2 * ez + 2.0 ** -16 + 2 * (chain + 8) * 2 * U)[:, :, None]
+                once = 2.0 ** -11 if self.dtype is BF16 and self.k.dtype is F8 else 0.0
+                rel = (2 * ez + once + 2.0 ** -16 + 2 * (chain + 8) * 2 * U)[:, :, None]
                 e = mag * rel * (1 + rel)
                 e = e + HALF_ULP[self.dtype] * (ref.abs() + e) + NEAR_ZERO[self.dtype]
                 assert bool(torch.isfinite(got).all())
