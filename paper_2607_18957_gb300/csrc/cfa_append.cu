@@ -6,6 +6,11 @@
  * angle in turns is the product of the position and the frequency in units of 2^-64 turns, modulo 2^64:
  * whole numbers, so that a far position loses nothing of its fraction, and no table is read.  A block
  * computes the sines and cosines of its tokens once and every head takes them from shared memory.
+ *
+ * Bound by memory: 8192 tokens of 64 + 2 * 8 heads of 128 bf16 59 us (5.6 TB/s, 0.83 of a copy; the sines
+ * come before a block's loads, which other blocks' hide in part), one token 2.4 us.  Blocks of 128 threads,
+ * two tokens of 64 pairs each: 256 threads 60 us, 512 73; two, one and eight tokens a block of 256 64, 75
+ * and 71.
  */
 #include <cuda_fp8.h>
 

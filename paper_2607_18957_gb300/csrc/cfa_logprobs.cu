@@ -16,6 +16,11 @@
  *
  * A row belongs to one block or to a cluster of blocks, whose results meet in the first one's shared
  * memory.
+ *
+ * Bound by memory with fp32 logits (2048 rows of 128,256 163 us, 0.95 of a copy); with 16-bit ones, which come
+ * twice as fast, by memory, exponentials and issue slots together (101 us, 5.2 TB/s).  Two values an
+ * instruction for t and the sums, and the largest two at a time, took it there from 132 us; a ring in shared
+ * memory in front of it was slower (98 us without the best, against 91).  One row with its 20 best 8.4 us.
  */
 #include <cooperative_groups.h>
 

