@@ -235,6 +235,13 @@ def test_large_scores():
     Setup([300, 2000], 8, 2, 128, scale=3.0).check(scale=-0.3)
 
 
+@pytest.mark.parametrize("cdtype", [F16, F8])
+@pytest.mark.parametrize("scale", [0.0, 1e-42, -1e-42, -0.1])
+def test_scales_around_zero(scale, cdtype):
+    """Down to where scale and the keys' scale together leave fp32: all keys count alike."""
+    Setup([100, 1, 33], 8, 2, 128, F16, cdtype).check(scale=scale)
+
+
 @pytest.mark.parametrize("heads,kv,dim,cdtype", [(8, 1, 128, BF16), (64, 8, 128, BF16), (16, 2, 256, F8),
                                                  (4, 4, 64, BF16)])
 def test_long_sequences_over_many_blocks(heads, kv, dim, cdtype):
