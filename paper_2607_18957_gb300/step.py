@@ -211,30 +211,36 @@ def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=N
         ops._start()
     torch = ops.torch
     device = qkv.get_device()
-    _on(qkv, "qkv", device)
+    if device < 0 or qkv.requires_grad:
+        _on(qkv, "qkv", device)
     if stream is not None or device != ops._device():
         with _elsewhere(stream, device):
             return append(qkv, k_cache, v_cache, slots, heads=heads, positions=positions,
                           frequencies=frequencies, interleaved=interleaved, magnitude=magnitude,
                           k_scale=k_scale, v_scale=v_scale, out=out)
-    dtype = qkv.dtype
-    code = _code(qkv, "qkv")
+    dtype, shape = qkv.dtype, qkv.shape
+    code = ops._CODE.get(dtype) or _code(qkv, "qkv")
     ccode, ks, vs = _cache(k_cache, v_cache, dtype, code, device)
     pages, page_size, kv, dim = k_cache.shape
-    if heads < 1 or len(qkv.shape) != 2 or qkv.shape[1] != (heads + 2 * kv) * dim:
-        raise ValueError(f"qkv: {tuple(qkv.shape)}, not rows of ({heads} + 2 * {kv}) * {dim}")
-    t, xs = qkv.shape[0], qkv.stride(0)
+    if heads < 1 or len(shape) != 2 or shape[1] != (heads + 2 * kv) * dim:
+        raise ValueError(f"qkv: {tuple(shape)}, not rows of ({heads} + 2 * {kv}) * {dim}")
+    t = shape[0]
+    xs, one = qkv.stride()
+    if one != 1:
+        _on(qkv, "qkv", device)
     sp = _ints(slots, "slots", device, (t,))
     if (positions is None) != (frequencies is None):
         raise ValueError("positions and frequencies belong together")
     pp = fp = qp = qs = rot = 0
     if positions is not None:
         pp = _ints(positions, "positions", device, (t,))
-        _on(frequencies, "frequencies", device)
-        if frequencies.dtype is not torch.float64 or len(frequencies.shape) != 1:
-            raise ValueError(f"frequencies: {frequencies.dtype} {tuple(frequencies.shape)}, not "
-                             "torch.float64 (R / 2,)")
-        rot = 2 * frequencies.shape[0]
+        if frequencies.get_device() != device or not frequencies.is_contiguous():
+            _on(frequencies, "frequencies", device)
+        pairs = frequencies.shape
+        if frequencies.dtype is not torch.float64 or len(pairs) != 1:
+            raise ValueError(f"frequencies: {frequencies.dtype} {tuple(pairs)}, not torch.float64 "
+                             "(R / 2,)")
+        rot = 2 * pairs[0]
         fp = frequencies.data_ptr()
     shape = (t, heads, dim)
     if out is not None:
@@ -279,31 +285,36 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
         ops._start()
     torch = ops.torch
     device = q.get_device()
-    _on(q, "q", device)
+    if device < 0 or q.requires_grad:
+        _on(q, "q", device)
     if stream is not None or device != ops._device():
         with _elsewhere(stream, device):
             return attend(q, k_cache, v_cache, pages, lengths, scale=scale, window=window,
                           k_scale=k_scale, v_scale=v_scale, lse=lse, out=out, workspace=workspace)
     shape, dtype = q.shape, q.dtype
-    code = _code(q, "q")
+    code = ops._CODE.get(dtype) or _code(q, "q")
     ccode, ks, vs = _cache(k_cache, v_cache, dtype, code, device)
     cache_pages, page_size, kv, dim = k_cache.shape
     if len(shape) == 3:
         (b, heads, d), new = shape, 1
-        rows = q
     elif len(shape) == 4:
         b, new, heads, d = shape
-        rows = q.flatten(0, 1) if q.is_contiguous() else q.view(b * new, heads, d)
     else:
         raise ValueError(f"q: shape {tuple(shape)}")
     if d != dim:
         raise ValueError(f"q has heads of {d}, the cache of {dim}")
-    if heads > 1 and q.stride(-2) != dim:
-        raise ValueError("q: the heads of a token must lie side by side")
-    qs = rows.stride(0)
-    _on(pages, "pages", device)
-    if len(pages.shape) != 2 or pages.shape[0] != b or pages.dtype is not torch.int32:
-        raise ValueError(f"pages: {pages.dtype} {tuple(pages.shape)}, not torch.int32 ({b}, P)")
+    if q.is_contiguous():
+        qs = heads * dim
+    else:
+        _on(q, "q", device)
+        if heads > 1 and q.stride(-2) != dim:
+            raise ValueError("q: the heads of a token must lie side by side")
+        qs = (q if len(shape) == 3 else q.view(b * new, heads, d)).stride(0)
+    table = pages.shape
+    if pages.get_device() != device or not pages.is_contiguous():
+        _on(pages, "pages", device)
+    if len(table) != 2 or table[0] != b or pages.dtype is not torch.int32:
+        raise ValueError(f"pages: {pages.dtype} {tuple(table)}, not torch.int32 ({b}, P)")
     np_ = _ints(lengths, "lengths", device, (b,))
     lp, sums = 0, None
     if out is None:
@@ -333,7 +344,7 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
 
     sizes = (new, heads, kv, dim)
     need = _ATTEND_BYTES.get(sizes)
-    args = (b, qs, os_, pages.stride(0), *ks, *vs, new, pages.shape[1], cache_pages, page_size, heads, kv,
+    args = (b, qs, os_, pages.stride(0), *ks, *vs, new, table[1], cache_pages, page_size, heads, kv,
             dim, window, code, ccode, 0, scale, k_scale, v_scale)
     ptrs = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), np_, o.data_ptr(), lp)
     if need is None:
@@ -375,18 +386,22 @@ def logprobs(logits, tokens, *, top=0, scale=1.0, out=None, stream=None):
         ops._start()
     torch = ops.torch
     device = logits.get_device()
-    _on(logits, "logits", device)
+    if device < 0 or logits.requires_grad:
+        _on(logits, "logits", device)
     if stream is not None or device != ops._device():
         with _elsewhere(stream, device):
             return logprobs(logits, tokens, top=top, scale=scale, out=out)
     shape = logits.shape
     if len(shape) == 2 and shape[1]:
         rows, cols = shape
-        xs = logits.stride(0)
+        xs, one = logits.stride()
+        if one != 1 and cols > 1:
+            _on(logits, "logits", device)
     else:
+        _on(logits, "logits", device)
         cols = shape[-1] if shape else 0
         rows, xs = _rows(logits, "logits", cols)
-    code = _code(logits, "logits")
+    code = ops._CODE.get(logits.dtype) or _code(logits, "logits")
     lead = shape[:-1]
     tp = _ints(tokens, "tokens", device, lead)
     top = int(top)
