@@ -498,3 +498,40 @@ def test_norm_of_many_rows_apart(extras, lead, dtype):
         mask = torch.ones_like(buf, dtype=torch.bool)
         mask[lead:].as_strided((t, c), (c + e, 1)).fill_(False)
         assert bool((buf[mask] == 7.0).all())
+
+
+@pytest.mark.parametrize("c", [16384, 16383])
+def test_norm_behind_32_bits(c):
+    """140,000 rows: the last ones begin behind 2^32 bytes and 2^31 elements."""
+    t, g = 140000, gen(c)
+    x = torch.zeros(t, c, dtype=BF16, device="cuda")
+    r = torch.zeros(t, c, dtype=BF16, device="cuda")
+    at = [0, 1, 65535, 131071, 131072, t - 2, t - 1]
+    x[at], r[at] = normal(g, (len(at), c), BF16), normal(g, (len(at), c), BF16)
+    w, r0 = normal(g, (c,), BF16), r[at].clone()
+    y, h = cfa.norm(x, w, residual=r, out=(torch.empty_like(x), r))
+    y64, ey, h64, eh = norm64(x[at], w, r0)
+    close(y[at], y64, ey)
+    close(h[at], h64, eh)
+    assert not bool(y[2:65535].any()) and not bool(h[131073:t - 2].any())
+
+
+def test_append_of_many_tokens():
+    """Rows of q/k/v behind 2^32 bytes."""
+    t, heads, kv, dim, page = 360000, 32, 8, 128, 64
+    g = gen(1)
+    qkv = torch.zeros(t, (heads + 2 * kv) * dim, dtype=BF16, device="cuda")
+    at = torch.tensor([0, 1, 174762, 174763, 349525, t - 1], device="cuda")
+    qkv[at] = normal(g, (len(at), qkv.shape[1]), BF16)
+    pages = t // page
+    kc, vc = (torch.empty(pages, page, kv, dim, dtype=BF16, device="cuda") for _ in range(2))
+    slots = torch.arange(t, dtype=torch.int32, device="cuda").flip(0).contiguous()
+    f = torch.tensor(cfa.rotary_frequencies(dim)[0], dtype=torch.float64, device="cuda")
+    positions = torch.arange(t, dtype=torch.int32, device="cuda")
+    q = cfa.append(qkv, kc, vc, slots, heads=heads, positions=positions, frequencies=f)
+    x = qkv[at].double().view(len(at), -1, dim)
+    y, e = turned64(x[:, :heads + kv], positions[at], f, False, 1.0)
+    close(q[at], y[:, :heads], rounded(y[:, :heads], e[:, :heads], BF16))
+    close(kc.view(-1, kv, dim)[t - 1 - at], y[:, heads:], rounded(y[:, heads:], e[:, heads:], BF16))
+    assert torch.equal(vc.view(-1, kv, dim)[t - 1 - at].double(), x[:, heads + kv:])
+    assert not bool(q[2:174762].any()) and not bool(kc.view(-1, kv, dim)[1:t - 1 - 349525].any())
