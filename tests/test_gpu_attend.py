@@ -248,6 +248,18 @@ def test_long_sequences_over_many_blocks(heads, kv, dim, cdtype):
     Setup([20000, 7], heads, kv, dim, BF16, cdtype, page=64).check()
 
 
+@pytest.mark.parametrize("lens,heads,kv,dim,new", [
+    ([200000], 16, 8, 128, 1), ([3, 90000, 120000, 1], 8, 8, 128, 1), ([150000, 30000], 16, 8, 128, 3),
+    ([400000, 31], 8, 8, 64, 1), ([210000], 8, 4, 256, 1), ([90] * 20 + [180000], 9, 9, 128, 1)])
+def test_very_long_sequences(lens, heads, kv, dim, new):
+    """Megabytes to every block, and the same bits every time."""
+    s = Setup(lens, heads, kv, dim, page=10000, new=new)
+    o, lse = s.check()
+    for _ in range(3):
+        again = s.run(lse=True)
+        assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
 def test_many_short_sequences():
     Setup([1 + i * 7 % 40 for i in range(700)], 8, 2, 64, page=8).check()
 
