@@ -4,7 +4,7 @@
  *
  * A pair (a, b) of a head's values turns by position * frequency: (a cos - b sin, b cos + a sin).  The
  * angle in turns is the product of the position and the frequency in units of 2^-64 turns, modulo 2^64:
- * whole numbers, so that a far position loses nothing of its fraction, and no table is read.  A block
+ * whole numbers, so that a far position keeps its fraction, and no table is read.  A block
  * computes the sines and cosines of its tokens once and every head takes them from shared memory.
  *
  * Bound by memory: 8192 tokens of 64 + 2 * 8 heads of 128 bf16 59 us (5.6 TB/s, 0.83 of a copy; the sines
