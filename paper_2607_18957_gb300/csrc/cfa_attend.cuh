@@ -377,8 +377,8 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
     using P = typename std::conditional<F8, __half, T>::type; /* of the probabilities and values */
     constexpr int W = S::kWarps, MT = S::kTiles, ROWS = S::kRows, STAGES = S::kStages;
     extern __shared__ __align__(128) uint8_t smem[];
-    constexpr int FIND = W > 8 ? 512 : W > 4 ? 256 : 128; /* a power of two that is at least the threads */
-    __shared__ uint32_t s_sum[W], s_before[FIND];
+    static_assert((W & (W - 1)) == 0, "");
+    __shared__ uint32_t s_sum[W], s_before[W * 32];
     __shared__ int32_t s_len[W * 32];
     __shared__ Place s_at[W + 1];     /* the borders of the warps' shares */
     __shared__ int64_t s_id[W + 1];   /* the tile that a border lies inside, or -1 */
@@ -421,7 +421,6 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
     }
     s_before[tid] = before;
     s_len[tid] = len;
-    if (tid < FIND - W * 32) s_before[W * 32 + tid] = 0xFFFFFFFFu;
     __syncthreads();
     /* Blocks have equal shares but for one slot, and so have a block's warps; few slots go to as many
      * blocks as have kLeast of them. */
@@ -449,7 +448,7 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
             const uint32_t q = at >> 32 ? (uint32_t)(at / tiles) : (uint32_t)at / (uint32_t)tiles;
             int k = 0;
 #pragma unroll
-            for (int o = FIND / 2; o; o >>= 1)
+            for (int o = W * 16; o; o >>= 1)
                 if (s_before[k + o] <= q) k += o;
             int b = k * per;
             int64_t x = at - s_before[k] * tiles;
@@ -884,9 +883,9 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
         const uint32_t held0 = __ballot_sync(kAllLanes, lane < W && s_part[min(lane, W - 1)][0]);
         const uint32_t held1 = __ballot_sync(kAllLanes, lane < W && s_part[min(lane, W - 1)][1]);
         const int groups = __popc(first_of);
-        int split = W >= 8 ? 8 : 4; /* warps of a group, a power of two */
+        int split = W; /* warps of a group, a power of two */
         while (split > 1 && (split * groups > W || split > MT)) split >>= 1;
-        for (int n = warp / split; n < groups && warp / split < W / split; n += W / split) {
+        for (int n = warp / split; n < groups; n += W / split) {
             const int e = __fns(first_of, 0, n + 1);
             const int last = 31 - __clz(__shfl_sync(kAllLanes, same, e));
             const bool outside = e == 0 || last == W;
