@@ -133,8 +133,9 @@ def rotary_frequencies(dim, base=10000.0, *, scaling=None, factor=1.0, length=No
               frequency is divided by factor and the first by one; "bands": with t the turns that a
               pair makes within `length` positions, pairs of t >= high keep their frequency, those of
               t <= low have it divided, between them smoothly; "ramp": the same, linear in the pair's
-              index between those that turn `fast` and `slow` times, and queries and keys grow by
-              `magnitude` (default 0.1 ln factor + 1)
+              index from the one that turns `fast` times, rounded down but not below 0, to the one that
+              turns `slow` times, rounded up, which may lie behind the last pair; and queries and keys
+              grow by `magnitude` (default 0.1 ln factor + 1)
     """
     if dim < 2 or dim % 2:
         raise ValueError(f"{dim} values do not make pairs")
@@ -155,7 +156,7 @@ def rotary_frequencies(dim, base=10000.0, *, scaling=None, factor=1.0, length=No
         else:
             def index(turns):
                 return half * math.log(length / (turns * 2 * math.pi)) / math.log(base)
-            first, last = max(math.floor(index(fast)), 0), min(math.ceil(index(slow)), half - 1)
+            first, last = max(math.floor(index(fast)), 0), math.ceil(index(slow))
             kept = [1.0 - (i - first) / max(last - first, 1e-3) for i in range(half)]
             grow = 0.1 * math.log(factor) + 1.0
         kept = [min(max(k, 0.0), 1.0) for k in kept]
