@@ -97,7 +97,10 @@ class _On:
 
     def __init__(self, stream, device):
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=device)
+            # torch takes the handle 0 for a request of one of its own streams, and does not know 1
+            # (cudaStreamLegacy): both are the default stream
+            stream = (torch.cuda.ExternalStream(stream, device=device) if stream > 1 else
+                      torch.cuda.default_stream(device))
         self.guard = torch.cuda.stream(stream)
 
     def __enter__(self):

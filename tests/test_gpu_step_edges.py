@@ -1,0 +1,56 @@
+"""A decoding step's operators at the edges of what their documentation allows."""
+import pytest
+import torch
+
+import paper_2607_18957_gb300 as cfa
+from paper_2607_18957_gb300 import ops
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def cuda_device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    torch.cuda.set_device(0)
+
+
+def same(a, b):
+    return all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def attention(seed, lens=(700, 1, 200), heads=8, kv=2, dim=128, page=16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(BF16)
+    b, per = len(lens), (max(lens) + page - 1) // page
+    table = torch.randperm(b * per, generator=g, device="cuda").to(torch.int32).view(b, per)
+    return dict(q=normal(b, heads, dim), k_cache=normal(b * per, page, kv, dim),
+                v_cache=normal(b * per, page, kv, dim), pages=table,
+                lengths=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+
+
+# ---- handles ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("handle", [0, 1])
+def test_handles_of_the_default_stream(handle):
+    """The default stream's own order holds for calls that are given its handle."""
+    norm = cfa.norm(torch.ones(2, 64, device="cuda"), torch.ones(64, device="cuda"))
+    assert norm.shape == (2, 64)
+    with ops._elsewhere(handle, 0):
+        assert ops._raw_stream(0) == torch.cuda.default_stream().cuda_stream
+    big = torch.randn(4096, 4096, device="cuda").to(BF16)
+    x, w = torch.zeros(300, 4096, device="cuda", dtype=BF16), torch.ones(4096, device="cuda", dtype=BF16)
+    for i in range(5):
+        x.zero_()
+        y = big
+        for _ in range(20):
+            y = (big @ y).sign()
+        x.copy_(y[:300] * (i + 1))
+        got = cfa.norm(x, w, stream=handle)
+        then = got.clone()  # on the default stream too, behind the call
+        torch.cuda.synchronize()
+        assert torch.equal(got, cfa.norm(x, w)) and torch.equal(then, got)
