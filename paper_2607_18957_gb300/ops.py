@@ -4,10 +4,13 @@ stacked experts.  Forward passes for serving; argument marshalling only.
 
 Every call enqueues on `stream` (a torch stream of the operands' device or a stream's handle; default:
 torch's current stream there) and returns at once.  Outputs and
-workspaces that a call makes come from torch's allocator, on that stream.  Operands are CUDA tensors
+workspaces that a call makes come from torch's allocator, on that stream.  For the handle
+cudaStreamPerThread, which torch takes for one stream, the calls and what they allocate are on a stream
+of torch's that the thread keeps for it, in the order of the thread's own.  Operands are CUDA tensors
 of one device whose last dimension is contiguous; rows may lie any distance apart.
 """
 import struct
+import threading
 
 from . import _lib
 
@@ -92,22 +95,39 @@ def _rows(t, name, cols):
     return n, stride
 
 
+PER_THREAD = 2  # cudaStreamPerThread
+_thread = threading.local()
+
+
 class _On:
     """A stream that a call enqueues on, current while the call allocates."""
 
     def __init__(self, stream, device):
+        self.around = None
         if isinstance(stream, int):
             # torch takes the handle 0 for a request of one of its own streams, and does not know 1
             # (cudaStreamLegacy): both are the default stream
-            stream = (torch.cuda.ExternalStream(stream, device=device) if stream > 1 else
-                      torch.cuda.default_stream(device))
+            handle, stream = stream, (torch.cuda.ExternalStream(stream, device=device) if stream > 1 else
+                                      torch.cuda.default_stream(device))
+            if handle == PER_THREAD:
+                # One handle, a stream in every thread: torch's allocator would give a thread what
+                # another's kernels still use.  A stream of torch's stands in for the thread's own.
+                self.around, own = stream, _thread.__dict__
+                stream = own.get(device)
+                if stream is None:
+                    stream = own[device] = torch.cuda.Stream(device)
+        self.stream = stream
         self.guard = torch.cuda.stream(stream)
 
     def __enter__(self):
+        if self.around is not None:
+            self.stream.wait_stream(self.around)
         self.guard.__enter__()
 
     def __exit__(self, *exc):
         self.guard.__exit__(*exc)
+        if self.around is not None:
+            self.around.wait_stream(self.stream)
 
 
 def _elsewhere(stream, device):

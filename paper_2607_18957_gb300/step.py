@@ -292,6 +292,10 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
         with _elsewhere(stream, device):
             return attend(q, k_cache, v_cache, pages, lengths, scale=scale, window=window,
                           k_scale=k_scale, v_scale=v_scale, lse=lse, out=out, workspace=workspace)
+    on = ops._raw_stream(device)
+    if on == ops.PER_THREAD:  # torch's current stream: its workspace is to be the thread's all the same
+        return attend(q, k_cache, v_cache, pages, lengths, scale=scale, window=window, k_scale=k_scale,
+                      v_scale=v_scale, lse=lse, out=out, workspace=workspace, stream=on)
     shape, dtype = q.shape, q.dtype
     code = ops._CODE.get(dtype) or _code(q, "q")
     ccode, ks, vs = _cache(k_cache, v_cache, dtype, code, device)
@@ -355,7 +359,6 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
         if len(_ATTEND_BYTES) >= 1024:
             _ATTEND_BYTES.clear()
         need = _ATTEND_BYTES[sizes] = size.value
-    on = ops._raw_stream(device)
     if workspace is not None:
         ops._workspace(workspace, need, q.device)
         need = workspace.numel() * workspace.element_size()

@@ -1,4 +1,6 @@
 """A decoding step's operators at the edges of what their documentation allows."""
+import threading
+
 import pytest
 import torch
 
@@ -54,3 +56,49 @@ def test_handles_of_the_default_stream(handle):
         then = got.clone()  # on the default stream too, behind the call
         torch.cuda.synchronize()
         assert torch.equal(got, cfa.norm(x, w)) and torch.equal(then, got)
+
+
+def test_a_call_is_in_the_order_of_the_threads_own_stream():
+    own = torch.cuda.ExternalStream(2)
+    big = torch.randn(4096, 4096, device="cuda").to(BF16)
+    x, w = torch.zeros(300, 4096, device="cuda", dtype=BF16), torch.ones(4096, device="cuda", dtype=BF16)
+    torch.cuda.synchronize()
+    for i in range(5):
+        with torch.cuda.stream(own):
+            x.zero_()
+            y = big
+            for _ in range(20):
+                y = (big @ y).sign()
+            x.copy_(y[:300] * (i + 1))
+            got = cfa.norm(x, w, stream=2)
+            then = got.clone()
+        own.synchronize()
+        assert torch.equal(got, cfa.norm(x, w)) and torch.equal(then, got)
+
+
+@pytest.mark.parametrize("current", [False, True])
+def test_threads_with_streams_of_their_own(current):
+    """Two threads' calls on cudaStreamPerThread, given or torch's current one, which overlap: the bits of
+    calls in turn."""
+    inputs = [attention(i, (60000, 30000)) for i in range(2)]
+    want = [[t.clone() for t in cfa.attend(**a, lse=True)] for a in inputs]
+    torch.cuda.synchronize()
+    wrong, start = [], threading.Barrier(2)
+
+    def work(i):
+        own = torch.cuda.ExternalStream(2)
+        start.wait()
+        for _ in range(40):
+            if current:
+                with torch.cuda.stream(own):
+                    got = [cfa.attend(**inputs[i], lse=True) for _ in range(5)]
+            else:
+                got = [cfa.attend(**inputs[i], lse=True, stream=2) for _ in range(5)]
+            own.synchronize()
+            wrong.extend(i for g in got if not same(g, want[i]))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert wrong == []

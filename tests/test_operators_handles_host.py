@@ -1,4 +1,7 @@
 """Streams that the operators' calls are given as handles, without a GPU: stand-ins for torch's streams."""
+import itertools
+import threading
+
 import pytest
 import torch
 
@@ -39,6 +42,8 @@ def log(monkeypatch):
             raise RuntimeError("invalid StreamId1")
         return Stream(f"{handle} on {device}")
 
+    numbers = itertools.count()
+    monkeypatch.setattr(torch.cuda, "Stream", lambda device: Stream(f"own {next(numbers)} on {device}"))
     monkeypatch.setattr(torch.cuda, "ExternalStream", external)
     monkeypatch.setattr(torch.cuda, "default_stream", lambda device: Stream(f"default on {device}"))
     monkeypatch.setattr(torch.cuda, "stream", Guard)
@@ -51,3 +56,24 @@ def test_handles_name_their_streams(log, handle, name):
     with ops._elsewhere(handle, 3):
         log.append("call")
     assert log == [("enter", name), "call", ("exit", name)]
+
+
+def test_every_thread_has_a_stream_in_the_place_of_the_handle_that_names_its_own(log):
+    """cudaStreamPerThread, 2, is another stream in every thread: calls go to a stream of the thread's,
+    between what is before and behind them on that of the handle."""
+    def work(devices):
+        for d in devices:
+            with pytest.raises(KeyError):
+                with ops._elsewhere(2, d):
+                    log.append("call")
+                    raise KeyError  # a refusal leaves the streams joined too
+    for devices in ((0, 0, 1), (0,)):
+        t = threading.Thread(target=work, args=(devices,))
+        t.start()
+        t.join()
+    want = []
+    for own, d in ((0, 0), (0, 0), (1, 1), (2, 0)):
+        own, theirs = f"own {own} on {d}", f"2 on {d}"
+        want += [(own, "waits for", theirs), ("enter", own), "call", ("exit", own),
+                 (theirs, "waits for", own)]
+    assert log == want
