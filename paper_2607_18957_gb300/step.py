@@ -27,7 +27,8 @@ SIZES = {"cfa_norm_args": _NORM.size, "cfa_append_args": _APPEND.size,
          "cfa_attend_args": _ATTEND.size,
          "cfa_logprobs_args": _LOGPROBS.size}
 _ATTEND_BYTES = {}  # workspace bytes by a call's sizes
-_KEPT = {}          # attend's workspaces, by device and stream: its calls there follow one another
+_KEPT = {}          # attend's workspaces, by device and stream of torch's: its calls there follow one another
+_FOREIGN = {}       # those of streams that are not torch's, by device and handle: (workspace, last call's end)
 
 
 def _like(t, name, device, shape, dtype, cols):
@@ -265,6 +266,38 @@ def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=N
     return q
 
 
+def _kept(device, on, need):
+    """A workspace for calls on the current stream, whose handle is `on`, that has none large enough:
+    (the workspace, an event to record behind the call or None).
+
+    torch's streams live as long as the process.  Any other's handle may be another stream's by now,
+    while the first one's last call is still under way: calls there wait for the one before."""
+    torch, key = ops.torch, (device, on)
+    stream = torch.cuda.current_stream(device)
+
+    def empty():
+        return torch.empty(need, dtype=torch.uint8, device=stream.device)
+    if not on or stream.stream_id != on:
+        if len(_KEPT) >= 64:
+            _KEPT.clear()
+        workspace = _KEPT[key] = empty()
+        return workspace, None
+    workspace, last = _FOREIGN.get(key, (None, None))
+    if last is not None:
+        stream.wait_event(last)
+    else:
+        last = torch.cuda.Event()
+        if len(_FOREIGN) >= 64:  # the oldest one's memory is free once its last call is over
+            old, end = _FOREIGN.pop(list(_FOREIGN)[0], (None, None))
+            if old is not None:
+                stream.wait_event(end)
+                old.record_stream(stream)
+    if workspace is None or workspace.numel() < need:
+        workspace = empty()
+    _FOREIGN[key] = workspace, last
+    return workspace, last
+
+
 def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale=1.0, v_scale=1.0,
            lse=False, out=None, workspace=None, stream=None):
     """Attention of new tokens over a paged cache that holds their keys and values already: like q, or
@@ -280,7 +313,8 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
               and -inf
     scale     of the scores (default: D ** -0.5)
     out       like q; with lse=True (out, lse)
-    workspace  uint8 tensor (default: the stream's; its size is cfa_attend_workspace of cfa.h)
+    workspace  uint8 tensor (default: the stream's; its size is cfa_attend_workspace of cfa.h), of which
+              calls that may overlap need one each
     """
     if ops.torch is None:
         ops._start()
@@ -359,6 +393,7 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
         if len(_ATTEND_BYTES) >= 1024:
             _ATTEND_BYTES.clear()
         need = _ATTEND_BYTES[sizes] = size.value
+    last = None
     if workspace is not None:
         ops._workspace(workspace, need, q.device)
         need = workspace.numel() * workspace.element_size()
@@ -367,11 +402,10 @@ def attend(q, k_cache, v_cache, pages, lengths, *, scale=None, window=0, k_scale
     else:
         workspace = _KEPT.get((device, on))
         if workspace is None or workspace.numel() < need:
-            if len(_KEPT) >= 64:
-                _KEPT.clear()
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            _KEPT[device, on] = workspace
+            workspace, last = _kept(device, on, need)
     st = ops._lib_c.cfa_attend_async(_ATTEND.pack(*ptrs, workspace.data_ptr(), need, *args), on)
+    if last is not None:
+        last.record(torch.cuda.current_stream(device))
     if st:
         _check(st)
     return (o, sums) if lse else o

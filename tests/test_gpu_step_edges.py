@@ -1,11 +1,12 @@
 """A decoding step's operators at the edges of what their documentation allows."""
+import ctypes
 import threading
 
 import pytest
 import torch
 
 import paper_2607_18957_gb300 as cfa
-from paper_2607_18957_gb300 import ops
+from paper_2607_18957_gb300 import ops, step
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +103,22 @@ def test_threads_with_streams_of_their_own(current):
     for t in threads:
         t.join()
     assert wrong == []
+
+
+def test_streams_that_are_made_and_destroyed_elsewhere():
+    """Streams that are destroyed while their call is under way: the next gets the same handle, or not."""
+    inputs = [attention(i, (60000, 30000)) for i in range(2)]
+    want = [[t.clone() for t in cfa.attend(**a, lse=True)] for a in inputs]
+    torch.cuda.synchronize()
+    kept = dict(step._KEPT)
+    cudart = torch.cuda.cudart()
+    got = []
+    for i in range(100):
+        handle = ctypes.c_void_p()
+        assert int(cudart.cudaStreamCreate(ctypes.addressof(handle))) == 0
+        got.append(cfa.attend(**inputs[i % 2], lse=True, stream=handle.value))
+        assert (0, handle.value) not in step._KEPT
+        assert int(cudart.cudaStreamDestroy(handle.value)) == 0
+    torch.cuda.synchronize()
+    assert all(same(g, want[i % 2]) for i, g in enumerate(got))
+    assert step._KEPT.keys() == kept.keys() and len(step._FOREIGN) <= 64

@@ -2,8 +2,11 @@
 import math
 
 import pytest
+import torch
 
 import paper_2607_18957_gb300 as cfa
+from paper_2607_18957_gb300 import build as cfa_build
+from paper_2607_18957_gb300 import ops, step
 
 
 @pytest.mark.parametrize("dim,base,length,factor", [
@@ -32,3 +35,65 @@ def test_ramp_leaves_pairs_that_turn_often_alone():
     f, _ = cfa.rotary_frequencies(128, 10000.0, scaling="ramp", factor=8.0, length=131072)
     assert f[45] == pytest.approx(10000.0 ** (-45 / 64), rel=1e-12, abs=0.0)
     assert f[63] == pytest.approx(10000.0 ** (-63 / 64) * (7 / 25 + 18 / 25 / 8), rel=1e-12, abs=0.0)
+
+
+class FakeStream:
+    """torch's current stream: a foreign one's id is its handle."""
+    device = "somewhere"
+
+    def __init__(self, id, log):
+        self.stream_id, self.log = id, log
+
+    def wait_event(self, event):
+        self.log.append(("waits", self.stream_id, event.number))
+
+
+def test_a_foreign_handle_may_name_another_stream_by_now(monkeypatch):
+    """Its kept workspace is used by a call that waits for the one before; torch's own streams need no
+    waits, and an old foreign one's memory goes back only behind its last call."""
+    cfa_build.build()
+    if ops.torch is None:
+        ops._start()
+    log, current = [], []
+
+    class Event:
+        made = 0
+
+        def __init__(self):
+            self.number = Event.made
+            Event.made += 1
+
+    class Memory:
+        def __init__(self, need, **kw):
+            self.need = need
+
+        def numel(self):
+            return self.need
+
+        def record_stream(self, stream):
+            log.append(("kept for", stream.stream_id, self.need))
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: current[-1])
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch, "empty", Memory)
+    monkeypatch.setattr(step, "_KEPT", {})
+    monkeypatch.setattr(step, "_FOREIGN", {})
+
+    def call(handle, need, id=None):
+        current.append(FakeStream(handle if id is None else id, log))
+        return step._kept(0, handle, need)
+    a, last = call(0x1000, 10)
+    assert last.number == 0 and log == []
+    b, again = call(0x1000, 10)
+    assert b is a and again is last and log == [("waits", 0x1000, 0)]
+    c, again = call(0x1000, 20)  # a larger one, behind the call with the smaller
+    assert c is not a and c.need == 20 and again is last and log == 2 * [("waits", 0x1000, 0)]
+    assert step._KEPT == {}
+    del log[:]
+    for handle, id in ((0, 0), (0x2000, 35)):  # torch's default stream and one of its pool
+        w, last = call(handle, 10, id)
+        assert last is None and step._KEPT[0, handle] is w
+    for i in range(64):
+        call(0x10000 + 16 * i, 1)
+    assert log == [("waits", 0x10000 + 16 * 63, 0), ("kept for", 0x10000 + 16 * 63, 20)]
+    assert len(step._FOREIGN) == 64 and (0, 0x1000) not in step._FOREIGN
