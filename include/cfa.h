@@ -793,7 +793,7 @@ cfa_status cfa_norm_async(const cfa_norm_args *args, cfa_stream stream);
  *             rotary_dim 0): nothing turns.  The pair i of the first rotary_dim values of a head, (i, i +
  *             rotary_dim / 2) or with CFA_APPEND_INTERLEAVED (2 i, 2 i + 1), turns by position *
  *             frequencies[i]: (a, b) -> magnitude * (a cos - b sin, b cos + a sin).  The angle is off by
- *             2^-52 of itself at most, its sine and cosine are in fp32
+ *             2^-52 of itself and |position| * 2^-65 turns at most, its sine and cosine are in fp32
  *   slots     [tokens]: where a token's keys and values go.  One below 0 or behind the last page: they go
  *             nowhere.  Two tokens with the same slot leave values of either
  *   q         [tokens, heads * head_dim] of dtype, the turned queries; may be qkv, same address and

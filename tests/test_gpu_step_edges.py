@@ -1,5 +1,6 @@
 """A decoding step's operators at the edges of what their documentation allows."""
 import ctypes
+import math
 import threading
 
 import pytest
@@ -122,3 +123,31 @@ def test_streams_that_are_made_and_destroyed_elsewhere():
     torch.cuda.synchronize()
     assert all(same(g, want[i % 2]) for i, g in enumerate(got))
     assert step._KEPT.keys() == kept.keys() and len(step._FOREIGN) <= 64
+
+
+# ---- angles -------------------------------------------------------------------------------------
+
+def test_angles_of_small_and_negative_frequencies():
+    """Pairs (1, 0), whose second value is the sine alone: bf16 holds it however small it is.  The angle is off
+    by 2^-52 of itself and 2^-65 turns a position, sine and rounding in fp32 by 2^-20 of the sine, the
+    result by half a step, 2^-8."""
+    f = [s * v for v in (1.0, 0.3, 1e-3, 1e-7, 1e-10, 1e-13, 1e-14, 1e-15) for s in (1, -1)]
+    p = [1, 3, 1000, 123456789, (1 << 31) - 1, -1, -77, 1 - (1 << 31)]
+    t, half = len(p), len(f)
+    qkv = torch.zeros(t, 3 * 2 * half, device="cuda", dtype=BF16)
+    qkv[:, :half] = 1.0
+    cache = [torch.zeros(1, t, 1, 2 * half, device="cuda", dtype=BF16) for _ in range(2)]
+    at = torch.arange(t, device="cuda", dtype=torch.int32)
+
+    def turned(sign):
+        return cfa.append(qkv, *cache, at, heads=1,
+                          positions=torch.tensor([sign * x for x in p], dtype=torch.int32, device="cuda"),
+                          frequencies=torch.tensor([sign * x for x in f], dtype=torch.float64, device="cuda"))
+    q = turned(1)
+    for i, x in enumerate(p):
+        for j, v in enumerate(f):
+            want, got = math.sin(x * v), q[i, 0, half + j].item()
+            off = abs(x * v) * 2.0 ** -51 + abs(x) * 2.0 ** -65 * 2 * math.pi + abs(want) * 2.0 ** -20
+            assert abs(got - want) <= off + (abs(want) + off) * 2.0 ** -8, (x, v)
+    # the other way round by a position of the other sign
+    assert torch.equal(turned(-1), q)
