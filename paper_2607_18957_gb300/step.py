@@ -236,7 +236,8 @@ def append(qkv, k_cache, v_cache, slots, *, heads, positions=None, frequencies=N
     pp = fp = qp = qs = rot = 0
     if positions is not None:
         pp = _ints(positions, "positions", device, (t,))
-        if frequencies.get_device() != device or not frequencies.is_contiguous():
+        if (frequencies.get_device() != device or not frequencies.is_contiguous() or
+                frequencies.requires_grad):
             _on(frequencies, "frequencies", device)
         pairs = frequencies.shape
         if frequencies.dtype is not torch.float64 or len(pairs) != 1:

@@ -151,3 +151,14 @@ def test_angles_of_small_and_negative_frequencies():
             assert abs(got - want) <= off + (abs(want) + off) * 2.0 ** -8, (x, v)
     # the other way round by a position of the other sign
     assert torch.equal(turned(-1), q)
+
+
+def test_frequencies_that_want_a_gradient_are_refused():
+    qkv = torch.zeros(2, 3 * 64, device="cuda", dtype=BF16)
+    cache = [torch.zeros(1, 2, 1, 64, device="cuda", dtype=BF16) for _ in range(2)]
+    at = torch.arange(2, device="cuda", dtype=torch.int32)
+    f = torch.zeros(32, device="cuda", dtype=torch.float64, requires_grad=True)
+    with pytest.raises(ValueError, match="frequencies requires a gradient"):
+        cfa.append(qkv, *cache, at, heads=1, positions=at, frequencies=f)
+    with torch.no_grad():
+        cfa.append(qkv, *cache, at, heads=1, positions=at, frequencies=f)
