@@ -574,8 +574,8 @@ __global__ void __launch_bounds__(Shape<D, NT, F8>::kWarps * 32, 1) cfa_attend_k
     float o[MT][NT][4], m[NT][2], l[NT][2];
     int hi_n[NT][2], hi_least = 0, hi_most = 0; /* keys below these are seen */
     /* Scores stay as the products leave them until they are exponents; a scale below 0 turns q round. */
-    /* (not 0: -inf marks what is not seen, and is to stay that) */
-    const float unit = a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * a.k_scale, 1.2e-38f);
+    /* (the least that fp32 has, not 0: -inf marks what is not seen, and is to stay that) */
+    const float unit = a.scale == 0.0f ? 1.0f : fmaxf(fabsf(a.scale) * kLog2e * a.k_scale, 1.4e-45f);
     const uint32_t q_and = a.scale == 0.0f ? 0u : 0xFFFFFFFFu, q_xor = a.scale < 0.0f ? 0x80008000u : 0u;
 
     auto start = [&] { /* a tile */

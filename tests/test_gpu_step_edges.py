@@ -11,7 +11,7 @@ from paper_2607_18957_gb300 import ops, step
 
 pytestmark = pytest.mark.gpu
 
-BF16 = torch.bfloat16
+BF16, F8 = torch.bfloat16, torch.float8_e4m3fn
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -162,3 +162,32 @@ def test_frequencies_that_want_a_gradient_are_refused():
         cfa.append(qkv, *cache, at, heads=1, positions=at, frequencies=f)
     with torch.no_grad():
         cfa.append(qkv, *cache, at, heads=1, positions=at, frequencies=f)
+
+
+# ---- scales -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cdtype", [BF16, F8])
+def test_scales_below_fp32s_normal_range_of_large_scores(cdtype):
+    """Scores of 2^122 to 2^127 times 2^-127 (over 8-bit keys 2^-57 times 2^-70): probabilities between 0.1
+    and 10 times their mean.  Sums of powers of two are exact; the scale has at least 20 bits there, the
+    values 8: 2^-8 for the result's rounding and 2^-10 for all else."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    heads, kv, dim, keys = 8, 2, 64, 200
+
+    def signs(*shape):
+        return (torch.randint(0, 2, shape, generator=g, device="cuda") * 2 - 1).float()
+    q, k = signs(1, heads, dim), signs(13, 16, kv, dim)
+    v = torch.randn(13, 16, kv, dim, generator=g, device="cuda").to(cdtype)
+    z = torch.einsum("hgd,nhd->hgn", q.view(kv, -1, dim).double(), k.view(-1, kv, dim)[:keys].double()) / 32
+    if cdtype is BF16:
+        q, k, scale, k_scale = q * 2.0 ** 61, k * 2.0 ** 61, 2.0 ** -127, 1.0
+    else:
+        q, k, scale, k_scale = q * 2.0 ** 114, k * 2.0 ** 8, 2.0 ** -57, 2.0 ** -70
+    pages = torch.arange(13, dtype=torch.int32, device="cuda")[None]
+    lengths = torch.tensor([keys], dtype=torch.int32, device="cuda")
+    o, lse = cfa.attend(q.to(BF16), k.to(cdtype), v, pages, lengths, scale=scale, k_scale=k_scale, lse=True)
+    p, v = torch.softmax(z, 2), v.view(-1, kv, dim)[:keys].double()
+    want = torch.einsum("hgn,nhd->hgd", p, v)
+    bound = 2.0 ** -8 * want.abs() + 2.0 ** -10 * torch.einsum("hgn,nhd->hgd", p, v.abs())
+    assert bool(((o.double().view_as(want) - want).abs() <= bound).all())
+    assert (lse.double().view(kv, -1) - torch.logsumexp(z, 2)).abs().max() < 2.0 ** -16
