@@ -842,6 +842,7 @@ cfa_status cfa_append_async(const cfa_append_args *args, cfa_stream stream);
  * out are held in fp32; probabilities enter the second product as sums of two 16-bit values (with BF16 over
  * an 8-bit cache as one F16 value, 2^-11 of it at most off).  In F16, or with an 8-bit cache, those below
  * 2^-28 of a row's largest count as 0.
+ * scale * log2(e), and that times k_scale, are finite in fp32.
  * head_dim is 64, 96, 128 or 256; q, out and the caches lie on the 16-byte grid with all their strides
  * (CFA_ERR_ALIGN).  max_pages * page_size is at most 2^30, new_tokens * heads / kv_heads at most 2^18.  The
  * keys are read once for every 16 rows of a key head (8 with a head_dim of 256), which suits few new tokens.
@@ -882,7 +883,7 @@ cfa_status cfa_attend_async(const cfa_attend_args *args, cfa_stream stream);
  *   logits    [rows, cols] of dtype (BF16, F16 or F32);  tokens [rows]
  *   logprobs, entropy [rows], top_logprobs and top_ids [rows, top], contiguous; the last two NULL with
  *             top 0
- * scale > 0 is the inverse temperature.  Sums are held in fp32.
+ * scale > 0 is the inverse temperature; scale * log2(e) is finite in fp32.  Sums are held in fp32.
  */
 typedef struct cfa_logprobs_args {
     const void *logits;

@@ -16,6 +16,14 @@ uint64_t size_of(int32_t dtype) { return dtype == CFA_DTYPE_F32 ? 4 : 2; }
 
 bool is_value(int32_t dtype) { return is_half(dtype) || dtype == CFA_DTYPE_F32; }
 
+/* Whether a scale of exponents is finite in powers of two as well, times k (infinite, it would make NaN of a
+ * difference of 0). */
+bool exponents_ok(float scale, float k)
+{
+    const float two = scale * 1.4426950408889634f;
+    return std::isfinite(two) && std::isfinite(two * k);
+}
+
 } // namespace
 
 /* ---- norm ---- */
@@ -259,7 +267,7 @@ extern "C" cfa_status cfa_attend_async(const cfa_attend_args *a, cfa_stream stre
         (int64_t)a->max_pages * a->page_size > kMostKeys)
         return refuse(CFA_ERR_INVAL, "cfa_attend: %lld sequences of %d pages of %d, %d in the cache",
                       (long long)a->sequences, a->max_pages, a->page_size, a->cache_pages);
-    if (a->window < 0 || a->window > kMostKeys || a->flags || !std::isfinite(a->scale))
+    if (a->window < 0 || a->window > kMostKeys || a->flags || !exponents_ok(a->scale, a->k_scale))
         return refuse(CFA_ERR_INVAL, "cfa_attend: window %d, scale %g, flags %u", a->window, a->scale,
                       a->flags);
     const int64_t slots = (int64_t)a->max_pages * a->page_size / 32 + 1;
@@ -340,7 +348,7 @@ extern "C" cfa_status cfa_logprobs_async(const cfa_logprobs_args *a, cfa_stream 
                       (long long)a->cols);
     if (a->top < 0 || a->top > CFA_LOGPROBS_MAX_TOP || a->top > a->cols)
         return refuse(CFA_ERR_INVAL, "cfa_logprobs: top %d of %lld", a->top, (long long)a->cols);
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || a->flags)
+    if (!(a->scale > 0.0f) || !exponents_ok(a->scale, 1.0f) || a->flags)
         return refuse(CFA_ERR_INVAL, "cfa_logprobs: scale %g, flags %u", a->scale, a->flags);
     if (a->rows > 1 && (a->stride < a->cols || a->stride >= kMost))
         return refuse(CFA_ERR_INVAL, "cfa_logprobs: row stride %lld of rows of %lld",

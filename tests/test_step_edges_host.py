@@ -97,3 +97,32 @@ def test_a_foreign_handle_may_name_another_stream_by_now(monkeypatch):
         call(0x10000 + 16 * i, 1)
     assert log == [("waits", 0x10000 + 16 * 63, 0), ("kept for", 0x10000 + 16 * 63, 20)]
     assert len(step._FOREIGN) == 64 and (0, 0x1000) not in step._FOREIGN
+
+
+P, MIB, INVAL = 0x7F0000000000, 1 << 20, -1
+
+
+@pytest.mark.parametrize("scale", [2.3e38, 2.4e38, 3.4e38])
+def test_logprobs_scale_has_room_in_powers_of_two(scale):
+    """The kernel's exponents are of 2: scale * log2(e) is finite, or the call is refused."""
+    lib = _library()
+    args = step._LOGPROBS.pack(P, P + 8 * MIB, P + 9 * MIB, P + 10 * MIB, 0, 0, 0, 100, 100,
+                               cfa._lib.DTYPE["f32"], 0, scale, 0)
+    assert lib.cfa_logprobs_async(args, None) == (0 if scale < 2.35e38 else INVAL)
+
+
+@pytest.mark.parametrize("scale,k_scale,ok", [(2.3e38, 1.0, True), (-2.4e38, 1.0, False), (1e30, 1e9, False),
+                                              (1e20, 1e17, True), (3e38, 0.1, False)])
+def test_attend_scales_have_room_in_powers_of_two(scale, k_scale, ok):
+    """scale * log2(e), and that times the keys' scale."""
+    lib = _library()
+    f8 = step.F8_E4M3 if k_scale != 1.0 else cfa._lib.DTYPE["bf16"]
+    args = step._ATTEND.pack(P, P + 8 * MIB, P + 16 * MIB, P + MIB, P + 2 * MIB, P + 3 * MIB, 0, P + 64 * MIB,
+                             64 * MIB, 0, 256, 256, 4, 2048, 128, 64, 2048, 128, 64, 1, 4, 8, 16, 4, 2, 64, 0,
+                             cfa._lib.DTYPE["bf16"], f8, 0, scale, k_scale, 1.0)
+    assert lib.cfa_attend_async(args, None) == (0 if ok else INVAL)
+
+
+def _library():
+    cfa_build.build()
+    return cfa._lib.load()
