@@ -38,6 +38,7 @@ class Step:
         f, self.magnitude = cfa.rotary_frequencies(dim, 500000.0, scaling="bands", factor=8.0, length=8192)
         self.frequencies = torch.tensor(f, dtype=torch.float64, device="cuda")
         self.tokens = torch.zeros(lengths.shape, dtype=torch.int32, device="cuda")
+        self.none = torch.full_like(self.tokens, -1)
 
     def rotary(self, positions):
         return dict(positions=positions, frequencies=self.frequencies, magnitude=self.magnitude)
@@ -50,7 +51,9 @@ class Step:
         cfa.append(qkv, self.k, self.v, slots, heads=self.heads, **self.rotary(positions))
 
     def __call__(self, slots):
-        """(logits, log probabilities of the tokens chosen, entropy, the best, their ids)"""
+        """(logits, log probabilities of the tokens chosen, entropy, the best, their ids)
+
+        The tokens chosen, which the next step takes in, are the best ones: none are given beforehand."""
         p, mlp, attn = self.p, LAYER + "mlp.", LAYER + "self_attn."
         x = p["model.embed_tokens.weight"][self.tokens]
         h = cfa.norm(x, p[LAYER + "input_layernorm.weight"])
@@ -63,7 +66,8 @@ class Step:
         m = cfa.linear(m, p[mlp + "down_proj.weight"])
         h, _ = cfa.norm(m, p["model.norm.weight"], residual=x)
         logits = cfa.linear(h, p["lm_head.weight"], out_dtype="f32")
-        return (logits, *cfa.logprobs(logits, self.tokens, top=TOP))
+        _, entropy, best, ids = cfa.logprobs(logits, self.none, top=TOP)
+        return logits, best[:, 0], entropy, best, ids
 
 
 def reference(w, tokens, heads, kv_heads, dim, frequencies):
@@ -90,7 +94,7 @@ def reference(w, tokens, heads, kv_heads, dim, frequencies):
 
 
 def run(sequences=5, hidden=512, steps=2, seed=0, graph=True):
-    """For each step the operators' results and the logits in 64 bits."""
+    """For each step the operators' results, the logits in 64 bits and the tokens chosen."""
     dim, vocab = 64, 1000
     heads, kv_heads = hidden // dim, max(1, hidden // dim // 4)
     m = dense_config("decode_step", seed, layers=1, hidden=hidden, n_q=heads, n_kv=kv_heads, head_dim=dim,
@@ -155,18 +159,17 @@ def run(sequences=5, hidden=512, steps=2, seed=0, graph=True):
     f = step.frequencies.cpu()
     wanted = [[None if s == padded else reference(w, told[s][:len(told[s]) - steps + i], heads, kv_heads, dim,
                                                   f) for s in range(sequences)] for i in range(steps)]
-    given = [[t[len(t) - steps + i - 1].item() for t in told] for i in range(steps)]
-    return found, wanted, given
+    chosen = [[t[len(t) - steps + i].item() for t in told] for i in range(steps)]
+    return found, wanted, chosen
 
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     for name, default in (("sequences", 5), ("hidden", 512), ("steps", 2)):
         ap.add_argument("--" + name, type=int, default=default)
-    results, expected, _ = run(**vars(ap.parse_args()))
-    for n, (r, e) in enumerate(zip(results, expected)):
+    for n, (r, e, tokens) in enumerate(zip(*run(**vars(ap.parse_args())))):
         for s, z in enumerate(e):
             if z is not None:
                 off = ((r[0][s].double() - z).norm() / z.norm()).item()
-                print(f"step {n} sequence {s}: best token {r[4][s, 0].item()}, log probability "
-                      f"{r[3][s, 0].item():.4f}, relative difference of the logits from 64 bits {off:.2e}")
+                print(f"step {n} sequence {s}: token {tokens[s]}, log probability {r[1][s].item():.4f}, "
+                      f"relative difference of the logits from 64 bits {off:.2e}")

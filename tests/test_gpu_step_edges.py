@@ -191,3 +191,16 @@ def test_scales_below_fp32s_normal_range_of_large_scores(cdtype):
     bound = 2.0 ** -8 * want.abs() + 2.0 ** -10 * torch.einsum("hgn,nhd->hgd", p, v.abs())
     assert bool(((o.double().view_as(want) - want).abs() <= bound).all())
     assert (lse.double().view(kv, -1) - torch.logsumexp(z, 2)).abs().max() < 2.0 ** -16
+
+
+# ---- the example --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_example_gives_the_log_probabilities_of_the_tokens_chosen(graph):
+    """Of those that the next step takes in: the likeliest."""
+    from examples import decode_step
+    found, _, chosen = decode_step.run(sequences=4, hidden=256, steps=4, graph=graph)
+    for (logits, lp, _, best, ids), tokens in zip(found, chosen):
+        assert tokens == ids[:, 0].tolist() and torch.equal(lp, best[:, 0])
+        z = torch.log_softmax(logits.double(), 1).gather(1, torch.tensor(tokens)[:, None])[:, 0]
+        assert (lp - z).abs().max() < 2.0 ** -15  # fp32, as the sums of test_gpu_decode.py
