@@ -153,6 +153,8 @@ def rotary_frequencies(dim, base=10000.0, *, scaling=None, factor=1.0, length=No
         if not length:
             raise ValueError(f"scaling {scaling!r} goes by the length of the original contexts")
         if scaling == "bands":
+            if not low < high:
+                raise ValueError(f"low {low} turns, high {high}")
             kept = [(length * v / (2 * math.pi) - low) / (high - low) for v in f]
         else:
             def index(turns):

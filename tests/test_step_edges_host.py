@@ -37,6 +37,14 @@ def test_ramp_leaves_pairs_that_turn_often_alone():
     assert f[63] == pytest.approx(10000.0 ** (-63 / 64) * (7 / 25 + 18 / 25 / 8), rel=1e-12, abs=0.0)
 
 
+@pytest.mark.parametrize("low,high", [(1.0, 1.0), (4.0, 1.0), (1.0, math.nan)])
+def test_bands_that_are_none_are_refused(low, high):
+    """Between low and high turns the frequencies pass over: the other way round they would be divided
+    where they are to be kept."""
+    with pytest.raises(ValueError, match="low .*high"):
+        cfa.rotary_frequencies(64, scaling="bands", factor=2.0, length=4096, low=low, high=high)
+
+
 class FakeStream:
     """torch's current stream: a foreign one's id is its handle."""
     device = "somewhere"
