@@ -836,12 +836,13 @@ cfa_status cfa_append_async(const cfa_append_args *args, cfa_stream stream);
  *   lengths   [sequences]: keys of each, the new tokens' among them; below 0 counts as 0, above max_pages *
  *             page_size as that
  *   workspace device memory of cfa_attend_workspace() bytes, 256-byte aligned; calls that may overlap
- *             need their own.  Its size goes by the head_dim and the heads alone
+ *             need their own.  Its size goes by the head_dim, the heads and new_tokens alone
  * A row that sees no key gets 0 and -inf; so does one whose scores all are -inf.  Whatever lies in
  * keys and values that a row does not see, NaN included, does not come into it.  Scores, maxima, sums and
  * out are held in fp32; probabilities enter the second product as sums of two 16-bit values (with BF16 over
  * an 8-bit cache as one F16 value, 2^-11 of it at most off).  In F16, or with an 8-bit cache, those below
- * 2^-28 of a row's largest count as 0.
+ * 2^-28 of a row's largest are rounded to multiples of 2^-38 of it (an infinite value makes NaN where the
+ * one or the other of the two comes out as 0).
  * scale * log2(e), and that times k_scale, are finite in fp32.
  * head_dim is 64, 96, 128 or 256; q, out and the caches lie on the 16-byte grid with all their strides
  * (CFA_ERR_ALIGN).  max_pages * page_size is at most 2^30, new_tokens * heads / kv_heads at most 2^18.  The

@@ -193,6 +193,27 @@ def test_scales_below_fp32s_normal_range_of_large_scores(cdtype):
     assert (lse.double().view(kv, -1) - torch.logsumexp(z, 2)).abs().max() < 2.0 ** -16
 
 
+@pytest.mark.parametrize("dtype,cdtype,score,value", [(torch.float16, torch.float16, -22.875, 60000.0),
+                                                      (BF16, F8, -22.0, 448.0), (BF16, BF16, -60.0, 2.0 ** 60)])
+def test_probabilities_far_below_the_largest(dtype, cdtype, score, value):
+    """One key that takes nearly all with values of 0, a thousand of e^-22.9 or e^-22 of it (2^-33, 2^-32),
+    which in fp16 are multiples of 2^-38 of the largest: off by 2^-39 of it each.  bf16 over bf16
+    has no such floor.  The rest is fp32's, 2^-10 for it, and the result's rounding."""
+    keys, dim = 1001, 64
+    k, v = (torch.zeros(63, 16, 1, dim, device="cuda", dtype=cdtype) for _ in range(2))
+    k.view(-1, dim)[1:, 0], v.view(-1, dim)[1:] = score, value
+    q = torch.zeros(1, 1, dim, device="cuda", dtype=dtype)
+    q[..., 0] = 1.0
+    pages = torch.arange(63, dtype=torch.int32, device="cuda")[None]
+    lengths = torch.tensor([keys], dtype=torch.int32, device="cuda")
+    o = cfa.attend(q, k, v, pages, lengths, scale=1.0).double()
+    n = keys - 1
+    want = n * math.exp(score) * value / (1 + n * math.exp(score))
+    floor = 0.0 if cdtype is BF16 else n * value * 2.0 ** -39
+    bound = floor + want * 2.0 ** -10 + want * (2.0 ** -8 if dtype is BF16 else 2.0 ** -11)
+    assert bool(((o - want).abs() <= bound).all()) and floor < want / 8
+
+
 # ---- the example --------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("graph", [False, True])
