@@ -177,7 +177,8 @@ __device__ __forceinline__ float2 unpack2(__half, uint32_t v)
 
 /* Probabilities enter the second product as sums of two 16-bit values: rounded to one alone they would put
  * the result off by as much as its own rounding does.  The first is cut off at least one of its units
- * below the probability, so that neither is 0 or negative and an infinite value stays what it is. */
+ * below the probability, so that neither is 0 or negative and an infinite value stays what it is (fp16: for
+ * probabilities from 2^-28 of the largest on, whose cut is still one of its units). */
 template <int UNIT> __device__ __forceinline__ float below(float v)
 {
     const uint32_t b = __float_as_uint(v);
@@ -197,7 +198,8 @@ __device__ __forceinline__ uint32_t split(__half, float x, float y, uint32_t &lo
     const __half2 v = __halves2half2(a, b);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-/* All probabilities and their sums are held 2^kUp times as large: fp16 has no smaller ones than 2^-24. */
+/* All probabilities and their sums are held 2^kUp times as large: fp16 has no smaller ones than 2^-24, nor
+ * all of its bits below 2^-14. */
 template <typename P> constexpr float kUp = 0.0f;
 template <> constexpr float kUp<__half> = 14.0f;
 
