@@ -107,8 +107,8 @@ class _On:
         if isinstance(stream, int):
             # torch takes the handle 0 for a request of one of its own streams, and does not know 1
             # (cudaStreamLegacy): both are the default stream
-            handle, stream = stream, (torch.cuda.ExternalStream(stream, device=device) if stream > 1 else
-                                      torch.cuda.default_stream(device))
+            handle, stream = stream, (torch.cuda.default_stream(device) if stream in (0, 1) else
+                                      torch.cuda.ExternalStream(stream, device=device))
             if handle == PER_THREAD:
                 # One handle, a stream in every thread: torch's allocator would give a thread what
                 # another's kernels still use.  A stream of torch's stands in for the thread's own.

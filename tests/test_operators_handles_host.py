@@ -50,7 +50,8 @@ def log(monkeypatch):
     return done
 
 
-@pytest.mark.parametrize("handle,name", [(0, "default on 3"), (1, "default on 3"), (4096, "4096 on 3")])
+@pytest.mark.parametrize("handle,name", [(0, "default on 3"), (1, "default on 3"), (4096, "4096 on 3"),
+                                         (-1, "-1 on 3")])
 def test_handles_name_their_streams(log, handle, name):
     """0 and cudaStreamLegacy are the default stream."""
     with ops._elsewhere(handle, 3):
